@@ -470,6 +470,195 @@ int md_kv_gather(const md_kv_cache* dst, const md_kv_cache* src, const int32_t* 
                  int32_t* dst_lens, void* stream);
 
 /*
+ * ---- The 4-bit KV cache ----
+ *
+ * A copy of a KV cache in the OCP microscaling format MXFP4, for drafting over the
+ * whole context at a fraction of its bytes (136 against 512 a token and head, d =
+ * 128, bf16): 32 consecutive channels of one (token, head) row share a scale byte
+ * s, each holds a 4-bit code, and a value is E2M1(code) * 2^(s - 127), exact in
+ * bf16 (infinite from 2^128 on); s = 255 makes all 32 values NaN.  E2M1: bit 3 the
+ * sign, bits 0..2 the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ *
+ * Row (blk, tok, hk), blk and tok as in md_attn_args, has its d / 2 code bytes at
+ * byte blk*stride_blk + tok*stride_tok + hk*stride_head of k (v), channel c in
+ * the low (c even) or high half of byte c / 2, and its d / 32 scale bytes at that
+ * offset / 16 of k_scale (v_scale).  The scales' layout thus follows the codes'.
+ * Any layout of whole rows works; [block][head][token] (stride_tok = d / 2)
+ * reads fastest: a head's tokens are then contiguous.
+ */
+typedef struct {
+  int32_t num_seqs;           /* B >= 0 */
+  int32_t num_kv_heads;       /* Hkv >= 1 */
+  int32_t head_dim;           /* d in {64, 128} */
+  void* k;                    /* codes; 16-byte aligned */
+  void* v;
+  void* k_scale;              /* scales; aligned to d / 32 bytes */
+  void* v_scale;
+  int64_t stride_blk, stride_tok, stride_head;  /* BYTES of codes, multiples of d / 2 */
+  int32_t page_size;          /* 0 = contiguous, else tokens per page (power of two) */
+  int32_t max_pages_per_seq;  /* columns of page_table (paged only) */
+  int64_t num_pages;          /* pages in the pool (paged only) */
+  const int32_t* page_table;  /* device [B, max_pages_per_seq], or NULL when contiguous */
+  int32_t capacity;           /* contiguous: tokens each sequence's block holds (>= 1);
+                                 paged: ignored (max_pages_per_seq * page_size) */
+} md_kv4_cache;
+
+/*
+ * Round n_new tokens' K and V rows of every sequence into the cache; arguments as
+ * md_kv_append (dtype: md_dtype of the rows).  Per 32 channels, a = max |x|:
+ *   scale 2^e, the smallest with a / 2^e < 7, i.e. e = floor(log2(8 a / 7)) - 2,
+ *   clamped to [-125, 125] (a = 0: e = -125);
+ *   code  the value nearest to x / 2^e, ties to the even code, 6 at most.
+ * (7 rounds to 6 or, one scale up, to 4 * 2 with the same error, so nothing else is
+ * cut off before the top of the range.)  A NaN or an infinity among the 32 makes them
+ * NaN: scale 255, codes 0.
+ * Positions past the capacity (or the table), and pages outside [0, num_pages),
+ * are not written.
+ * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers, bad sizes or strides,
+ * a bad dtype, n_new < 0, lens_out overlapping pos0; MD_ERR_UNSUPPORTED for
+ * head_dim not in {64,128}, a token stride over 2^25 bytes or B * n_new * Hkv >
+ * 2^31 - 1; MD_ERR_HIP.
+ */
+int md_kv4_append(const md_kv4_cache* c, int32_t n_new, int32_t dtype, const void* k_new,
+                  const void* v_new, const int32_t* pos0, int32_t* lens_out, void* stream);
+
+/*
+ * The values of n tokens' rows of every sequence, positions pos0[b] .. pos0[b] + n
+ * - 1 (md_kv4_append's inverse, but for the rounding):
+ *   k_out, v_out  device [B, n, Hkv, d] out, contiguous, dtype MD_F32 or MD_BF16
+ *                 (the values are exact in both), 16-byte aligned
+ * Rows at positions outside the cache, and on pages outside [0, num_pages), are zeros.
+ * Errors as md_kv4_append.
+ */
+int md_kv4_read(const md_kv4_cache* c, int32_t n, int32_t dtype, const int32_t* pos0, void* k_out,
+                void* v_out, void* stream);
+
+/* Attention over a 4-bit cache: the fields and conventions of md_attn_args. */
+typedef struct {
+  int32_t q_len;              /* L in [1, 16]; G * L <= 64 */
+  int32_t num_q_heads;        /* Hq, a multiple of the cache's num_kv_heads */
+  int32_t dtype;              /* md_dtype of q and o */
+  float sm_scale;             /* <= 0: 1/sqrt(d) */
+  const void* q;              /* [B, L, Hq, d], contiguous, 16-byte aligned */
+  const int32_t* kv_lens;     /* device [B], the L tokens of the call included */
+  int32_t max_kv_len;         /* HOST bound on every kv_lens[b] */
+  void* o;                    /* [B, L, Hq, d], dtype of q, 16-byte aligned */
+  float* lse;                 /* [B, L, Hq] or NULL */
+  void* workspace;            /* >= md_kv4_workspace_bytes(), 256-byte aligned, any contents */
+  size_t workspace_bytes;
+} md_kv4_attn_args;
+
+/*
+ * md_verify_attn's and md_draft_attn's attention with K and V read from a 4-bit
+ * cache: over the whole context, or over the first n_sink tokens and each query's
+ * last `window` positions.  Scores are products with the cache's exact values;
+ * softmax and sums are fp32, with fp32 queries throughout, with bf16 ones the
+ * softmax weights are rounded to bf16 before they multiply V (lse is not).
+ * A query that sees no key gets o = 0, lse = -inf.  A NaN or infinity in a row
+ * of K or V reaches only the queries that see that row.  kv_lens[b] is clamped to
+ * [0, max_kv_len]; tokens on pages outside [0, num_pages) are not dereferenced, and
+ * the queries that see them get unspecified results.
+ * Errors: MD_ERR_INVALID_ARG and MD_ERR_UNSUPPORTED as md_verify_attn,
+ * md_draft_attn and md_kv4_append (a contiguous cache must hold max_kv_len tokens);
+ * MD_ERR_WORKSPACE; MD_ERR_HIP.
+ */
+int md_kv4_verify_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, void* stream);
+int md_kv4_draft_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int32_t n_sink,
+                      int32_t window, void* stream);
+
+/* Workspace bytes of these calls (mode MD_MODE_VERIFY or MD_MODE_DRAFT; n_sink and
+ * window for the latter): host arithmetic on the sizes and the current device's
+ * compute units; 0 where none is needed and for malformed arguments.  A buffer for
+ * a max_kv_len serves every smaller one. */
+size_t md_kv4_workspace_bytes(const md_kv4_cache* c, const md_kv4_attn_args* a, int32_t mode,
+                              int32_t n_sink, int32_t window);
+
+/*
+ * ---- Sampled acceptance ----
+ *
+ * Verification of drafted tokens against the target's probabilities, from given random
+ * numbers (speculative sampling: the tokens are distributed as the target's own).
+ * Per sequence b, with L = n_draft + 1:
+ *   accepted[b] = a, the length of the leading run of i < n_draft with
+ *                 u[b][i] * q_i(d_i) < p_i(d_i), where d_i = draft[b][i], p_i =
+ *                 target_probs[b][i], q_i = draft_probs[b][i], or without draft_probs
+ *                 (drafts chosen, not sampled) 1 at d_i and 0 elsewhere.  A draft
+ *                 outside [0, vocab) is not accepted;
+ *   r           = max(p_a - q_a, 0) where a < n_draft, p_a where a = n_draft; p_a if
+ *                 these are all 0;
+ *   t           = the least token with r(0) + .. + r(t) > u[b][n_draft] * sum r, or the
+ *                 last one with r > 0 if there is none such (u >= 1); 0 if p_a is all 0;
+ *   tokens[b]   = d_0 .. d_{a-1}, t, then -1: as md_greedy_accept, for md_kv_commit.
+ * Rows need not sum to 1.  A probability that is negative, NaN or infinite counts
+ * as 0.  Products and sums are 64-bit.
+ *   target_probs  device [B, L, vocab] in dtype (MD_F32 or MD_BF16), contiguous
+ *   draft_probs   device [B, n_draft, vocab] in dtype, or NULL
+ *   draft         device int32 [B, n_draft]
+ *   u             device fp32 [B, L], uniform in [0, 1): entry n_draft draws t
+ *   accepted      device int32 [B] out
+ *   tokens        device int32 [B, L] out
+ *   workspace     >= md_spec_accept_workspace_bytes(), 256-byte aligned, any contents
+ * Only the rows p_a and q_a are read whole.  Errors: MD_ERR_INVALID_ARG for NULL or
+ * misaligned pointers (probabilities: their element size), n_draft outside [0, 1023],
+ * vocab outside [1, 2^30], a bad dtype; MD_ERR_UNSUPPORTED for num_seqs > 2^25 - 1;
+ * MD_ERR_WORKSPACE; MD_ERR_HIP.
+ */
+int md_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype,
+                   const void* target_probs, const void* draft_probs, const int32_t* draft,
+                   const float* u, int32_t* accepted, int32_t* tokens, void* workspace,
+                   size_t workspace_bytes, void* stream);
+size_t md_spec_accept_workspace_bytes(int32_t num_seqs, int32_t n_draft, int32_t vocab);
+
+/*
+ * ---- Queries and keys of a step ----
+ *
+ * RMS norm of every query and key head and the rotation by position, in one pass
+ * from the projections to what the attention reads, and the new K and V rows into
+ * the cache in the same pass.  Per row x (one token's head):
+ *   y = norm ? x / sqrt(mean(x^2) + eps) * weight : x
+ *   pairs (y1, y2) = (y1 cos t - y2 sin t, y2 cos t + y1 sin t), t = position *
+ *   inv_freq[j], over the first rot_dim channels: pair j is (j, j + rot_dim / 2), or
+ *   (2j, 2j + 1) where interleaved; channels from rot_dim on are not turned.
+ * Position of row i of sequence b: pos0[b] + i.  Arithmetic is fp32, angles are
+ * reduced in 64 bits (exact to far positions), results are rounded once.
+ */
+typedef struct {
+  int32_t num_seqs;           /* B >= 0 */
+  int32_t n_new;              /* tokens a sequence, >= 0 */
+  int32_t num_q_heads, num_kv_heads;  /* >= 1 */
+  int32_t head_dim;           /* d in {64, 128} */
+  int32_t dtype;              /* md_dtype of every tensor but inv_freq */
+  int32_t norm;               /* 0: rotation only (weights NULL), else RMS norm */
+  float eps;                  /* >= 0 */
+  const void* q_weight;       /* device [d], or NULL: ones */
+  const void* k_weight;
+  int32_t rot_dim;            /* a multiple of 16 in [0, d] */
+  int32_t interleaved;
+  const float* inv_freq;      /* device fp32 [rot_dim / 2] */
+  const void* q;              /* row (b, i, h) at b*q_stride_seq + i*q_stride_tok + h*d */
+  const void* k_new;          /* the same; strides are elements, multiples of 16 bytes */
+  const void* v_new;          /* read where a cache is given, else NULL */
+  int64_t q_stride_seq, q_stride_tok;
+  int64_t k_stride_seq, k_stride_tok;
+  int64_t v_stride_seq, v_stride_tok;
+  const int32_t* pos0;        /* device int32 [B] */
+  void* q_out;                /* [B, n_new, Hq, d] contiguous; may be q itself (in place) */
+  void* k_out;                /* [B, n_new, Hkv, d] contiguous, or NULL with a cache; may be k_new */
+  int32_t* lens_out;          /* device int32 [B] or NULL: pos0[b] + n_new */
+} md_qk_norm_rope_args;
+
+/*
+ * cache: NULL, or the cache that takes the K rows (normed and rotated) and the V rows (as
+ * they are) at positions pos0[b] + i, with md_kv_append's bounds.
+ * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers (weights and inv_freq: 16
+ * and 4 bytes), bad sizes or strides, neither cache nor k_out, a v_new without or a cache
+ * without a v_new, a cache of other sizes, q_out or k_out that overlaps an input in any other way
+ * than being q or k_new itself, lens_out overlapping pos0; MD_ERR_UNSUPPORTED
+ * for head_dim not in {64,128} or B * n_new > 2^31 - 1; MD_ERR_HIP.
+ */
+int md_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* cache, void* stream);
+
+/*
  * ---- Speculative-decoding cost model (Sec. 3.1 Eq. 1-2; Sec. 4.1 Eq. 3-4) ----
  *
  * Host-only arithmetic (no device, no stream), for choosing the speculation

@@ -15,6 +15,13 @@ CPU fallback: if the library is missing, every call raises.
     md_kv_commit(lens, accepted, q_len, ...)      (in place)
     md_streaming_list(prompt_lens, Hkv, n_sink, window) -> (idx, idx_len)
     md_kv_gather(dst_k, dst_v, src_k, src_v, idx, idx_len, src_lens, ...) -> dst_lens
+    kv4_empty(blocks, tokens, Hkv, d)             -> Kv4Cache (a 4-bit KV cache)
+    md_kv4_append(cache, k_new, v_new, pos0, ...) -> lens_out
+    md_kv4_read(cache, pos0, n, ...)              -> (k, v)
+    md_kv4_verify_attn(q, cache, kv_lens, ...)    -> (o, lse)
+    md_kv4_draft_attn(q, cache, kv_lens, n_sink, window, ...) -> (o, lse)
+    md_spec_accept(target_probs, draft_probs, draft, u, ...) -> (accepted, tokens)
+    md_qk_norm_rope(q, k_new, pos0, inv_freq, ...) -> (q_out, k_out, lens_out)
     md_sd_expected_tokens / md_sd_latency_ratio / md_sd_best_gamma /
     md_sd_alpha_from_omega                        (host-only cost model, Eq. 1-4)
 
@@ -27,7 +34,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from typing import Optional
+from typing import Any, NamedTuple, Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmagicdec.so")
@@ -44,7 +51,9 @@ EXPORTED = ["md_verify_attn", "md_draft_attn", "md_draft_attn_indexed", "md_merg
             "md_streaming_list", "md_kv_gather", "md_sd_expected_tokens", "md_sd_latency_ratio",
             "md_sd_best_gamma", "md_sd_alpha_from_omega",
             "md_status_str", "md_last_hip_error", "md_attn_args_size",
-            "md_attn_noalloc",
+            "md_attn_noalloc", "md_kv4_append", "md_kv4_read", "md_kv4_verify_attn",
+            "md_kv4_draft_attn", "md_kv4_workspace_bytes", "md_spec_accept",
+            "md_spec_accept_workspace_bytes", "md_qk_norm_rope",
             "md_bench_stream_read", "md_bench_evict", "md_bench_copy", "md_bench_fill",
             "md_bench_attn_stamps"]
 MD_NOALLOC_SCRATCH_BYTES = 33 << 20
@@ -99,6 +108,49 @@ class MdKvCache(ctypes.Structure):
     ]
 
 
+class MdKv4Cache(ctypes.Structure):
+    """Mirror of ``md_kv4_cache``."""
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("stride_blk", ctypes.c_int64), ("stride_tok", ctypes.c_int64),
+        ("stride_head", ctypes.c_int64),
+        ("page_size", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("num_pages", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+        ("capacity", ctypes.c_int32),
+    ]
+
+
+class MdKv4AttnArgs(ctypes.Structure):
+    """Mirror of ``md_kv4_attn_args``."""
+    _fields_ = [
+        ("q_len", ctypes.c_int32), ("num_q_heads", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("sm_scale", ctypes.c_float), ("q", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p),
+        ("max_kv_len", ctypes.c_int32), ("o", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class MdQkNormRopeArgs(ctypes.Structure):
+    """Mirror of ``md_qk_norm_rope_args``."""
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("n_new", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+        ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+        ("inv_freq", ctypes.c_void_p),
+        ("q", ctypes.c_void_p), ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p),
+        ("q_stride_seq", ctypes.c_int64), ("q_stride_tok", ctypes.c_int64),
+        ("k_stride_seq", ctypes.c_int64), ("k_stride_tok", ctypes.c_int64),
+        ("v_stride_seq", ctypes.c_int64), ("v_stride_tok", ctypes.c_int64),
+        ("pos0", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+        ("lens_out", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -146,6 +198,23 @@ def load_library(path: str = LIB_PATH):
     lib.md_kv_gather.argtypes = [ctypes.POINTER(MdKvCache), ctypes.POINTER(MdKvCache), vp, i32,
                                  vp, vp, vp, vp]
     lib.md_kv_gather.restype = ctypes.c_int
+    kv4_p, kv4_args_p = ctypes.POINTER(MdKv4Cache), ctypes.POINTER(MdKv4AttnArgs)
+    lib.md_kv4_append.argtypes = [kv4_p, i32, i32, vp, vp, vp, vp, vp]
+    lib.md_kv4_append.restype = ctypes.c_int
+    lib.md_kv4_read.argtypes = [kv4_p, i32, i32, vp, vp, vp, vp]
+    lib.md_kv4_read.restype = ctypes.c_int
+    lib.md_kv4_verify_attn.argtypes = [kv4_p, kv4_args_p, vp]
+    lib.md_kv4_verify_attn.restype = ctypes.c_int
+    lib.md_kv4_draft_attn.argtypes = [kv4_p, kv4_args_p, i32, i32, vp]
+    lib.md_kv4_draft_attn.restype = ctypes.c_int
+    lib.md_kv4_workspace_bytes.argtypes = [kv4_p, kv4_args_p, i32, i32, i32]
+    lib.md_kv4_workspace_bytes.restype = sz
+    lib.md_spec_accept.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.md_spec_accept.restype = ctypes.c_int
+    lib.md_spec_accept_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.md_spec_accept_workspace_bytes.restype = sz
+    lib.md_qk_norm_rope.argtypes = [ctypes.POINTER(MdQkNormRopeArgs), ctypes.POINTER(MdKvCache), vp]
+    lib.md_qk_norm_rope.restype = ctypes.c_int
     f64 = ctypes.c_double
     lib.md_sd_expected_tokens.argtypes = [i32, f64]
     lib.md_sd_expected_tokens.restype = f64
@@ -207,6 +276,29 @@ def _stream_scoped(fn):
     return wrapped
 
 
+def _device_scoped(fn):
+    """_stream_scoped, with the device of the call's first argument (a tensor or a
+    Kv4Cache) as the current one: the library takes its plans and its launches to
+    the current device."""
+    scoped = _stream_scoped(fn)
+
+    @functools.wraps(fn)
+    def wrapped(first, *args, **kw):
+        t = first[0] if isinstance(first, tuple) else first
+        dev = t.get_device()
+        if dev < 0:
+            raise ValueError(f"tensors must be on a GPU, not {t.device}")
+        stream = kw.get("stream")
+        if stream is not None and stream.device.index != dev:
+            raise ValueError(f"stream is on {stream.device}; the call runs on {t.device}")
+        torch = _torch()
+        if torch.cuda.current_device() == dev:
+            return scoped(first, *args, **kw)
+        with torch.cuda.device(dev):
+            return scoped(first, *args, **kw)
+    return wrapped
+
+
 def _stream_handle(t, stream):
     """The HIP stream of a call on t's device: `stream`, else the current one
     (read without building a Stream object where torch offers that)."""
@@ -221,6 +313,10 @@ def _stream_handle(t, stream):
 
 def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _on_gpu(ref, **tensors):
@@ -734,6 +830,305 @@ def md_kv_gather(dst_k, dst_v, src_k, src_v, idx, idx_len, src_lens, *, dst_page
     return dst_lens
 
 
+class Kv4Cache(NamedTuple):
+    """A KV cache in 4 bits (see include/magicdec.h).  k, v: uint8 codes, two a
+    byte, [B, S_alloc, Hkv, d / 2], or paged [P, page_size, Hkv, d / 2];
+    k_scale, v_scale: uint8 [.., Hkv, d / 32], the scale of each 32 channels.  Any
+    strides of whole rows; the scales' are the codes' / 16."""
+    k: Any
+    v: Any
+    k_scale: Any
+    v_scale: Any
+
+
+def kv4_empty(blocks, tokens, num_kv_heads, head_dim, device="cuda") -> Kv4Cache:
+    """An uninitialised cache of `blocks` sequences (or pages) of `tokens` tokens in the
+    layout that reads fastest: a head's tokens are contiguous in memory."""
+    torch = _torch()
+
+    def empty(width):
+        return torch.empty((blocks, num_kv_heads, tokens, width), dtype=torch.uint8,
+                           device=device).transpose(1, 2)
+    return Kv4Cache(empty(head_dim // 2), empty(head_dim // 2), empty(head_dim // 32),
+                    empty(head_dim // 32))
+
+
+def make_kv4_cache(cache, *, num_seqs=None, page_table=None) -> MdKv4Cache:
+    """Fill md_kv4_cache from the cache's tensors (no data is read or moved)."""
+    torch = _torch()
+    k, v, ks, vs = cache
+    shape, st, u8 = k.shape, k.stride(), torch.uint8
+    if len(shape) != 4 or v.shape != shape or v.stride() != st or st[3] != 1:
+        raise ValueError("cache k and v must be 4-D with equal shapes and strides, codes unit-stride")
+    if k.dtype != u8 or v.dtype != u8 or ks.dtype != u8 or vs.dtype != u8:
+        raise ValueError("a 4-bit cache's tensors are uint8")
+    half = shape[3]
+    if half % 16 or ks.shape != shape[:3] + (half // 16,) or vs.shape != ks.shape:
+        raise ValueError("k_scale and v_scale must be [.., d / 32] for codes [.., d / 2]")
+    gpu = k.get_device()
+    if gpu < 0 or v.get_device() != gpu or ks.get_device() != gpu or vs.get_device() != gpu or (
+            page_table is not None and page_table.get_device() != gpu):
+        _on_gpu(k, v=v, k_scale=ks, v_scale=vs, page_table=page_table)
+    # A dimension of size one has no stride of its own; every other one is the codes' / 16.
+    for t in (ks, vs):
+        for n, a, b in zip(shape, st, t.stride()[:3]):
+            if n > 1 and a != 16 * b:
+                raise ValueError("the scales' strides must be the codes' / 16")
+        if half > 16 and t.stride(3) != 1:
+            raise ValueError("the scales of a row must be contiguous")
+    page = max_pages = pages = cap = 0
+    pt = None
+    if page_table is None:
+        B, cap = shape[0] if num_seqs is None else num_seqs, shape[1]
+        if B > shape[0]:
+            raise ValueError("a contiguous cache must hold num_seqs sequences")
+    else:
+        if page_table.dtype != torch.int32 or not page_table.is_contiguous() or page_table.dim() != 2:
+            raise ValueError("page_table must be contiguous int32 [B, max_pages]")
+        B = page_table.shape[0] if num_seqs is None else num_seqs
+        if page_table.shape[0] < B:
+            raise ValueError("page_table must have a row per sequence")
+        page, max_pages, pages = shape[1], page_table.shape[1], shape[0]
+        pt = page_table.data_ptr()
+    # The stride of a dimension of size one is never used, but must be a whole row's.
+    sb, stok, sh = (x if n > 1 else half for n, x in zip(shape[:3], st))
+    return MdKv4Cache(B, shape[2], 2 * half, k.data_ptr(), v.data_ptr(), ks.data_ptr(),
+                      vs.data_ptr(), sb, stok, sh, page, max_pages, pages, pt, cap)
+
+
+@_device_scoped
+def md_kv4_append(cache, k_new, v_new, pos0, *, page_table=None, lens_out=None, stream=None):
+    """Round k_new/v_new [B, n_new, Hkv, d] into the 4-bit cache at positions pos0[b] + i
+    (in place).  Returns lens_out [B] int32 = pos0 + n_new."""
+    lib = load_library()
+    B, n_new = k_new.shape[:2]
+    if k_new.shape != v_new.shape or not k_new.is_contiguous() or not v_new.is_contiguous():
+        raise ValueError("k_new and v_new must be contiguous [B, n_new, Hkv, d] of equal shape")
+    if k_new.dtype != v_new.dtype:
+        raise ValueError("k_new and v_new must share a dtype")
+    c = make_kv4_cache(cache, num_seqs=B, page_table=page_table)
+    if B and k_new.shape[2:] != (c.num_kv_heads, c.head_dim):
+        raise ValueError("appended rows must have the cache's heads and head_dim")
+    _on_gpu(cache.k, k_new=k_new, v_new=v_new, pos0=pos0, lens_out=lens_out)
+    _ints("pos0", pos0, B)
+    if lens_out is None:
+        lens_out = pos0.new_empty((B,))
+    _ints("lens_out", lens_out, B)
+    _check(lib.md_kv4_append(ctypes.byref(c), n_new, _dtype_code(k_new), k_new.data_ptr(),
+                             v_new.data_ptr(), pos0.data_ptr(), lens_out.data_ptr(),
+                             _stream_handle(cache.k, stream)))
+    return lens_out
+
+
+@_device_scoped
+def md_kv4_read(cache, pos0, n, *, page_table=None, dtype=None, k_out=None, v_out=None,
+                stream=None):
+    """The values of positions pos0[b] .. pos0[b] + n - 1 of the 4-bit cache: (k, v)
+    [B, n, Hkv, d] in dtype (bfloat16 unless given; exact in float32 too), zeros
+    outside the cache."""
+    torch = _torch()
+    lib = load_library()
+    B = pos0.shape[0]
+    c = make_kv4_cache(cache, num_seqs=B, page_table=page_table)
+    shape = (B, n, c.num_kv_heads, c.head_dim)
+    _on_gpu(cache.k, pos0=pos0, k_out=k_out, v_out=v_out)
+    _ints("pos0", pos0, B)
+    if dtype is None:
+        dtype = torch.bfloat16 if k_out is None else k_out.dtype
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    for t in (k_out, v_out):
+        if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+            raise ValueError("k_out and v_out must be contiguous [B, n, Hkv, d] of one dtype")
+    _check(lib.md_kv4_read(ctypes.byref(c), n, _dtype_code(k_out), pos0.data_ptr(),
+                           k_out.data_ptr(), v_out.data_ptr(), _stream_handle(cache.k, stream)))
+    return k_out, v_out
+
+
+def _kv4_args(q, c, kv_lens, max_kv_len, sm_scale, out, lse, workspace):
+    B, L, Hq, d = q.shape
+    if d != c.head_dim:
+        raise ValueError("q's head_dim must be the cache's")
+    if not q.is_contiguous() or (out is not None and not out.is_contiguous()):
+        raise ValueError("q and o must be contiguous [B, L, Hq, d]")
+    if out is not None and (out.shape != q.shape or out.dtype != q.dtype):
+        raise ValueError("o must have q's shape and dtype")
+    torch = _torch()
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
+                            or lse.numel() < B * L * Hq):
+        raise ValueError("lse must be contiguous float32 [B, L, Hq]")
+    gpu = q.get_device()
+    for t in (kv_lens, out, lse, workspace):
+        if gpu < 0 or (t is not None and t.get_device() != gpu):
+            _on_gpu(q, kv_lens=kv_lens, out=out, lse=lse, workspace=workspace)
+    _ints("kv_lens", kv_lens, B)
+    if max_kv_len is None:  # a bound that needs no device sync
+        max_kv_len = c.max_pages_per_seq * c.page_size if c.page_size else c.capacity
+    return MdKv4AttnArgs(L, Hq, _dtype_code(q), float(sm_scale), q.data_ptr(), kv_lens.data_ptr(),
+                         int(max_kv_len), None if out is None else out.data_ptr(),
+                         None if lse is None else lse.data_ptr(),
+                         None if workspace is None else workspace.data_ptr(),
+                         0 if workspace is None else workspace.numel() * workspace.element_size())
+
+
+def md_kv4_workspace_bytes(q, cache, kv_lens, *, mode=MD_MODE_VERIFY, n_sink=0, window=1,
+                           max_kv_len=None, page_table=None) -> int:
+    """Workspace bytes md_kv4_verify_attn or md_kv4_draft_attn needs for these tensors."""
+    c = make_kv4_cache(cache, num_seqs=q.shape[0], page_table=page_table)
+    a = _kv4_args(q, c, kv_lens, max_kv_len, 0.0, None, None, None)
+    return int(load_library().md_kv4_workspace_bytes(ctypes.byref(c), ctypes.byref(a), mode, n_sink,
+                                                     window))
+
+
+@_device_scoped
+def _kv4_attention(q, cache, kv_lens, mode, n_sink, window, *, max_kv_len=None, page_table=None,
+                   sm_scale=0.0, out=None, lse=None, return_lse=True, workspace=None, stream=None):
+    torch = _torch()
+    lib = load_library()
+    c = make_kv4_cache(cache, num_seqs=q.shape[0], page_table=page_table)
+    if cache.k.get_device() != q.get_device():
+        _on_gpu(q, cache=cache.k)
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and return_lse:
+        lse = q.new_empty(q.shape[:3], dtype=torch.float32)
+    a = _kv4_args(q, c, kv_lens, max_kv_len, sm_scale, out, lse, workspace)
+    rc, ra = ctypes.byref(c), ctypes.byref(a)
+    if workspace is None:
+        need = lib.md_kv4_workspace_bytes(rc, ra, mode, n_sink, window)
+        if need:
+            workspace = q.new_empty((need,), dtype=torch.uint8)
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), need
+    s = _stream_handle(q, stream)
+    if mode == MD_MODE_VERIFY:
+        st = lib.md_kv4_verify_attn(rc, ra, s)
+    else:
+        st = lib.md_kv4_draft_attn(rc, ra, n_sink, window, s)
+    if st != MD_OK:
+        _check(st)
+    return out, lse
+
+
+def md_kv4_verify_attn(q, cache, kv_lens, **kw):
+    """md_verify_attn over a 4-bit cache (see include/magicdec.h)."""
+    return _kv4_attention(q, cache, kv_lens, MD_MODE_VERIFY, 0, 1, **kw)
+
+
+def md_kv4_draft_attn(q, cache, kv_lens, n_sink, window, **kw):
+    """md_draft_attn (sinks and window) over a 4-bit cache (see include/magicdec.h)."""
+    return _kv4_attention(q, cache, kv_lens, MD_MODE_DRAFT, int(n_sink), int(window), **kw)
+
+
+@_device_scoped
+def md_spec_accept(target_probs, draft_probs, draft, u, *, accepted=None, tokens=None,
+                   workspace=None, stream=None):
+    """Sampled acceptance: target_probs [B, gamma + 1, vocab] and draft_probs [B, gamma,
+    vocab] (or None: drafts chosen, not sampled), float32/bfloat16; draft [B, gamma]
+    int32; u [B, gamma + 1] float32 in [0, 1) -> (accepted [B], tokens [B, gamma + 1]), int32."""
+    torch = _torch()
+    lib = load_library()
+    B, L, vocab = target_probs.shape
+    if not target_probs.is_contiguous():
+        raise ValueError("target_probs must be contiguous [B, gamma + 1, vocab]")
+    if draft_probs is not None and (draft_probs.shape != (B, L - 1, vocab)
+                                    or draft_probs.dtype != target_probs.dtype
+                                    or not draft_probs.is_contiguous()):
+        raise ValueError("draft_probs must be contiguous [B, gamma, vocab] in target_probs' dtype")
+    if draft.shape != (B, L - 1) or draft.dtype != torch.int32 or not draft.is_contiguous():
+        raise ValueError("draft must be contiguous int32 [B, gamma]")
+    if u.shape != (B, L) or u.dtype != torch.float32 or not u.is_contiguous():
+        raise ValueError("u must be contiguous float32 [B, gamma + 1]")
+    _on_gpu(target_probs, draft_probs=draft_probs, draft=draft, u=u, accepted=accepted,
+            tokens=tokens, workspace=workspace)
+    if accepted is None:
+        accepted = draft.new_empty((B,))
+    else:
+        _ints("accepted", accepted, B)
+    if tokens is None:
+        tokens = draft.new_empty((B, L))
+    else:
+        _ints("tokens", tokens, B * L)
+    if workspace is None:
+        need = lib.md_spec_accept_workspace_bytes(B, L - 1, vocab)
+        workspace = torch.empty((max(need, 1),), dtype=torch.uint8, device=target_probs.device)
+    _check(lib.md_spec_accept(B, L - 1, vocab, _dtype_code(target_probs), target_probs.data_ptr(),
+                              None if draft_probs is None or L == 1 else draft_probs.data_ptr(),
+                              draft.data_ptr() if L > 1 else None, u.data_ptr(),
+                              accepted.data_ptr(), tokens.data_ptr(), workspace.data_ptr(),
+                              workspace.numel() * workspace.element_size(),
+                              _stream_handle(target_probs, stream)))
+    return accepted, tokens
+
+
+def _token_rows(name, t, shape):
+    """The (sequence, token) element strides of rows [B, n, heads, d] whose heads are dense."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
+    sb, st, sh, sc = t.stride()
+    if (sc != 1 and shape[3] > 1) or (sh != shape[3] and shape[2] > 1):
+        raise ValueError(f"the heads of a token of {name} must be contiguous")
+    if shape[1] == 1:  # a dimension of size one has no stride of its own
+        st = shape[2] * shape[3]
+    return (shape[1] * st if shape[0] == 1 else sb), st
+
+
+@_device_scoped
+def md_qk_norm_rope(q, k_new, pos0, inv_freq, *, norm=True, q_weight=None, k_weight=None, eps=1e-6,
+                    interleaved=False, v_new=None, k=None, v=None, page_table=None, q_out=None,
+                    k_out=None, lens_out=None, stream=None):
+    """RMS norm (norm=False: none) of the heads of q [B, n, Hq, d] and k_new [B, n, Hkv, d] and
+    their rotation by position pos0[b] + i, over the first 2 * len(inv_freq) channels.
+    With a cache k, v (contiguous, or paged with page_table) the K rows and v_new's
+    rows are written into it.  q, k_new and v_new may be views of one projection.
+    Returns (q_out, k_out, lens_out); k_out is None with a cache unless given."""
+    torch = _torch()
+    lib = load_library()
+    B, n, Hq, d = q.shape
+    Hkv = k_new.shape[2]
+    qs, ks = _token_rows("q", q, (B, n, Hq, d)), _token_rows("k_new", k_new, (B, n, Hkv, d))
+    vs = (0, 0)
+    c = None
+    dt = q.dtype
+    if (k is None) != (v is None) or (k is None) != (v_new is None):
+        raise ValueError("a cache takes k, v and v_new together")
+    if k is not None:
+        vs = _token_rows("v_new", v_new, (B, n, Hkv, d))
+        c = make_kv_cache(k, v, num_seqs=B, page_table=page_table)
+        if k.dtype != dt or v_new.dtype != dt or k.get_device() != q.get_device():
+            raise ValueError("the cache and v_new must have q's dtype and device")
+    elif page_table is not None:
+        raise ValueError("page_table without a cache")
+    if k_new.dtype != dt:
+        raise ValueError("q and k_new must share a dtype")
+    _on_gpu(q, k_new=k_new, v_new=v_new, pos0=pos0, inv_freq=inv_freq, q_weight=q_weight,
+            k_weight=k_weight, q_out=q_out, k_out=k_out, lens_out=lens_out)
+    _ints("pos0", pos0, B)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and (w.dtype != dt or w.shape != (d,) or not w.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous [d] in q's dtype")
+    if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be contiguous float32 [rot_dim / 2]")
+    if q_out is None:
+        q_out = torch.empty((B, n, Hq, d), dtype=dt, device=q.device)
+    if k_out is None and c is None:
+        k_out = torch.empty((B, n, Hkv, d), dtype=dt, device=q.device)
+    for name, t, h in (("q_out", q_out, Hq), ("k_out", k_out, Hkv)):
+        if t is not None and (t.shape != (B, n, h, d) or t.dtype != dt or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous [B, n, heads, d] in q's dtype")
+    if lens_out is None:
+        lens_out = pos0.new_empty((B,))
+    _ints("lens_out", lens_out, B)
+    a = MdQkNormRopeArgs(B, n, Hq, Hkv, d, _dtype_code(q), int(bool(norm)), float(eps),
+                         _addr(q_weight), _addr(k_weight), 2 * inv_freq.numel(), int(bool(interleaved)),
+                         _addr(inv_freq), q.data_ptr(), k_new.data_ptr(), _addr(v_new), *qs, *ks, *vs,
+                         pos0.data_ptr(), q_out.data_ptr(), _addr(k_out), lens_out.data_ptr())
+    _check(lib.md_qk_norm_rope(ctypes.byref(a), None if c is None else ctypes.byref(c),
+                               _stream_handle(q, stream)))
+    return q_out, k_out, lens_out
+
+
 def md_sd_expected_tokens(gamma: int, alpha: float) -> float:
     """Eq. 1: expected tokens per verification (NaN for invalid arguments)."""
     return load_library().md_sd_expected_tokens(int(gamma), float(alpha))
@@ -774,3 +1169,9 @@ greedy_accept = md_greedy_accept
 kv_commit = md_kv_commit
 streaming_list = md_streaming_list
 kv_gather = md_kv_gather
+kv4_append = md_kv4_append
+kv4_read = md_kv4_read
+kv4_verify_attn = md_kv4_verify_attn
+kv4_draft_attn = md_kv4_draft_attn
+spec_accept = md_spec_accept
+qk_norm_rope = md_qk_norm_rope

@@ -17,7 +17,8 @@ LIB = os.path.join(PKG, "libmagicdec.so")
 ARCH = "gfx950"
 
 SOURCES = ["api.cpp", "plan.cpp", "costmodel.cpp", "attn.hip", "attn_agpr.hip", "merge.hip",
-           "snapkv.hip", "step.hip", "bench.hip", "noalloc.hip"]
+           "snapkv.hip", "step.hip", "bench.hip", "noalloc.hip", "plan_ops.cpp", "api_ops.cpp",
+           "kv4.hip", "kv4_attn.hip", "spec.hip", "norm_rope.hip"]
 
 
 def hipcc() -> str:

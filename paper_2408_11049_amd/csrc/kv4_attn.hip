@@ -1,0 +1,590 @@
+// kv4_attn.hip -- decode attention over a 4-bit KV cache (MXFP4; format in kv4.h).
+//
+//   s = scale q.K_j,  o = sum_j exp(s_j - lse) V_j
+//
+// A unit is a (sequence, KV head): its G * L query rows share one pass over its K and
+// V.  136 bytes a token and head (d = 128) instead of bf16's 512 leave a compute
+// unit some 380 cycles per 32 tokens at the HBM rate, so the work per element
+// decides the layout:
+//   K   never passes through LDS.  A lane loads 32 consecutive channels of a token --
+//       one 16-byte load, one scale -- and v_cvt_scalef32_pk_bf16_fp4 turns them
+//       into four MFMA A operands; the contraction's order is free, so Q is held in
+//       the same channel order.  The scale costs nothing: the conversion applies it,
+//       exactly.
+//   V   is converted the same way, then staged in LDS as bf16 rows and read back
+//       transposed (ds_read_b64_tr_b16), since O^T += V^T P^T contracts over tokens.
+//   S^T, the softmax state and O^T keep each lane on one query row, as in
+//   attn_kernel.h: no lane moves between the two products.
+// fp32 queries: K and V are exact in bf16, so Q and P split into three bf16 parts
+// (24 bits) give fp32 products on the bf16 matrix instructions.
+//
+// Work split: the 32-token tiles of all units form one stream cut into equal ranges,
+// one a workgroup, so neither ragged lengths nor few sequences leave units idle; a
+// unit that a cut crosses is computed in pieces, which a second launch joins.
+#include "kv4.h"
+
+namespace md {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef const __attribute__((address_space(4))) int32_t const_i32;
+
+namespace {
+
+constexpr int T = kKv4Tile;
+constexpr int W = kWaves;
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+__device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// 8 codes -> 8 bf16 values.
+__device__ __forceinline__ u32x4 values8(uint32_t codes, float scale) {
+  return u32x4{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
+}
+// The scale's power of two; byte 255 becomes infinity's pattern with a mantissa bit: NaN.
+__device__ __forceinline__ float scale_of(uint32_t byte) {
+  return __uint_as_float((byte << 23) | (byte == 255u ? 0x400000u : 0u));
+}
+
+// ---- the tiles of a sequence ----
+// Tiles are cut at multiples of T of the token position, so a tile's blocks of 16
+// lie in one page of 16 tokens or more.  Tile v of a unit is real tile v below
+// `head` (sinks), v - head + tail0 from there on (the windows).
+struct Tiles {
+  int S;      // clamped length
+  int n;      // tiles that hold a visible token
+  int head, tail0;
+};
+__device__ __forceinline__ Tiles tiles_of(const Kv4AttnParams& p, int b) {
+  Tiles t;
+  t.S = max(min(p.kv_lens[b], p.max_kv_len), 0);
+  const int end = (t.S + T - 1) / T;
+  t.head = end;
+  t.tail0 = end;
+  t.n = end;
+  if (p.mode == MD_MODE_DRAFT) {
+    const int lo = t.S - p.L - p.window + 1;  // first position of any window
+    const int sinks = p.n_sink / T + (p.n_sink % T != 0);
+    if (lo > 0 && lo / T > sinks) {
+      t.head = sinks;
+      t.tail0 = lo / T;
+      t.n = sinks + end - t.tail0;
+    }
+  }
+  return t;
+}
+
+// Balanced plan: units in order (sequence, head), max(1, tiles) stream tiles each; range w
+// of NW is [w TT / NW, (w + 1) TT / NW).
+struct Cursor {
+  int t, hi;       // next stream tile, end of the range
+  int b, hk;       // the current unit
+  int g0, gt;      // its first stream tile and its number of tiles
+  int TT, NW;
+};
+
+// Inclusive tile counts of the sequences in sl[0..B); the total.  256 threads.
+__device__ int scan_tiles(const Kv4AttnParams& p, int* sl) {
+  constexpr int kPer = kKv4BalMaxSeqs / 256;
+  __shared__ int wave_sum[W];
+  const int tid = threadIdx.x, lane = tid & 63;
+  int v[kPer], mine = 0;
+  for (int e = 0; e < kPer; ++e) {
+    const int b = tid * kPer + e;
+    v[e] = b < p.B ? max(tiles_of(p, b).n, 1) * p.Hkv : 0;
+    mine += v[e];
+  }
+  int incl = mine;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 63) wave_sum[tid >> 6] = incl;
+  __syncthreads();
+  int run = incl - mine;
+  for (int w = 0; w < (tid >> 6); ++w) run += wave_sum[w];
+  for (int e = 0; e < kPer; ++e) {
+    run += v[e];
+    if (tid * kPer + e < p.B) sl[tid * kPer + e] = run;
+  }
+  __syncthreads();
+  return uniform(sl[p.B - 1]);
+}
+
+// The unit that holds stream tile t.  sl as scan_tiles leaves it.
+__device__ void unit_at(const Kv4AttnParams& p, const int* sl, int t, Cursor& c) {
+  int lo = 0, hi = p.B - 1;  // the first sequence whose inclusive count passes t
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (sl[mid] > t) hi = mid;
+    else lo = mid + 1;
+  }
+  c.b = uniform(lo);
+  const int ex = c.b ? uniform(sl[c.b - 1]) : 0;
+  c.gt = (uniform(sl[c.b]) - ex) / p.Hkv;
+  c.hk = (t - ex) / c.gt;
+  c.g0 = ex + c.hk * c.gt;
+}
+
+// Ranges of a stream of TT tiles: at least a tile for each wave where there are as many.
+__device__ __forceinline__ int ranges(int grid, int TT) { return min(grid, max(1, TT / W)); }
+__device__ __forceinline__ int range_start(const Cursor& c, int w) {
+  return static_cast<int>(static_cast<int64_t>(w) * c.TT / c.NW);
+}
+__device__ __forceinline__ int range_of(const Cursor& c, int t) {
+  return static_cast<int>((static_cast<int64_t>(t + 1) * c.NW - 1) / c.TT);
+}
+
+// Row r of a unit: query token i = r / G, query head hk * G + r % G.
+__device__ __forceinline__ int64_t out_row(const Kv4AttnParams& p, int b, int hk, int r) {
+  return (static_cast<int64_t>(b) * p.L + r / p.G) * p.Hq + hk * p.G + r % p.G;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store4(const Kv4AttnParams& p, int64_t e, f32x4 x) {
+  if constexpr (BF16)
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.o) + e) =
+        u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+  else
+    *reinterpret_cast<f32x4*>(static_cast<float*>(p.o) + e) = x;
+}
+
+// O and lse of a row from its unnormalised O, running max (log2) and sum.  A sum of 0: no
+// visible key.  A NaN sum (a NaN score) makes the row NaN.
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+}
+
+// PG: 0 contiguous, 1 pages of at least 16 tokens, 2 smaller pages.
+template <int D, bool BF16, int NT, int PG>
+__global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(NT <= 2 && BF16 ? 2 : 1)))
+kv4_attn_kernel(const Kv4AttnParams p) {
+  constexpr int LB = D / 8;         // code bytes a lane loads of a token: D / 4 channels
+  constexpr int LW = LB / 4;        // their dwords: MFMA steps over the channels
+  constexpr int CB = D / 16;        // 16-channel blocks of O
+  constexpr int PARTS = BF16 ? 1 : 3;
+  constexpr int ROWS = NT * 16;
+  constexpr int DEPTH = 2;          // tiles in flight a wave
+  constexpr int VROW = D * 2 + 32;  // bytes of a staged V row
+  constexpr int MROW = D + 4;       // floats of a row in the waves' merge
+  constexpr int kMergeO = W * ROWS * MROW * 4;
+  constexpr int kMerge = kMergeO + 2 * W * ROWS * 4;
+  constexpr int kScan = kKv4BalMaxSeqs * 4;
+  constexpr int kV = W * T * VROW;
+  constexpr int kLds = kV > kMerge ? (kV > kScan ? kV : kScan) : (kMerge > kScan ? kMerge : kScan);
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kLds];
+
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
+  const int wave = uniform(tid >> 6);
+
+  Cursor c{};
+  if (p.balanced) {
+    int* sl = reinterpret_cast<int*>(lds);
+    c.TT = scan_tiles(p, sl);
+    c.NW = ranges(static_cast<int>(gridDim.x), c.TT);
+    const int w = static_cast<int>(blockIdx.x);
+    if (w >= c.NW) return;  // the whole workgroup
+    c.t = range_start(c, w);
+    c.hi = range_start(c, w + 1);
+    unit_at(p, sl, c.t, c);
+    __syncthreads();  // the LDS is reused
+  } else {
+    c.b = static_cast<int>(blockIdx.x) / p.Hkv;
+    c.hk = static_cast<int>(blockIdx.x) % p.Hkv;
+  }
+
+  for (;;) {  // one pass a piece
+    const int b = c.b, hk = c.hk;
+    Tiles u = tiles_of(p, b);
+    u.S = uniform(u.S);
+    u.n = uniform(u.n);
+    u.head = uniform(u.head);
+    u.tail0 = uniform(u.tail0);
+    if (!p.balanced) c = Cursor{0, max(u.n, 1), b, hk, 0, max(u.n, 1), max(u.n, 1), 1};
+    const int S = u.S;
+    const int lt0 = c.t - c.g0;
+    const int lt1 = min(c.hi, c.g0 + c.gt) - c.g0;
+    const bool whole = lt0 == 0 && lt1 == c.gt;
+    const int n_tiles = min(lt1, u.n) - lt0;  // <= 0: nothing visible
+
+    int row_pos[NT];  // position of this lane's query rows; padding rows see nothing
+    u32x4 q[NT][PARTS][LW];
+    for (int rt = 0; rt < NT; ++rt) {
+      const int r = rt * 16 + l16;
+      row_pos[rt] = r < p.R ? S - p.L + r / p.G : -1;
+      const int64_t e = r < p.R ? out_row(p, b, hk, r) * D + grp * (D / 4) : 0;
+      for (int w = 0; w < LW; ++w) {
+        if constexpr (BF16) {
+          q[rt][0][w] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + e + w * 8);
+        } else {
+          const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(p.q) + e + w * 8);
+          for (int h = 0; h < 2; ++h) {
+            f32x4 x = src[h];
+            for (int k = 0; k < PARTS; ++k) {  // the leading 8 bits, then those of the rest
+              const uint32_t a0 = pack2(x[0], x[1]), a1 = pack2(x[2], x[3]);
+              q[rt][k][w][2 * h] = a0;
+              q[rt][k][w][2 * h + 1] = a1;
+              x = f32x4{x[0] - lo_f32(a0), x[1] - hi_f32(a0), x[2] - lo_f32(a1), x[3] - hi_f32(a1)};
+            }
+          }
+        }
+        if (r >= p.R)
+          for (int k = 0; k < PARTS; ++k) q[rt][k][w] = u32x4{0, 0, 0, 0};
+      }
+    }
+
+    // ---- loads ----
+    struct TileRegs {
+      uint32_t k[2][LW], v[2][LW];
+      uint32_t ks[2], vs[2];
+    };
+    const int pmask = (1 << p.c.page_shift) - 1;
+    const_i32* ptab = PG ? (const_i32*)(p.c.page_table + static_cast<int64_t>(b) * p.c.max_pages)
+                         : nullptr;
+    const int64_t head_off = static_cast<int64_t>(hk) * p.c.s_head;
+    const uint32_t s_tok = static_cast<uint32_t>(p.c.s_tok);
+    const uint32_t sidx = grp * (D / 4) / 32;  // this lane's scale byte in its row
+    auto real_tile = [&](int v) { return v < u.head ? v : v - u.head + u.tail0; };
+    // Tokens past the sequence are read as its last one and masked below.
+    auto load_tile = [&](TileRegs& r, int v) {
+      const int t0 = real_tile(lt0 + min(v, n_tiles - 1)) * T;
+      for (int tb = 0; tb < 2; ++tb) {
+        const int bt = min(t0 + tb * 16, (S - 1) & ~15);  // a block with a real token
+        const int dt = min(l16, S - 1 - bt);
+        int64_t base;
+        uint32_t off = static_cast<uint32_t>(dt) * s_tok;
+        if constexpr (PG == 0) {
+          base = static_cast<int64_t>(b) * p.c.s_blk + head_off +
+                 static_cast<int64_t>(bt) * p.c.s_tok;
+        } else if constexpr (PG == 1) {
+          const int pid = ptab[bt >> p.c.page_shift];
+          const bool ok = pid >= 0 && pid < p.c.num_pages;  // else the pool's first block
+          base = ok ? static_cast<int64_t>(pid) * p.c.s_blk + head_off +
+                          static_cast<int64_t>(bt & pmask) * p.c.s_tok
+                    : 0;
+        } else {
+          const int t = bt + dt;
+          const int pid = ptab[t >> p.c.page_shift];
+          const bool ok = pid >= 0 && pid < p.c.num_pages;
+          base = ok ? static_cast<int64_t>(pid) * p.c.s_blk + head_off +
+                          static_cast<int64_t>(t & pmask) * p.c.s_tok
+                    : 0;
+          off = 0;
+        }
+        const unsigned char* kp = p.c.k + base + (off + grp * LB);
+        const unsigned char* vp = p.c.v + base + (off + grp * LB);
+        if constexpr (LW == 4) {
+          const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp));
+          const u32x4 d = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp));
+          for (int w = 0; w < 4; ++w) {
+            r.k[tb][w] = a[w];
+            r.v[tb][w] = d[w];
+          }
+        } else {
+          const u32x2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(kp));
+          const u32x2 d = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vp));
+          for (int w = 0; w < 2; ++w) {
+            r.k[tb][w] = a[w];
+            r.v[tb][w] = d[w];
+          }
+        }
+        r.ks[tb] = *(p.c.ks + (base >> 4) + ((off >> 4) + sidx));
+        r.vs[tb] = *(p.c.vs + (base >> 4) + ((off >> 4) + sidx));
+      }
+    };
+
+    float m_run[NT], l_run[NT];
+    f32x4 acc[NT][CB];
+    for (int rt = 0; rt < NT; ++rt) {
+      m_run[rt] = -INFINITY;
+      l_run[rt] = 0.f;
+      for (int cb = 0; cb < CB; ++cb) acc[rt][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    unsigned char* vt = lds + wave * (T * VROW);
+    constexpr float kLazy = 8.f;  // log2 headroom before the running max must move
+
+    auto visible = [&](int t, int pos) {
+      return t <= pos && (p.mode != MD_MODE_DRAFT || t < p.n_sink || t > pos - p.window);
+    };
+
+    auto process = [&](TileRegs& ring, int v) {
+      const int t0 = real_tile(lt0 + v) * T;
+      const TileRegs r = ring;
+      load_tile(ring, v + DEPTH * W);
+
+      // Uniform: does any real row see less than the whole tile?
+      bool masked = t0 + T - 1 > S - p.L;
+      if (p.mode == MD_MODE_DRAFT)
+        masked = masked || !(t0 + T <= p.n_sink || t0 > S - 1 - p.window);
+
+      // V into LDS as bf16 rows.  In a masked tile a row past the sequence, or one that is NaN
+      // in this lane's block, is staged as zeros: 0 * NaN must not reach a query that does
+      // not see it; those that see it get their NaN below.
+      unsigned long long nan_at[2] = {0, 0};
+      for (int tb = 0; tb < 2; ++tb) {
+        float vs = scale_of(r.vs[tb]);
+        uint32_t keep = 0xffffffffu;
+        if (masked) {
+          const bool past = t0 + tb * 16 + l16 >= S;
+          const bool bad = r.vs[tb] == 255u;
+          nan_at[tb] = __ballot(bad && !past);
+          if (past || bad) {
+            vs = 1.f;
+            keep = 0u;
+          }
+        }
+        unsigned char* dst = vt + (tb * 16 + l16) * VROW + grp * (D / 2);
+        for (int w = 0; w < LW; ++w)
+          *reinterpret_cast<u32x4*>(dst + w * 16) = values8(r.v[tb][w] & keep, vs);
+      }
+
+      // S^T = K Q^T.
+      f32x4 s[NT][2];
+      for (int tb = 0; tb < 2; ++tb) {
+        for (int rt = 0; rt < NT; ++rt) s[rt][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const float ks = scale_of(r.ks[tb]);
+        for (int w = 0; w < LW; ++w) {
+          const bf16x8 kk = __builtin_bit_cast(bf16x8, values8(r.k[tb][w], ks));
+          for (int rt = 0; rt < NT; ++rt)
+            for (int k = PARTS - 1; k >= 0; --k)
+              s[rt][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  kk, __builtin_bit_cast(bf16x8, q[rt][k][w]), s[rt][tb], 0, 0, 0);
+        }
+      }
+
+      // Softmax weights, in the log2 domain: lane's row l16, tokens tb*16 + 4 grp + e.
+      u32x4 pb[NT][PARTS];
+      for (int rt = 0; rt < NT; ++rt) {
+        float x[8];
+        for (int tb = 0; tb < 2; ++tb)
+          for (int e = 0; e < 4; ++e) {
+            x[tb * 4 + e] = s[rt][tb][e] * p.scale_log2;
+            if (masked && !visible(t0 + tb * 16 + 4 * grp + e, row_pos[rt]))
+              x[tb * 4 + e] = -INFINITY;
+          }
+        float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                         fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        if (__any(mx > m_run[rt] + kLazy)) {
+          const float m_new = fmaxf(m_run[rt], mx);
+          const float alpha = m_new == -INFINITY ? 1.f : exp2_fast(m_run[rt] - m_new);
+          m_run[rt] = m_new;
+          l_run[rt] *= alpha;
+          for (int cb = 0; cb < CB; ++cb) acc[rt][cb] *= alpha;
+        }
+        const float m_use = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
+        float sum = 0.f;
+        for (int j = 0; j < 8; ++j) {
+          x[j] = exp2_fast(x[j] - m_use);
+          sum += x[j];
+        }
+        l_run[rt] += sum;  // of the unrounded weights: lse keeps fp32
+        for (int k = 0; k < PARTS; ++k)
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t h = pack2(x[2 * j], x[2 * j + 1]);
+            pb[rt][k][j] = h;
+            if constexpr (!BF16) {
+              x[2 * j] -= lo_f32(h);
+              x[2 * j + 1] -= hi_f32(h);
+            }
+          }
+      }
+
+      // O^T += V^T P^T.  Transposed reads: lane k of a 16-lane group supplies row 4 grp + k / 4
+      // and channels cb*16 + 4 (k % 4) .. + 3, and lane i gets channel cb*16 + i of those rows.
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      for (int cb = 0; cb < CB; ++cb) {
+        const unsigned char* src =
+            vt + (4 * grp + (l16 >> 2)) * VROW + (cb * 16 + 4 * (l16 & 3)) * 2;
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src));
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * VROW));
+        const u32x2 a = __builtin_bit_cast(u32x2, lo), d = __builtin_bit_cast(u32x2, hi);
+        const bf16x8 va = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], d[0], d[1]});
+        for (int rt = 0; rt < NT; ++rt)
+          for (int k = PARTS - 1; k >= 0; --k)
+            acc[rt][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                va, __builtin_bit_cast(bf16x8, pb[rt][k]), acc[rt][cb], 0, 0, 0);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+
+      // NaN blocks of V of a masked tile: into the rows that see the token.
+      for (int tb = 0; tb < 2; ++tb)
+        for (unsigned long long left = nan_at[tb]; left; left &= left - 1) {
+          const int at = __ffsll(static_cast<long long>(left)) - 1;
+          const int t = t0 + tb * 16 + (at & 15), block = (at >> 4) * (D / 4) / 32;
+          for (int rt = 0; rt < NT; ++rt)
+            if (visible(t, row_pos[rt]))
+              for (int cb = 0; cb < CB; ++cb)
+                if (cb / 2 == block) acc[rt][cb] += __uint_as_float(0x7fc00000u);
+        }
+    };
+
+    if (n_tiles > 0) {
+      TileRegs ring[DEPTH];
+      for (int s = 0; s < DEPTH; ++s) load_tile(ring[s], wave + s * W);
+      for (int v = wave; v < n_tiles; v += DEPTH * W) {
+#pragma unroll
+        for (int s = 0; s < DEPTH; ++s)
+          if (v + s * W < n_tiles) process(ring[s], v + s * W);
+      }
+    }
+
+    // ---- join the waves: each row's max, then sums weighted by 2^(m_w - M), in wave order
+    for (int rt = 0; rt < NT; ++rt) {
+      l_run[rt] += __shfl_xor(l_run[rt], 16);
+      l_run[rt] += __shfl_xor(l_run[rt], 32);
+    }
+    __syncthreads();
+    float* mo = reinterpret_cast<float*>(lds);
+    float* sm = reinterpret_cast<float*>(lds + kMergeO);
+    float* sl = sm + W * ROWS;
+    for (int rt = 0; rt < NT; ++rt) {
+      if (grp == 0) {
+        sm[wave * ROWS + rt * 16 + l16] = m_run[rt];
+        sl[wave * ROWS + rt * 16 + l16] = l_run[rt];
+      }
+      for (int cb = 0; cb < CB; ++cb)
+        *reinterpret_cast<f32x4*>(mo + (wave * ROWS + rt * 16 + l16) * MROW + cb * 16 + grp * 4) =
+            acc[rt][cb];
+    }
+    __syncthreads();
+    // A cut unit's piece: slot 2w for the first piece of range w, 2w + 1 for its last.
+    const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) +
+                         (p.balanced && c.t != range_start(c, static_cast<int>(blockIdx.x)));
+    constexpr int kQuads = D / 4;
+    for (int item = tid; item < p.R * kQuads; item += W * 64) {
+      const int r = item / kQuads, c0 = item % kQuads * 4;
+      float M = -INFINITY;
+      for (int w = 0; w < W; ++w) M = fmaxf(M, sm[w * ROWS + r]);
+      const float m_use = M == -INFINITY ? 0.f : M;
+      float L = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < W; ++w) {
+        const float f = exp2_fast(sm[w * ROWS + r] - m_use);
+        L += f * sl[w * ROWS + r];
+        const f32x4 x = *reinterpret_cast<const f32x4*>(mo + (w * ROWS + r) * MROW + c0);
+        for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+      }
+      if (whole) {
+        const int64_t row = out_row(p, b, hk, r);
+        const float inv = inverse(L);
+        for (int j = 0; j < 4; ++j) o[j] *= inv;
+        store4<BF16>(p, row * D + c0, o);
+        if (c0 == 0 && p.lse) p.lse[row] = lse_of(M, L);
+      } else {
+        *reinterpret_cast<f32x4*>(p.part_o + (slot * p.R + r) * D + c0) = o;
+        if (c0 == 0)
+          *reinterpret_cast<f32x2*>(p.part_ml + (slot * p.R + r) * 2) = f32x2{M, L};
+      }
+    }
+
+    // ---- the next piece of the range
+    c.t = min(c.hi, c.g0 + c.gt);
+    if (c.t >= c.hi) return;
+    c.g0 += c.gt;
+    if (++c.hk == p.Hkv) {
+      c.hk = 0;
+      ++c.b;
+      c.gt = max(uniform(tiles_of(p, c.b).n), 1);
+    }
+    __syncthreads();  // the LDS is reused
+  }
+}
+
+// Joins the pieces of the units that range boundaries cut: workgroup w takes the unit
+// that boundary w crosses, if it is the unit's first.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(W * 64) kv4_join_kernel(const Kv4AttnParams p) {
+  __shared__ int sl[kKv4BalMaxSeqs];
+  Cursor c{};
+  c.TT = scan_tiles(p, sl);
+  c.NW = ranges(static_cast<int>(gridDim.x), c.TT);
+  const int w = static_cast<int>(blockIdx.x);
+  if (w == 0 || w >= c.NW) return;
+  const int t = range_start(c, w);
+  unit_at(p, sl, t, c);
+  if (t == c.g0 || range_start(c, w - 1) > c.g0) return;  // no cut, or not the first
+  const int w0 = w - 1, w1 = range_of(c, c.g0 + c.gt - 1);
+  const int first = 2 * w0 + (range_start(c, w0) != c.g0);
+  constexpr int kQuads = D / 4;
+  for (int item = threadIdx.x; item < p.R * kQuads; item += W * 64) {
+    const int r = item / kQuads, c0 = item % kQuads * 4;
+    float M = -INFINITY;
+    for (int k = w0; k <= w1; ++k)
+      M = fmaxf(M, p.part_ml[(static_cast<int64_t>(k == w0 ? first : 2 * k) * p.R + r) * 2]);
+    const float m_use = M == -INFINITY ? 0.f : M;
+    float L = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k = w0; k <= w1; ++k) {
+      const int64_t row = static_cast<int64_t>(k == w0 ? first : 2 * k) * p.R + r;
+      const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + row * 2);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + row * D + c0);
+      const float f = exp2_fast(ml[0] - m_use);
+      L += f * ml[1];
+      for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+    }
+    const int64_t row = out_row(p, c.b, c.hk, r);
+    const float inv = inverse(L);
+    for (int j = 0; j < 4; ++j) o[j] *= inv;
+    store4<BF16>(p, row * D + c0, o);
+    if (c0 == 0 && p.lse) p.lse[row] = lse_of(M, L);
+  }
+}
+
+template <int D, bool BF16, int NT>
+hipError_t launch_nt(const Kv4AttnParams& p, const Kv4Plan& pl, hipStream_t s) {
+  const dim3 g(static_cast<uint32_t>(pl.n_blocks)), blk(W * 64);
+  if (!p.c.page_table)
+    hipLaunchKernelGGL((kv4_attn_kernel<D, BF16, NT, 0>), g, blk, 0, s, p);
+  else if (p.c.page_shift >= 4)
+    hipLaunchKernelGGL((kv4_attn_kernel<D, BF16, NT, 1>), g, blk, 0, s, p);
+  else
+    hipLaunchKernelGGL((kv4_attn_kernel<D, BF16, NT, 2>), g, blk, 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !pl.balanced) return e;
+  hipLaunchKernelGGL((kv4_join_kernel<D, BF16>), g, blk, 0, s, p);
+  return hipGetLastError();
+}
+
+template <int D, bool BF16>
+hipError_t launch_d(const Kv4AttnParams& p, const Kv4Plan& pl, hipStream_t s) {
+  switch (pl.NT) {
+    case 1: return launch_nt<D, BF16, 1>(p, pl, s);
+    case 2: return launch_nt<D, BF16, 2>(p, pl, s);
+    case 3: return launch_nt<D, BF16, 3>(p, pl, s);
+    default: return launch_nt<D, BF16, 4>(p, pl, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_kv4_attn(const Kv4AttnParams& p, const Kv4Plan& pl, int head_dim, bool bf16,
+                           hipStream_t s) {
+  if (head_dim == 128)
+    return bf16 ? launch_d<128, true>(p, pl, s) : launch_d<128, false>(p, pl, s);
+  return bf16 ? launch_d<64, true>(p, pl, s) : launch_d<64, false>(p, pl, s);
+}
+
+}  // namespace md

@@ -1,0 +1,227 @@
+// norm_rope.hip -- RMS norm of query and key heads and the rotation by position, with
+// the new K and V rows written into the cache in the same pass.
+//
+//   y = x / sqrt(mean x^2 + eps) * w;  (y1, y2) -> (y1 cos t - y2 sin t, y2 cos t + y1 sin t)
+//
+// Bound by HBM for prompts, by latency for a step: every row is read once and written
+// once.  A row of d channels is d / 8 threads of 8 channels (16 bytes of bf16), so its
+// sum of squares is reduced over 8 or 16 neighbouring lanes and a pair's other half is
+// one lane exchange away.  A workgroup takes one token: the rot / 2 angles are turned
+// into cosines and sines once (64-bit product and reduction, so far positions keep
+// their fraction of a turn) and serve all the token's heads from LDS, while the
+// rows' loads are in flight.
+#include "kv4.h"
+
+namespace md {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+namespace {
+
+template <bool BF16>
+struct Raw {  // 8 channels as stored
+  u32x4 w[BF16 ? 1 : 2];
+};
+
+template <bool BF16>
+__device__ __forceinline__ Raw<BF16> load_raw(const void* base, int64_t e) {
+  Raw<BF16> r;
+  const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const char*>(base) + e * (BF16 ? 2 : 4));
+  r.w[0] = p[0];
+  if constexpr (!BF16) r.w[1] = p[1];
+  return r;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store_raw(void* base, int64_t e, const Raw<BF16>& r) {
+  u32x4* p = reinterpret_cast<u32x4*>(static_cast<char*>(base) + e * (BF16 ? 2 : 4));
+  p[0] = r.w[0];
+  if constexpr (!BF16) p[1] = r.w[1];
+}
+
+template <bool BF16>
+__device__ __forceinline__ void widen(const Raw<BF16>& r, float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (BF16) {
+      x[2 * j] = __uint_as_float(r.w[0][j] << 16);
+      x[2 * j + 1] = __uint_as_float(r.w[0][j] & 0xffff0000u);
+    } else {
+      x[j] = __uint_as_float(r.w[0][j]);
+      x[4 + j] = __uint_as_float(r.w[1][j]);
+    }
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ Raw<BF16> narrow(const float (&x)[8]) {
+  Raw<BF16> r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (BF16) {
+      r.w[0][j] = __builtin_bit_cast(
+          uint32_t, __builtin_convertvector(f32x2{x[2 * j], x[2 * j + 1]}, bf16x2));
+    } else {
+      r.w[0][j] = __float_as_uint(x[j]);
+      r.w[1][j] = __float_as_uint(x[4 + j]);
+    }
+  }
+  return r;
+}
+
+// Row `row` of a token: Hq query heads, Hkv key heads, then (with a cache) Hkv value heads.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeParams p) {
+  constexpr int LPR = D / 8;       // threads a row
+  constexpr int RPP = 256 / LPR;   // rows a pass
+  constexpr int U = 4;             // passes whose loads are in flight together
+  __shared__ float cs[D / 2], sn[D / 2];
+  const int tid = threadIdx.x;
+  const int c = tid % LPR, rr = tid / LPR;
+  const int token = blockIdx.x;
+  const int b = token / p.n, i = token - b * p.n;
+  const int rows = p.Hq + p.Hkv * (p.has_cache ? 2 : 1);
+  const int32_t base = p.pos0[b];
+  const int64_t pos = static_cast<int64_t>(base) + i;
+  const int64_t qoff = b * p.q_seq + i * p.q_tok, koff = b * p.k_seq + i * p.k_tok,
+                voff = b * p.v_seq + i * p.v_tok;
+
+  const int first = static_cast<int>(blockIdx.y) * RPP;
+  const int step = static_cast<int>(gridDim.y) * RPP;
+  bool angles = false;
+  for (int r0 = first; r0 < rows; r0 += U * step) {
+    Raw<BF16> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int row = r0 + u * step + rr;
+      if (row >= rows) continue;
+      const void* src = row < p.Hq ? p.q : (row < p.Hq + p.Hkv ? p.k : p.v);
+      const int64_t at = row < p.Hq ? qoff + static_cast<int64_t>(row) * D
+                         : row < p.Hq + p.Hkv ? koff + static_cast<int64_t>(row - p.Hq) * D
+                                              : voff + static_cast<int64_t>(row - p.Hq - p.Hkv) * D;
+      raw[u] = load_raw<BF16>(src, at + c * 8);
+    }
+    if (!angles) {
+      for (int j = tid; j < p.rot / 2; j += 256) {
+        constexpr double kInv2Pi = 0.15915494309189533577;
+        constexpr double k2PiHi = 6.283185307179586232, k2PiLo = 2.4492935982947064e-16;
+        const double t = static_cast<double>(pos) * static_cast<double>(p.inv_freq[j]);
+        const double n = rint(t * kInv2Pi);
+        const float f = static_cast<float>(fma(-n, k2PiLo, fma(-n, k2PiHi, t)));
+        sincosf(f, &sn[j], &cs[j]);
+      }
+      __syncthreads();
+      angles = true;
+    }
+    // Where position pos lives in the cache (uniform over the workgroup).
+    bool in = p.has_cache && pos >= 0;
+    int64_t cache_at = 0;
+    if (in) {
+      int64_t blk = b, tok = pos;
+      if (p.paged) {
+        const int64_t pg = pos >> p.c.page_shift;
+        in = pg < p.c.max_pages;
+        blk = in ? p.c.page_table[static_cast<int64_t>(b) * p.c.max_pages + pg] : 0;
+        in = in && blk >= 0 && blk < p.c.num_pages;
+        tok = pos & ((int64_t{1} << p.c.page_shift) - 1);
+      } else {
+        in = pos < p.c.capacity;
+      }
+      cache_at = blk * p.c.s_blk + tok * p.c.s_tok;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int row = r0 + u * step + rr;
+      if (r0 + u * step >= rows) break;  // uniform: the lanes of a row exchange values below
+      const bool live = row < rows;
+      const bool is_q = row < p.Hq, is_k = !is_q && row < p.Hq + p.Hkv;
+      const int head = is_q ? row : (is_k ? row - p.Hq : row - p.Hq - p.Hkv);
+      float x[8];
+      if (live) {
+        widen<BF16>(raw[u], x);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = 0.f;
+      }
+      if (p.norm) {
+        float ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ss += x[j] * x[j];
+        for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
+        const float rs = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
+        const void* w = is_q ? p.q_weight : p.k_weight;
+        float wt[8];
+        if (w && live) {
+          widen<BF16>(load_raw<BF16>(w, c * 8), wt);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) wt[j] = 1.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = x[j] * rs * wt[j];
+      }
+      if (p.interleaved) {
+        if (c * 8 < p.rot) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float co = cs[c * 4 + j], si = sn[c * 4 + j];
+            const float y1 = x[2 * j], y2 = x[2 * j + 1];
+            x[2 * j] = y1 * co - y2 * si;
+            x[2 * j + 1] = y2 * co + y1 * si;
+          }
+        }
+      } else {
+        const int half = p.rot / 16;  // threads a half of the turned channels takes
+        const int lane = tid & 63;
+        const bool lo = c < half, hi = !lo && c < 2 * half;
+        const int other = lo ? lane + half : (hi ? lane - half : lane);
+        const int j0 = (lo ? c : c - half) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float y = __shfl(x[j], other);
+          if (lo || hi) {
+            const float co = cs[j0 + j], si = sn[j0 + j];
+            x[j] = lo ? x[j] * co - y * si : x[j] * co + y * si;
+          }
+        }
+      }
+      if (!live) continue;
+      if (is_q) {
+        store_raw<BF16>(p.q_out, (static_cast<int64_t>(token) * p.Hq + head) * D + c * 8,
+                        narrow<BF16>(x));
+        continue;
+      }
+      // A value row moves as it is.
+      const Raw<BF16> out = is_k ? narrow<BF16>(x) : raw[u];
+      if (is_k && p.k_out)
+        store_raw<BF16>(p.k_out, (static_cast<int64_t>(token) * p.Hkv + head) * D + c * 8, out);
+      if (in) store_raw<BF16>(is_k ? p.c.k : p.c.v, cache_at + head * p.c.s_head + c * 8, out);
+    }
+  }
+  if (blockIdx.y == 0 && i == 0 && tid == 0 && p.lens_out) p.lens_out[b] = base + p.n;
+}
+
+}  // namespace
+
+hipError_t launch_qk_norm_rope(const NormRopeParams& p, int head_dim, bool bf16, hipStream_t s) {
+  const int64_t tokens = static_cast<int64_t>(p.B) * p.n;
+  const int rows = p.Hq + p.Hkv * (p.has_cache ? 2 : 1);
+  const int passes = (rows + 256 / (head_dim / 8) - 1) / (256 / (head_dim / 8));
+  // Few tokens: a workgroup for each pass of a token's rows instead of one for all.
+  const int64_t cus = device_cu_count();
+  const int split = static_cast<int>(tokens * 2 <= cus ? passes : 1);
+  const dim3 g(static_cast<uint32_t>(tokens), static_cast<uint32_t>(split)), b(256);
+  if (head_dim == 128) {
+    if (bf16) hipLaunchKernelGGL((qk_norm_rope_kernel<128, true>), g, b, 0, s, p);
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<128, false>), g, b, 0, s, p);
+  } else {
+    if (bf16) hipLaunchKernelGGL((qk_norm_rope_kernel<64, true>), g, b, 0, s, p);
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<64, false>), g, b, 0, s, p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace md

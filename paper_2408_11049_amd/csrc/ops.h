@@ -1,0 +1,49 @@
+// ops.h -- host-side checks and plans of the 4-bit KV cache, sampled acceptance
+// and the query/key norm with rotation.  No HIP types, so they compile and run
+// without a GPU.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "internal.h"
+#include "magicdec.h"
+
+namespace md {
+
+// Tokens of one step of a wave of the 4-bit attention.
+constexpr int kKv4Tile = 32;
+// Byte stride of a token row: a tile's rows are addressed with 32-bit offsets.
+constexpr int64_t kKv4MaxTokStride = int64_t{1} << 25;
+// The balanced plan ranks every sequence's tiles in each workgroup.
+constexpr int kKv4BalMaxSeqs = 1024;
+
+int validate_kv4_cache(const md_kv4_cache* c);
+// The buffers of a call that touches the cache (B > 0).
+int validate_kv4_buffers(const md_kv4_cache* c);
+
+struct Kv4Plan {
+  int32_t G = 0, R = 0, NT = 0;   // query heads a KV head, query rows a unit, 16-row tiles
+  bool balanced = false;
+  int32_t n_blocks = 0;           // workgroups
+  size_t part_o_bytes = 0, part_ml_bytes = 0, workspace_bytes = 0;
+};
+int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                         int window);
+Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                      int window, int num_cus);
+int validate_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                      int window, Kv4Plan* plan);
+
+struct SpecPlan {
+  int32_t n_chunks = 0, chunk_len = 0;
+  size_t workspace_bytes = 0;
+};
+constexpr int kSpecMaxChunks = 64;
+int validate_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype);
+SpecPlan make_spec_plan(int32_t num_seqs, int32_t vocab, int num_cus);
+
+// Sizes, strides, pointers and overlaps; c may be NULL (no cache).
+int validate_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* c);
+
+}  // namespace md

@@ -1,0 +1,210 @@
+// plan_ops.cpp -- argument checks and work plans of the 4-bit KV cache, sampled
+// acceptance and the query/key norm with rotation.  Pure host arithmetic, no HIP
+// call: every error path runs on a machine without a GPU.
+#include <limits.h>
+
+#include <algorithm>
+
+#include "ops.h"
+
+namespace md {
+
+namespace {
+
+bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+typedef __int128 wide;  // byte spans of any strides
+
+// Whether [a, a + n) and [b, b + m) share a byte.
+bool overlap(const void* a, wide n, const void* b, wide m) {
+  const wide x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && n && m && x < y + m && y < x + n;
+}
+
+}  // namespace
+
+int validate_kv4_cache(const md_kv4_cache* c) {
+  if (!c || c->num_seqs < 0 || c->num_kv_heads < 1 || c->head_dim < 1) return MD_ERR_INVALID_ARG;
+  if (c->page_size != 0) {
+    if (c->page_size < 0 || (c->page_size & (c->page_size - 1)) || c->max_pages_per_seq < 1 ||
+        c->num_pages < 1 || c->num_pages > INT32_MAX)
+      return MD_ERR_INVALID_ARG;
+  } else if (c->page_table || c->capacity < 1) {
+    return MD_ERR_INVALID_ARG;
+  }
+  if (c->stride_blk < 0 || c->stride_tok < 0 || c->stride_head < 0) return MD_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return MD_ERR_UNSUPPORTED;
+  const int64_t row = c->head_dim / 2;
+  if (c->stride_blk % row || c->stride_tok % row || c->stride_head % row)
+    return MD_ERR_INVALID_ARG;
+  // Rows of neighbouring heads and tokens must not share bytes.
+  const int64_t toks = c->page_size ? c->page_size : c->capacity;
+  if ((c->num_kv_heads > 1 && c->stride_head < row) || (toks > 1 && c->stride_tok < row))
+    return MD_ERR_INVALID_ARG;
+  if (c->stride_tok > kKv4MaxTokStride) return MD_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(c->num_seqs) * c->num_kv_heads > INT32_MAX) return MD_ERR_UNSUPPORTED;
+  return MD_OK;
+}
+
+int validate_kv4_buffers(const md_kv4_cache* c) {
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale) return MD_ERR_INVALID_ARG;
+  const uintptr_t sc = static_cast<uintptr_t>(c->head_dim) / 32;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, sc) ||
+      !aligned(c->v_scale, sc))
+    return MD_ERR_INVALID_ARG;
+  if (c->page_size && (!c->page_table || !aligned(c->page_table, 4))) return MD_ERR_INVALID_ARG;
+  return MD_OK;
+}
+
+int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                         int window) {
+  if (!a || (mode != MD_MODE_VERIFY && mode != MD_MODE_DRAFT)) return MD_ERR_INVALID_ARG;
+  if (mode == MD_MODE_DRAFT && (n_sink < 0 || window < 1)) return MD_ERR_INVALID_ARG;
+  if (a->q_len < 1 || a->q_len > 16 || a->num_q_heads < 1 || a->max_kv_len < a->q_len)
+    return MD_ERR_INVALID_ARG;
+  if (a->dtype != MD_F32 && a->dtype != MD_BF16) return MD_ERR_INVALID_ARG;
+  const int st = validate_kv4_cache(c);
+  if (st == MD_ERR_INVALID_ARG) return st;
+  if (a->num_q_heads % c->num_kv_heads) return MD_ERR_INVALID_ARG;
+  if (c->page_size ? ceil_div(a->max_kv_len, c->page_size) > c->max_pages_per_seq
+                   : c->capacity < a->max_kv_len)
+    return MD_ERR_INVALID_ARG;
+  if (st != MD_OK) return st;
+  if (static_cast<int64_t>(a->num_q_heads / c->num_kv_heads) * a->q_len > kMaxRows)
+    return MD_ERR_UNSUPPORTED;
+  if (a->max_kv_len > kMaxPosition) return MD_ERR_UNSUPPORTED;
+  if (mode == MD_MODE_DRAFT && (window > kMaxPosition || n_sink > kMaxPosition))
+    return MD_ERR_UNSUPPORTED;
+  return MD_OK;
+}
+
+Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                      int window, int num_cus) {
+  Kv4Plan p;
+  p.G = a->num_q_heads / c->num_kv_heads;
+  p.R = p.G * a->q_len;
+  p.NT = (p.R + 15) / 16;
+  const int64_t units = static_cast<int64_t>(c->num_seqs) * c->num_kv_heads;
+  // Most tiles of any unit: the whole context, or sinks and the union of the windows,
+  // each cut at tile boundaries.
+  int64_t tiles = ceil_div(a->max_kv_len, kKv4Tile);
+  if (mode == MD_MODE_DRAFT)
+    tiles = std::min(tiles, ceil_div(n_sink, kKv4Tile) +
+                                ceil_div(int64_t{window} + a->q_len - 1, kKv4Tile) + 1);
+  const int64_t cus = num_cus > 0 ? num_cus : 256;
+  const int64_t slots = cus * (p.NT <= 2 ? 2 : 1);
+  p.n_blocks = static_cast<int32_t>(units);
+  if (tiles * kKv4Tile > kWholeTokens && c->num_seqs <= kKv4BalMaxSeqs &&
+      tiles * units < (int64_t{1} << 30)) {
+    p.balanced = true;
+    p.n_blocks = static_cast<int32_t>(std::min(slots, ceil_div(tiles * units, kWaves)));
+    p.part_o_bytes =
+        align_up(static_cast<size_t>(2 * p.n_blocks) * p.R * c->head_dim * sizeof(float), 256);
+    p.part_ml_bytes = align_up(static_cast<size_t>(2 * p.n_blocks) * p.R * 2 * sizeof(float), 256);
+    p.workspace_bytes = p.part_o_bytes + p.part_ml_bytes;
+  }
+  return p;
+}
+
+int validate_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                      int window, Kv4Plan* plan) {
+  const int st = check_kv4_attn_sizes(c, a, mode, n_sink, window);
+  if (st != MD_OK) return st;
+  if (c->num_seqs == 0) return MD_OK;
+  const int bufs = validate_kv4_buffers(c);
+  if (bufs != MD_OK) return bufs;
+  if (!a->q || !a->o || !a->kv_lens || !aligned(a->q, 16) || !aligned(a->o, 16) ||
+      !aligned(a->kv_lens, 4) || !aligned(a->lse, 4))
+    return MD_ERR_INVALID_ARG;
+  *plan = make_kv4_plan(c, a, mode, n_sink, window, device_cu_count());
+  if (plan->workspace_bytes && (!a->workspace || a->workspace_bytes < plan->workspace_bytes ||
+                                !aligned(a->workspace, 256)))
+    return MD_ERR_WORKSPACE;
+  return MD_OK;
+}
+
+int validate_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype) {
+  if (num_seqs < 0 || n_draft < 0 || n_draft > 1023 || vocab < 1 || vocab > (1 << 30))
+    return MD_ERR_INVALID_ARG;
+  if (dtype != MD_F32 && dtype != MD_BF16) return MD_ERR_INVALID_ARG;
+  if (num_seqs > (1 << 25) - 1) return MD_ERR_UNSUPPORTED;  // num_seqs * kSpecMaxChunks workgroups
+  return MD_OK;
+}
+
+SpecPlan make_spec_plan(int32_t num_seqs, int32_t vocab, int num_cus) {
+  SpecPlan pl;
+  const int64_t cus = num_cus > 0 ? num_cus : 256;
+  constexpr int64_t kMinChunk = 2048;
+  int64_t n = ceil_div(8 * cus, std::max(num_seqs, 1));
+  n = std::max<int64_t>(1, std::min({n, ceil_div(vocab, kMinChunk), int64_t{kSpecMaxChunks}}));
+  const int64_t len = ceil_div(ceil_div(vocab, n), 8) * 8;  // whole 16-byte vectors
+  pl.chunk_len = static_cast<int32_t>(len);
+  pl.n_chunks = static_cast<int32_t>(ceil_div(vocab, len));
+  pl.workspace_bytes = static_cast<size_t>(num_seqs) * pl.n_chunks * sizeof(double);
+  return pl;
+}
+
+int validate_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* c) {
+  if (!a) return MD_ERR_INVALID_ARG;
+  if (a->num_seqs < 0 || a->n_new < 0 || a->num_q_heads < 1 || a->num_kv_heads < 1 ||
+      a->head_dim < 1)
+    return MD_ERR_INVALID_ARG;
+  if (a->dtype != MD_F32 && a->dtype != MD_BF16) return MD_ERR_INVALID_ARG;
+  if (!(a->eps >= 0.f)) return MD_ERR_INVALID_ARG;
+  if (!a->norm && (a->q_weight || a->k_weight)) return MD_ERR_INVALID_ARG;
+  if (a->rot_dim < 0 || a->rot_dim > a->head_dim || a->rot_dim % 16) return MD_ERR_INVALID_ARG;
+  const int64_t es = a->dtype == MD_BF16 ? 2 : 4;
+  for (int64_t s : {a->q_stride_seq, a->q_stride_tok, a->k_stride_seq, a->k_stride_tok,
+                    a->v_stride_seq, a->v_stride_tok})
+    if (s < 0 || s % (16 / es)) return MD_ERR_INVALID_ARG;
+  if (c) {
+    const int st = validate_kv_cache(c, a->n_new);
+    if (st != MD_OK) return st;
+    if (c->num_seqs != a->num_seqs || c->num_kv_heads != a->num_kv_heads ||
+        c->head_dim != a->head_dim || c->dtype != a->dtype)
+      return MD_ERR_INVALID_ARG;
+  }
+  if (a->head_dim != 64 && a->head_dim != 128) return MD_ERR_UNSUPPORTED;
+  const int64_t tokens = static_cast<int64_t>(a->num_seqs) * a->n_new;
+  if (tokens > INT32_MAX) return MD_ERR_UNSUPPORTED;
+  if (tokens == 0) return MD_OK;
+  if (!a->q || !a->k_new || !a->pos0 || !a->q_out || (!c && !a->k_out) || (c != nullptr) != (a->v_new != nullptr))
+    return MD_ERR_INVALID_ARG;
+  if (a->rot_dim && !a->inv_freq) return MD_ERR_INVALID_ARG;
+  for (const void* x : {a->q, a->k_new, a->v_new, a->q_weight, a->k_weight,
+                        static_cast<const void*>(a->q_out), static_cast<const void*>(a->k_out)})
+    if (!aligned(x, 16)) return MD_ERR_INVALID_ARG;
+  if (!aligned(a->inv_freq, 4) || !aligned(a->pos0, 4) || !aligned(a->lens_out, 4))
+    return MD_ERR_INVALID_ARG;
+  if (c && (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16) ||
+            !aligned(c->page_table, 4)))
+    return MD_ERR_INVALID_ARG;
+  const wide nb = static_cast<wide>(a->num_seqs) * 4;
+  if (overlap(a->lens_out, nb, a->pos0, nb)) return MD_ERR_INVALID_ARG;
+  // In place only row for row: any other overlap would read rows already written.
+  const int64_t d = a->head_dim, B = a->num_seqs, n = a->n_new;
+  struct Rows {
+    const void* p;
+    int64_t seq, tok, heads;
+    bool dense(wide n_tok, wide hd) const { return tok == heads * hd && seq == n_tok * tok; }
+    wide bytes(wide b, wide n_tok, wide hd, wide e) const {
+      return ((b - 1) * seq + (n_tok - 1) * tok + heads * hd) * e;
+    }
+  };
+  const Rows in[3] = {{a->q, a->q_stride_seq, a->q_stride_tok, a->num_q_heads},
+                      {a->k_new, a->k_stride_seq, a->k_stride_tok, a->num_kv_heads},
+                      {a->v_new, a->v_stride_seq, a->v_stride_tok, a->num_kv_heads}};
+  const Rows out[2] = {{a->q_out, n * a->num_q_heads * d, a->num_q_heads * d, a->num_q_heads},
+                       {a->k_out, n * a->num_kv_heads * d, a->num_kv_heads * d, a->num_kv_heads}};
+  for (int o = 0; o < 2; ++o)
+    for (int i = 0; i < 3; ++i)
+      if (overlap(out[o].p, out[o].bytes(B, n, d, es), in[i].p, in[i].bytes(B, n, d, es)) &&
+          !(o == i && out[o].p == in[i].p && in[i].dense(n, d)))
+        return MD_ERR_INVALID_ARG;
+  if (overlap(out[0].p, out[0].bytes(B, n, d, es), out[1].p, out[1].bytes(B, n, d, es)))
+    return MD_ERR_INVALID_ARG;
+  return MD_OK;
+}
+
+}  // namespace md
