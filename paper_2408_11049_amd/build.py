@@ -38,7 +38,8 @@ def _flags():
 # passes fit their register budgets either way, and the vector work that reads
 # each score then needs no copy out of an AGPR.  attn.hip: measured there.
 _MFMA_IN_VGPRS = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-EXTRA_FLAGS = {"snapkv.hip": _MFMA_IN_VGPRS, "attn.hip": _MFMA_IN_VGPRS}
+EXTRA_FLAGS = {"snapkv.hip": _MFMA_IN_VGPRS, "attn.hip": _MFMA_IN_VGPRS,
+               "kv4_attn.hip": _MFMA_IN_VGPRS}
 
 
 def _compile(src: str, verbose: bool) -> str:

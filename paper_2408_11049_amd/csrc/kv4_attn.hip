@@ -33,7 +33,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-typedef const __attribute__((address_space(4))) int32_t const_i32;
 
 namespace {
 
@@ -226,17 +225,21 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 
     int row_pos[NT];  // position of this lane's query rows; padding rows see nothing
     u32x4 q[NT][PARTS][LW];
+#pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
       const int r = rt * 16 + l16;
       row_pos[rt] = r < p.R ? S - p.L + r / p.G : -1;
       const int64_t e = r < p.R ? out_row(p, b, hk, r) * D + grp * (D / 4) : 0;
+#pragma unroll
       for (int w = 0; w < LW; ++w) {
         if constexpr (BF16) {
           q[rt][0][w] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + e + w * 8);
         } else {
           const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(p.q) + e + w * 8);
+#pragma unroll
           for (int h = 0; h < 2; ++h) {
             f32x4 x = src[h];
+#pragma unroll
             for (int k = 0; k < PARTS; ++k) {  // the leading 8 bits, then those of the rest
               const uint32_t a0 = pack2(x[0], x[1]), a1 = pack2(x[2], x[3]);
               q[rt][k][w][2 * h] = a0;
@@ -246,6 +249,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
           }
         }
         if (r >= p.R)
+#pragma unroll
           for (int k = 0; k < PARTS; ++k) q[rt][k][w] = u32x4{0, 0, 0, 0};
       }
     }
@@ -256,17 +260,36 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       uint32_t ks[2], vs[2];
     };
     const int pmask = (1 << p.c.page_shift) - 1;
-    const_i32* ptab = PG ? (const_i32*)(p.c.page_table + static_cast<int64_t>(b) * p.c.max_pages)
-                         : nullptr;
+    const int32_t* ptab = PG ? p.c.page_table + static_cast<int64_t>(b) * p.c.max_pages : nullptr;
     const int64_t head_off = static_cast<int64_t>(hk) * p.c.s_head;
     const uint32_t s_tok = static_cast<uint32_t>(p.c.s_tok);
     const uint32_t sidx = grp * (D / 4) / 32;  // this lane's scale byte in its row
     auto real_tile = [&](int v) { return v < u.head ? v : v - u.head + u.tail0; };
-    // Tokens past the sequence are read as its last one and masked below.
-    auto load_tile = [&](TileRegs& r, int v) {
-      const int t0 = real_tile(lt0 + min(v, n_tiles - 1)) * T;
+    // First token of block tb of piece tile v, in a block that holds a real token.
+    auto block_at = [&](int v, int tb) {
+      return min(real_tile(lt0 + min(v, n_tiles - 1)) * T + tb * 16, (S - 1) & ~15);
+    };
+    // An id outside the pool reads the pool's first page: in bounds, results unspecified.
+    auto page_ok = [&](int id) { return id >= 0 && id < p.c.num_pages ? id : 0; };
+
+    // Page ids (pages of 16 tokens or more): lane j holds that of block j % 2 of this wave's
+    // tile batch + j / 2, so one load serves 32 tiles; the next batch's is in flight.
+    int ids = 0, ids_next = 0;
+    auto load_ids = [&](int batch) {
+      if constexpr (PG == 1) {
+        const int bt = block_at(wave + (batch + lane / 2) * W, lane % 2);
+        return page_ok(ptab[bt >> p.c.page_shift]);
+      }
+      return 0;
+    };
+
+    // Tile k of this wave (piece tile wave + k W).  Tokens past the sequence are read as its
+    // last one, tiles past the piece as its last one; both are discarded.
+    auto load_tile = [&](TileRegs& r, int k) {
+      const int v = wave + k * W;
+#pragma unroll
       for (int tb = 0; tb < 2; ++tb) {
-        const int bt = min(t0 + tb * 16, (S - 1) & ~15);  // a block with a real token
+        const int bt = block_at(v, tb);
         const int dt = min(l16, S - 1 - bt);
         int64_t base;
         uint32_t off = static_cast<uint32_t>(dt) * s_tok;
@@ -274,18 +297,13 @@ kv4_attn_kernel(const Kv4AttnParams p) {
           base = static_cast<int64_t>(b) * p.c.s_blk + head_off +
                  static_cast<int64_t>(bt) * p.c.s_tok;
         } else if constexpr (PG == 1) {
-          const int pid = ptab[bt >> p.c.page_shift];
-          const bool ok = pid >= 0 && pid < p.c.num_pages;  // else the pool's first block
-          base = ok ? static_cast<int64_t>(pid) * p.c.s_blk + head_off +
-                          static_cast<int64_t>(bt & pmask) * p.c.s_tok
-                    : 0;
+          const int id = __builtin_amdgcn_readlane(ids, (k & 31) * 2 + tb);
+          base = static_cast<int64_t>(id) * p.c.s_blk + head_off +
+                 static_cast<int64_t>(bt & pmask) * p.c.s_tok;
         } else {
           const int t = bt + dt;
-          const int pid = ptab[t >> p.c.page_shift];
-          const bool ok = pid >= 0 && pid < p.c.num_pages;
-          base = ok ? static_cast<int64_t>(pid) * p.c.s_blk + head_off +
-                          static_cast<int64_t>(t & pmask) * p.c.s_tok
-                    : 0;
+          base = static_cast<int64_t>(page_ok(ptab[t >> p.c.page_shift])) * p.c.s_blk + head_off +
+                 static_cast<int64_t>(t & pmask) * p.c.s_tok;
           off = 0;
         }
         const unsigned char* kp = p.c.k + base + (off + grp * LB);
@@ -293,6 +311,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
         if constexpr (LW == 4) {
           const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp));
           const u32x4 d = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp));
+#pragma unroll
           for (int w = 0; w < 4; ++w) {
             r.k[tb][w] = a[w];
             r.v[tb][w] = d[w];
@@ -300,6 +319,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
         } else {
           const u32x2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(kp));
           const u32x2 d = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vp));
+#pragma unroll
           for (int w = 0; w < 2; ++w) {
             r.k[tb][w] = a[w];
             r.v[tb][w] = d[w];
@@ -312,9 +332,13 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 
     float m_run[NT], l_run[NT];
     f32x4 acc[NT][CB];
+    uint32_t nan_v[NT];  // bit i: the row sees a token whose V is NaN in channels 32 i ..
+#pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
       m_run[rt] = -INFINITY;
       l_run[rt] = 0.f;
+      nan_v[rt] = 0;
+#pragma unroll
       for (int cb = 0; cb < CB; ++cb) acc[rt][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     unsigned char* vt = lds + wave * (T * VROW);
@@ -324,80 +348,117 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       return t <= pos && (p.mode != MD_MODE_DRAFT || t < p.n_sink || t > pos - p.window);
     };
 
-    auto process = [&](TileRegs& ring, int v) {
-      const int t0 = real_tile(lt0 + v) * T;
-      const TileRegs r = ring;
-      load_tile(ring, v + DEPTH * W);
-
-      // Uniform: does any real row see less than the whole tile?
-      bool masked = t0 + T - 1 > S - p.L;
-      if (p.mode == MD_MODE_DRAFT)
-        masked = masked || !(t0 + T <= p.n_sink || t0 > S - 1 - p.window);
-
+    // One tile.  masked (uniform): some query row does not see all of it.  `refill` issues
+    // the loads that reuse the tile's registers, once they are free.
+    auto process = [&](bool masked, const TileRegs& r, int t0, auto refill) {
       // V into LDS as bf16 rows.  In a masked tile a row past the sequence, or one that is NaN
       // in this lane's block, is staged as zeros: 0 * NaN must not reach a query that does
-      // not see it; those that see it get their NaN below.
-      unsigned long long nan_at[2] = {0, 0};
-      for (int tb = 0; tb < 2; ++tb) {
-        float vs = scale_of(r.vs[tb]);
-        uint32_t keep = 0xffffffffu;
-        if (masked) {
+      // not see it; those that see it are noted and get their NaN at the end.
+      float vscale[2] = {scale_of(r.vs[0]), scale_of(r.vs[1])};
+      uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
+      if (masked) {
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
           const bool past = t0 + tb * 16 + l16 >= S;
           const bool bad = r.vs[tb] == 255u;
-          nan_at[tb] = __ballot(bad && !past);
+          for (unsigned long long left = __ballot(bad && !past); left; left &= left - 1) {
+            const int at = __ffsll(static_cast<long long>(left)) - 1;
+#pragma unroll
+            for (int rt = 0; rt < NT; ++rt)
+              if (visible(t0 + tb * 16 + (at & 15), row_pos[rt]))
+                nan_v[rt] |= 1u << ((at >> 4) * (D / 4) / 32);
+          }
           if (past || bad) {
-            vs = 1.f;
-            keep = 0u;
+            vscale[tb] = 1.f;
+            keep[tb] = 0u;
           }
         }
+      }
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb) {
         unsigned char* dst = vt + (tb * 16 + l16) * VROW + grp * (D / 2);
+#pragma unroll
         for (int w = 0; w < LW; ++w)
-          *reinterpret_cast<u32x4*>(dst + w * 16) = values8(r.v[tb][w] & keep, vs);
+          *reinterpret_cast<u32x4*>(dst + w * 16) = values8(r.v[tb][w] & keep[tb], vscale[tb]);
       }
 
+      __builtin_amdgcn_sched_barrier(0);
       // S^T = K Q^T.
       f32x4 s[NT][2];
+#pragma unroll
       for (int tb = 0; tb < 2; ++tb) {
+#pragma unroll
         for (int rt = 0; rt < NT; ++rt) s[rt][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
         const float ks = scale_of(r.ks[tb]);
+#pragma unroll
         for (int w = 0; w < LW; ++w) {
           const bf16x8 kk = __builtin_bit_cast(bf16x8, values8(r.k[tb][w], ks));
+#pragma unroll
           for (int rt = 0; rt < NT; ++rt)
+#pragma unroll
             for (int k = PARTS - 1; k >= 0; --k)
               s[rt][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                   kk, __builtin_bit_cast(bf16x8, q[rt][k][w]), s[rt][tb], 0, 0, 0);
         }
       }
 
-      // Softmax weights, in the log2 domain: lane's row l16, tokens tb*16 + 4 grp + e.
-      u32x4 pb[NT][PARTS];
-      for (int rt = 0; rt < NT; ++rt) {
-        float x[8];
-        for (int tb = 0; tb < 2; ++tb)
-          for (int e = 0; e < 4; ++e) {
-            x[tb * 4 + e] = s[rt][tb][e] * p.scale_log2;
-            if (masked && !visible(t0 + tb * 16 + 4 * grp + e, row_pos[rt]))
-              x[tb * 4 + e] = -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);
+      refill();
+      __builtin_amdgcn_sched_barrier(0);
+
+      // Softmax weights, in the log2 domain: lane's row l16, tokens tb*16 + 4 grp + e.  The
+      // running max of a row moves only when one of its scores passes it by kLazy, so
+      // most tiles need no exchange between the four lanes of a row; until then a weight
+      // is at most 2^kLazy.
+      float xs[NT][8];
+#pragma unroll
+      for (int rt = 0; rt < NT; ++rt)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) xs[rt][j] = s[rt][j / 4][j % 4] * p.scale_log2;
+      if (masked) {
+        const int first = t0 + 4 * grp;
+#pragma unroll
+        for (int rt = 0; rt < NT; ++rt) {
+          // visible() of this lane's tokens, relative to its first: up to `last`, and above
+          // `gone` or below `sinks`.  (Padding rows see none: their `last` is below 0.)
+          const int last = row_pos[rt] - first, sinks = p.n_sink - first;
+          const int gone = p.mode == MD_MODE_DRAFT
+                               ? static_cast<int>(static_cast<uint32_t>(last) - p.window)
+                               : INT32_MIN;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int t = j / 4 * 16 + j % 4;
+            if (!(t <= last && (t > gone || t < sinks))) xs[rt][j] = -INFINITY;
           }
+        }
+      }
+      u32x4 pb[NT][PARTS];
+#pragma unroll
+      for (int rt = 0; rt < NT; ++rt) {
+        float(&x)[8] = xs[rt];
         float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
                          fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
         if (__any(mx > m_run[rt] + kLazy)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
           const float m_new = fmaxf(m_run[rt], mx);
           const float alpha = m_new == -INFINITY ? 1.f : exp2_fast(m_run[rt] - m_new);
           m_run[rt] = m_new;
           l_run[rt] *= alpha;
+#pragma unroll
           for (int cb = 0; cb < CB; ++cb) acc[rt][cb] *= alpha;
         }
         const float m_use = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
         float sum = 0.f;
+#pragma unroll
         for (int j = 0; j < 8; ++j) {
           x[j] = exp2_fast(x[j] - m_use);
           sum += x[j];
         }
         l_run[rt] += sum;  // of the unrounded weights: lse keeps fp32
+#pragma unroll
         for (int k = 0; k < PARTS; ++k)
+#pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t h = pack2(x[2 * j], x[2 * j + 1]);
             pb[rt][k][j] = h;
@@ -413,6 +474,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
         const unsigned char* src =
             vt + (4 * grp + (l16 >> 2)) * VROW + (cb * 16 + 4 * (l16 & 3)) * 2;
@@ -420,7 +482,9 @@ kv4_attn_kernel(const Kv4AttnParams p) {
         const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * VROW));
         const u32x2 a = __builtin_bit_cast(u32x2, lo), d = __builtin_bit_cast(u32x2, hi);
         const bf16x8 va = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], d[0], d[1]});
+#pragma unroll
         for (int rt = 0; rt < NT; ++rt)
+#pragma unroll
           for (int k = PARTS - 1; k >= 0; --k)
             acc[rt][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                 va, __builtin_bit_cast(bf16x8, pb[rt][k]), acc[rt][cb], 0, 0, 0);
@@ -428,30 +492,46 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-
-      // NaN blocks of V of a masked tile: into the rows that see the token.
-      for (int tb = 0; tb < 2; ++tb)
-        for (unsigned long long left = nan_at[tb]; left; left &= left - 1) {
-          const int at = __ffsll(static_cast<long long>(left)) - 1;
-          const int t = t0 + tb * 16 + (at & 15), block = (at >> 4) * (D / 4) / 32;
-          for (int rt = 0; rt < NT; ++rt)
-            if (visible(t, row_pos[rt]))
-              for (int cb = 0; cb < CB; ++cb)
-                if (cb / 2 == block) acc[rt][cb] += __uint_as_float(0x7fc00000u);
-        }
     };
 
-    if (n_tiles > 0) {
+    // Tiles of this wave.
+    const int mine = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;
+    if (mine > 0) {
       TileRegs ring[DEPTH];
-      for (int s = 0; s < DEPTH; ++s) load_tile(ring[s], wave + s * W);
-      for (int v = wave; v < n_tiles; v += DEPTH * W) {
+      ids = load_ids(0);
+      ids_next = load_ids(32);
 #pragma unroll
-        for (int s = 0; s < DEPTH; ++s)
-          if (v + s * W < n_tiles) process(ring[s], v + s * W);
+      for (int s = 0; s < DEPTH; ++s) load_tile(ring[s], s);
+      for (int k0 = 0; k0 < mine; k0 += DEPTH) {
+#pragma unroll
+        for (int s = 0; s < DEPTH; ++s) {
+          const int k = k0 + s;
+          if (k >= mine) break;
+          auto refill = [&]() {
+            if (PG == 1 && ((k + DEPTH) & 31) == 0) {
+              ids = ids_next;
+              ids_next = load_ids(k + DEPTH + 32);
+            }
+            load_tile(ring[s], k + DEPTH);
+          };
+          const int t0 = real_tile(lt0 + wave + k * W) * T;
+          bool masked = t0 + T - 1 > S - p.L;
+          if (p.mode == MD_MODE_DRAFT)
+            masked = masked || !(t0 + T <= p.n_sink || t0 > S - 1 - p.window);
+          process(masked, ring[s], t0, refill);
+        }
       }
     }
+#pragma unroll
+    for (int rt = 0; rt < NT; ++rt)
+      if (__any(nan_v[rt] != 0)) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+          if ((nan_v[rt] >> (cb / 2)) & 1u) acc[rt][cb] += __uint_as_float(0x7fc00000u);
+      }
 
     // ---- join the waves: each row's max, then sums weighted by 2^(m_w - M), in wave order
+#pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
       l_run[rt] += __shfl_xor(l_run[rt], 16);
       l_run[rt] += __shfl_xor(l_run[rt], 32);
@@ -460,11 +540,13 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     float* mo = reinterpret_cast<float*>(lds);
     float* sm = reinterpret_cast<float*>(lds + kMergeO);
     float* sl = sm + W * ROWS;
+#pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
       if (grp == 0) {
         sm[wave * ROWS + rt * 16 + l16] = m_run[rt];
         sl[wave * ROWS + rt * 16 + l16] = l_run[rt];
       }
+#pragma unroll
       for (int cb = 0; cb < CB; ++cb)
         *reinterpret_cast<f32x4*>(mo + (wave * ROWS + rt * 16 + l16) * MROW + cb * 16 + grp * 4) =
             acc[rt][cb];
