@@ -79,6 +79,8 @@ int run_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int
   p.Hkv = c->num_kv_heads;
   p.G = pl.G;
   p.R = pl.R;
+  p.passes = pl.passes;
+  p.units = c->num_kv_heads * pl.passes;
   const float scale =
       a->sm_scale > 0.f ? a->sm_scale : 1.0f / sqrtf(static_cast<float>(c->head_dim));
   p.scale_log2 = scale * 1.44269504088896340736f;

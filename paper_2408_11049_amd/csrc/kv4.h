@@ -50,13 +50,14 @@ struct Kv4AttnParams {
   const int32_t* kv_lens;
   int32_t max_kv_len;
   int32_t B, L, Hq, Hkv, G, R;
+  int32_t passes, units;      // passes over a head's K and V; units of a sequence: Hkv * passes
   float scale_log2;           // softmax scale * log2(e)
   int32_t mode, n_sink, window;
   int32_t balanced;           // 1: workgroups share all units' tiles equally
   void* o;
   float* lse;
-  float* part_o;              // balanced: [2 * workgroups][R][d], unnormalised
-  float* part_ml;             // balanced: [2 * workgroups][R][2]: running max (log2), sum
+  float* part_o;              // balanced: [2 * workgroups][16 NT][d], unnormalised
+  float* part_ml;             // balanced: [2 * workgroups][16 NT][2]: running max (log2), sum
 };
 
 hipError_t launch_kv4_attn(const Kv4AttnParams& p, const Kv4Plan& pl, int head_dim, bool bf16,

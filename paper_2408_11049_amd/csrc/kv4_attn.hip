@@ -3,7 +3,7 @@
 //   s = scale q.K_j,  o = sum_j exp(s_j - lse) V_j
 //
 // A unit is a (sequence, KV head): its G * L query rows share one pass over its K and
-// V.  136 bytes a token and head (d = 128) instead of bf16's 512 leave a compute
+// V (fp32 queries: 32 of them do, more take a second pass, for want of registers).  136 bytes a token and head (d = 128) instead of bf16's 512 leave a compute
 // unit some 380 cycles per 32 tokens at the HBM rate, so the work per element
 // decides the layout:
 //   K   never passes through LDS.  A lane loads 32 consecutive channels of a token --
@@ -56,6 +56,13 @@ __device__ __forceinline__ u32x4 values8(uint32_t codes, float scale) {
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
 }
+template <int N>
+__device__ __forceinline__ void load_words(const unsigned char* at, uint32_t (&w)[N]) {
+  typedef uint32_t vec __attribute__((ext_vector_type(N)));
+  const vec x = __builtin_nontemporal_load(reinterpret_cast<const vec*>(at));
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = x[i];
+}
 // The scale's power of two; byte 255 becomes infinity's pattern with a mantissa bit: NaN.
 __device__ __forceinline__ float scale_of(uint32_t byte) {
   return __uint_as_float((byte << 23) | (byte == 255u ? 0x400000u : 0u));
@@ -89,11 +96,11 @@ __device__ __forceinline__ Tiles tiles_of(const Kv4AttnParams& p, int b) {
   return t;
 }
 
-// Balanced plan: units in order (sequence, head), max(1, tiles) stream tiles each; range w
+// Balanced plan: units in order (sequence, unit), max(1, tiles) stream tiles each; range w
 // of NW is [w TT / NW, (w + 1) TT / NW).
 struct Cursor {
   int t, hi;       // next stream tile, end of the range
-  int b, hk;       // the current unit
+  int b, j;        // the current unit: unit j of sequence b
   int g0, gt;      // its first stream tile and its number of tiles
   int TT, NW;
 };
@@ -106,7 +113,7 @@ __device__ int scan_tiles(const Kv4AttnParams& p, int* sl) {
   int v[kPer], mine = 0;
   for (int e = 0; e < kPer; ++e) {
     const int b = tid * kPer + e;
-    v[e] = b < p.B ? max(tiles_of(p, b).n, 1) * p.Hkv : 0;
+    v[e] = b < p.B ? max(tiles_of(p, b).n, 1) * p.units : 0;
     mine += v[e];
   }
   int incl = mine;
@@ -136,9 +143,9 @@ __device__ void unit_at(const Kv4AttnParams& p, const int* sl, int t, Cursor& c)
   }
   c.b = uniform(lo);
   const int ex = c.b ? uniform(sl[c.b - 1]) : 0;
-  c.gt = (uniform(sl[c.b]) - ex) / p.Hkv;
-  c.hk = (t - ex) / c.gt;
-  c.g0 = ex + c.hk * c.gt;
+  c.gt = (uniform(sl[c.b]) - ex) / p.units;
+  c.j = (t - ex) / c.gt;
+  c.g0 = ex + c.j * c.gt;
 }
 
 // Ranges of a stream of TT tiles: at least a tile for each wave where there are as many.
@@ -205,18 +212,20 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     unit_at(p, sl, c.t, c);
     __syncthreads();  // the LDS is reused
   } else {
-    c.b = static_cast<int>(blockIdx.x) / p.Hkv;
-    c.hk = static_cast<int>(blockIdx.x) % p.Hkv;
+    c.b = static_cast<int>(blockIdx.x) / p.units;
+    c.j = static_cast<int>(blockIdx.x) % p.units;
   }
 
   for (;;) {  // one pass a piece
-    const int b = c.b, hk = c.hk;
+    const int b = c.b, hk = c.j / p.passes;
+    const int r0 = c.j % p.passes * ROWS;   // its rows of the head's R: r0 .. r0 + rows - 1
+    const int rows = min(p.R - r0, ROWS);
     Tiles u = tiles_of(p, b);
     u.S = uniform(u.S);
     u.n = uniform(u.n);
     u.head = uniform(u.head);
     u.tail0 = uniform(u.tail0);
-    if (!p.balanced) c = Cursor{0, max(u.n, 1), b, hk, 0, max(u.n, 1), max(u.n, 1), 1};
+    if (!p.balanced) c = Cursor{0, max(u.n, 1), b, c.j, 0, max(u.n, 1), max(u.n, 1), 1};
     const int S = u.S;
     const int lt0 = c.t - c.g0;
     const int lt1 = min(c.hi, c.g0 + c.gt) - c.g0;
@@ -228,8 +237,9 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 #pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
       const int r = rt * 16 + l16;
-      row_pos[rt] = r < p.R ? S - p.L + r / p.G : -1;
-      const int64_t e = r < p.R ? out_row(p, b, hk, r) * D + grp * (D / 4) : 0;
+      const bool live = r < rows;
+      row_pos[rt] = live ? S - p.L + (r0 + r) / p.G : -1;
+      const int64_t e = live ? out_row(p, b, hk, r0 + r) * D + grp * (D / 4) : 0;
 #pragma unroll
       for (int w = 0; w < LW; ++w) {
         if constexpr (BF16) {
@@ -248,7 +258,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
             }
           }
         }
-        if (r >= p.R)
+        if (!live)
 #pragma unroll
           for (int k = 0; k < PARTS; ++k) q[rt][k][w] = u32x4{0, 0, 0, 0};
       }
@@ -283,66 +293,59 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       return 0;
     };
 
-    // Tile k of this wave (piece tile wave + k W).  Tokens past the sequence are read as its
-    // last one, tiles past the piece as its last one; both are discarded.
+    // Tile k of this wave (piece tile wave + k W).  A block's 16 rows are read whole, those past
+    // the sequence too where they are in the cache (masked below): the lanes' offsets are then
+    // the same for every block.  Tiles past the piece are its last one, never used.
+    const uint32_t code_off = static_cast<uint32_t>(l16) * s_tok + grp * LB;
+    const uint32_t scale_off = static_cast<uint32_t>(l16) * (s_tok >> 4) + sidx;
     auto load_tile = [&](TileRegs& r, int k) {
       const int v = wave + k * W;
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb) {
         const int bt = block_at(v, tb);
-        const int dt = min(l16, S - 1 - bt);
         int64_t base;
-        uint32_t off = static_cast<uint32_t>(dt) * s_tok;
+        uint32_t code = code_off, scale = scale_off;
         if constexpr (PG == 0) {
           base = static_cast<int64_t>(b) * p.c.s_blk + head_off +
                  static_cast<int64_t>(bt) * p.c.s_tok;
+          if (bt + 16 > p.c.capacity) {  // the cache ends inside the block
+            const uint32_t dt = static_cast<uint32_t>(min(l16, S - 1 - bt));
+            code = dt * s_tok + grp * LB;
+            scale = dt * (s_tok >> 4) + sidx;
+          }
         } else if constexpr (PG == 1) {
           const int id = __builtin_amdgcn_readlane(ids, (k & 31) * 2 + tb);
           base = static_cast<int64_t>(id) * p.c.s_blk + head_off +
                  static_cast<int64_t>(bt & pmask) * p.c.s_tok;
         } else {
-          const int t = bt + dt;
+          const int t = min(bt + l16, S - 1);
           base = static_cast<int64_t>(page_ok(ptab[t >> p.c.page_shift])) * p.c.s_blk + head_off +
                  static_cast<int64_t>(t & pmask) * p.c.s_tok;
-          off = 0;
+          code = grp * LB;
+          scale = sidx;
         }
-        const unsigned char* kp = p.c.k + base + (off + grp * LB);
-        const unsigned char* vp = p.c.v + base + (off + grp * LB);
-        if constexpr (LW == 4) {
-          const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp));
-          const u32x4 d = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp));
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            r.k[tb][w] = a[w];
-            r.v[tb][w] = d[w];
-          }
-        } else {
-          const u32x2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(kp));
-          const u32x2 d = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vp));
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            r.k[tb][w] = a[w];
-            r.v[tb][w] = d[w];
-          }
-        }
-        r.ks[tb] = *(p.c.ks + (base >> 4) + ((off >> 4) + sidx));
-        r.vs[tb] = *(p.c.vs + (base >> 4) + ((off >> 4) + sidx));
+        load_words(p.c.k + base + code, r.k[tb]);
+        load_words(p.c.v + base + code, r.v[tb]);
+        r.ks[tb] = *(p.c.ks + (base >> 4) + scale);
+        r.vs[tb] = *(p.c.vs + (base >> 4) + scale);
       }
     };
 
-    float m_run[NT], l_run[NT];
+    float m_run[NT], l_run[NT];  // log2; 0 and a threshold of -inf: no key seen yet
+    float lazy[NT];
     f32x4 acc[NT][CB];
     uint32_t nan_v[NT];  // bit i: the row sees a token whose V is NaN in channels 32 i ..
 #pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
-      m_run[rt] = -INFINITY;
+      m_run[rt] = 0.f;
+      lazy[rt] = -INFINITY;
       l_run[rt] = 0.f;
       nan_v[rt] = 0;
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) acc[rt][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     unsigned char* vt = lds + wave * (T * VROW);
-    constexpr float kLazy = 8.f;  // log2 headroom before the running max must move
+    constexpr float kLazy = 8.f;
 
     auto visible = [&](int t, int pos) {
       return t <= pos && (p.mode != MD_MODE_DRAFT || t < p.n_sink || t > pos - p.window);
@@ -350,12 +353,11 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 
     // One tile.  masked (uniform): some query row does not see all of it.  `refill` issues
     // the loads that reuse the tile's registers, once they are free.
-    auto process = [&](bool masked, const TileRegs& r, int t0, auto refill) {
+    auto process = [&](bool masked, TileRegs& r, int t0, auto refill) {
       // V into LDS as bf16 rows.  In a masked tile a row past the sequence, or one that is NaN
       // in this lane's block, is staged as zeros: 0 * NaN must not reach a query that does
       // not see it; those that see it are noted and get their NaN at the end.
       float vscale[2] = {scale_of(r.vs[0]), scale_of(r.vs[1])};
-      uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
       if (masked) {
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
@@ -370,7 +372,8 @@ kv4_attn_kernel(const Kv4AttnParams p) {
           }
           if (past || bad) {
             vscale[tb] = 1.f;
-            keep[tb] = 0u;
+#pragma unroll
+            for (int w = 0; w < LW; ++w) r.v[tb][w] = 0u;
           }
         }
       }
@@ -379,7 +382,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
         unsigned char* dst = vt + (tb * 16 + l16) * VROW + grp * (D / 2);
 #pragma unroll
         for (int w = 0; w < LW; ++w)
-          *reinterpret_cast<u32x4*>(dst + w * 16) = values8(r.v[tb][w] & keep[tb], vscale[tb]);
+          *reinterpret_cast<u32x4*>(dst + w * 16) = values8(r.v[tb][w], vscale[tb]);
       }
 
       __builtin_amdgcn_sched_barrier(0);
@@ -406,15 +409,10 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       refill();
       __builtin_amdgcn_sched_barrier(0);
 
-      // Softmax weights, in the log2 domain: lane's row l16, tokens tb*16 + 4 grp + e.  The
-      // running max of a row moves only when one of its scores passes it by kLazy, so
-      // most tiles need no exchange between the four lanes of a row; until then a weight
-      // is at most 2^kLazy.
-      float xs[NT][8];
-#pragma unroll
-      for (int rt = 0; rt < NT; ++rt)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) xs[rt][j] = s[rt][j / 4][j % 4] * p.scale_log2;
+      // Softmax weights 2^y, y = c s - m, c = scale * log2 e: lane's row l16, tokens tb*16 + 4
+      // grp + e.  A row's m moves only when some y passes kLazy (at first: whenever a key is
+      // visible), so most tiles need no exchange between the four lanes of a row; until
+      // then a weight is at most 2^kLazy.
       if (masked) {
         const int first = t0 + 4 * grp;
 #pragma unroll
@@ -428,31 +426,36 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int t = j / 4 * 16 + j % 4;
-            if (!(t <= last && (t > gone || t < sinks))) xs[rt][j] = -INFINITY;
+            if (!(t <= last && (t > gone || t < sinks))) s[rt][j / 4][j % 4] = -INFINITY;
           }
         }
       }
       u32x4 pb[NT][PARTS];
 #pragma unroll
       for (int rt = 0; rt < NT; ++rt) {
-        float(&x)[8] = xs[rt];
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = fmaf(s[rt][j / 4][j % 4], p.scale_log2, -m_run[rt]);
         float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
                          fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        if (__any(mx > m_run[rt] + kLazy)) {
+        if (__any(mx > lazy[rt])) {
           mx = fmaxf(mx, __shfl_xor(mx, 16));
           mx = fmaxf(mx, __shfl_xor(mx, 32));
-          const float m_new = fmaxf(m_run[rt], mx);
-          const float alpha = m_new == -INFINITY ? 1.f : exp2_fast(m_run[rt] - m_new);
-          m_run[rt] = m_new;
-          l_run[rt] *= alpha;
+          if (mx > lazy[rt]) {  // the same for the four lanes of a row
+            const float alpha = lazy[rt] == kLazy ? exp2_fast(-mx) : 1.f;
+            m_run[rt] += mx;
+            lazy[rt] = kLazy;
+            l_run[rt] *= alpha;
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb) acc[rt][cb] *= alpha;
+            for (int cb = 0; cb < CB; ++cb) acc[rt][cb] *= alpha;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = fmaf(s[rt][j / 4][j % 4], p.scale_log2, -m_run[rt]);
         }
-        const float m_use = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          x[j] = exp2_fast(x[j] - m_use);
+          x[j] = exp2_fast(x[j]);
           sum += x[j];
         }
         l_run[rt] += sum;  // of the unrounded weights: lse keeps fp32
@@ -501,26 +504,38 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       ids = load_ids(0);
       ids_next = load_ids(32);
 #pragma unroll
-      for (int s = 0; s < DEPTH; ++s) load_tile(ring[s], s);
-      for (int k0 = 0; k0 < mine; k0 += DEPTH) {
+      for (int s = 0; s < DEPTH; ++s) {
+        // In the order of the loop's refills: a wait for one tile leaves the later ones in flight.
+        __builtin_amdgcn_sched_barrier(0);
+        load_tile(ring[s], s);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      auto one = [&](TileRegs& r, int k, auto refill) {
+        const int t0 = real_tile(lt0 + wave + k * W) * T;
+        bool masked = t0 + T - 1 > S - p.L;
+        if (p.mode == MD_MODE_DRAFT)
+          masked = masked || !(t0 + T <= p.n_sink || t0 > S - 1 - p.window);
+        process(masked, r, t0, refill);
+      };
+      // No slot of the ring is skipped inside the loop: one that was filled on some paths only
+      // would be copied at the loop's end, and the copy would wait for its loads.
+      int k0 = 0;
+      for (; k0 + DEPTH <= mine; k0 += DEPTH) {
 #pragma unroll
         for (int s = 0; s < DEPTH; ++s) {
           const int k = k0 + s;
-          if (k >= mine) break;
-          auto refill = [&]() {
+          one(ring[s], k, [&]() {
             if (PG == 1 && ((k + DEPTH) & 31) == 0) {
               ids = ids_next;
               ids_next = load_ids(k + DEPTH + 32);
             }
             load_tile(ring[s], k + DEPTH);
-          };
-          const int t0 = real_tile(lt0 + wave + k * W) * T;
-          bool masked = t0 + T - 1 > S - p.L;
-          if (p.mode == MD_MODE_DRAFT)
-            masked = masked || !(t0 + T <= p.n_sink || t0 > S - 1 - p.window);
-          process(masked, ring[s], t0, refill);
+          });
         }
       }
+#pragma unroll
+      for (int s = 0; s + 1 < DEPTH; ++s)
+        if (k0 + s < mine) one(ring[s], k0 + s, []() {});
     }
 #pragma unroll
     for (int rt = 0; rt < NT; ++rt)
@@ -543,7 +558,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 #pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
       if (grp == 0) {
-        sm[wave * ROWS + rt * 16 + l16] = m_run[rt];
+        sm[wave * ROWS + rt * 16 + l16] = lazy[rt] == -INFINITY ? -INFINITY : m_run[rt];
         sl[wave * ROWS + rt * 16 + l16] = l_run[rt];
       }
 #pragma unroll
@@ -556,7 +571,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) +
                          (p.balanced && c.t != range_start(c, static_cast<int>(blockIdx.x)));
     constexpr int kQuads = D / 4;
-    for (int item = tid; item < p.R * kQuads; item += W * 64) {
+    for (int item = tid; item < rows * kQuads; item += W * 64) {
       const int r = item / kQuads, c0 = item % kQuads * 4;
       float M = -INFINITY;
       for (int w = 0; w < W; ++w) M = fmaxf(M, sm[w * ROWS + r]);
@@ -570,15 +585,15 @@ kv4_attn_kernel(const Kv4AttnParams p) {
         for (int j = 0; j < 4; ++j) o[j] += f * x[j];
       }
       if (whole) {
-        const int64_t row = out_row(p, b, hk, r);
+        const int64_t row = out_row(p, b, hk, r0 + r);
         const float inv = inverse(L);
         for (int j = 0; j < 4; ++j) o[j] *= inv;
         store4<BF16>(p, row * D + c0, o);
         if (c0 == 0 && p.lse) p.lse[row] = lse_of(M, L);
       } else {
-        *reinterpret_cast<f32x4*>(p.part_o + (slot * p.R + r) * D + c0) = o;
+        *reinterpret_cast<f32x4*>(p.part_o + (slot * ROWS + r) * D + c0) = o;
         if (c0 == 0)
-          *reinterpret_cast<f32x2*>(p.part_ml + (slot * p.R + r) * 2) = f32x2{M, L};
+          *reinterpret_cast<f32x2*>(p.part_ml + (slot * ROWS + r) * 2) = f32x2{M, L};
       }
     }
 
@@ -586,8 +601,8 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     c.t = min(c.hi, c.g0 + c.gt);
     if (c.t >= c.hi) return;
     c.g0 += c.gt;
-    if (++c.hk == p.Hkv) {
-      c.hk = 0;
+    if (++c.j == p.units) {
+      c.j = 0;
       ++c.b;
       c.gt = max(uniform(tiles_of(p, c.b).n), 1);
     }
@@ -597,7 +612,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 
 // Joins the pieces of the units that range boundaries cut: workgroup w takes the unit
 // that boundary w crosses, if it is the unit's first.
-template <int D, bool BF16>
+template <int D, bool BF16, int NT>
 __global__ void __launch_bounds__(W * 64) kv4_join_kernel(const Kv4AttnParams p) {
   __shared__ int sl[kKv4BalMaxSeqs];
   Cursor c{};
@@ -610,24 +625,26 @@ __global__ void __launch_bounds__(W * 64) kv4_join_kernel(const Kv4AttnParams p)
   if (t == c.g0 || range_start(c, w - 1) > c.g0) return;  // no cut, or not the first
   const int w0 = w - 1, w1 = range_of(c, c.g0 + c.gt - 1);
   const int first = 2 * w0 + (range_start(c, w0) != c.g0);
-  constexpr int kQuads = D / 4;
-  for (int item = threadIdx.x; item < p.R * kQuads; item += W * 64) {
+  constexpr int kQuads = D / 4, ROWS = NT * 16;
+  const int hk = c.j / p.passes, r0 = c.j % p.passes * ROWS;
+  const int rows = min(p.R - r0, ROWS);
+  for (int item = threadIdx.x; item < rows * kQuads; item += W * 64) {
     const int r = item / kQuads, c0 = item % kQuads * 4;
     float M = -INFINITY;
     for (int k = w0; k <= w1; ++k)
-      M = fmaxf(M, p.part_ml[(static_cast<int64_t>(k == w0 ? first : 2 * k) * p.R + r) * 2]);
+      M = fmaxf(M, p.part_ml[(static_cast<int64_t>(k == w0 ? first : 2 * k) * ROWS + r) * 2]);
     const float m_use = M == -INFINITY ? 0.f : M;
     float L = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int k = w0; k <= w1; ++k) {
-      const int64_t row = static_cast<int64_t>(k == w0 ? first : 2 * k) * p.R + r;
+      const int64_t row = static_cast<int64_t>(k == w0 ? first : 2 * k) * ROWS + r;
       const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + row * 2);
       const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + row * D + c0);
       const float f = exp2_fast(ml[0] - m_use);
       L += f * ml[1];
       for (int j = 0; j < 4; ++j) o[j] += f * x[j];
     }
-    const int64_t row = out_row(p, c.b, c.hk, r);
+    const int64_t row = out_row(p, c.b, hk, r0 + r);
     const float inv = inverse(L);
     for (int j = 0; j < 4; ++j) o[j] *= inv;
     store4<BF16>(p, row * D + c0, o);
@@ -646,18 +663,24 @@ hipError_t launch_nt(const Kv4AttnParams& p, const Kv4Plan& pl, hipStream_t s) {
     hipLaunchKernelGGL((kv4_attn_kernel<D, BF16, NT, 2>), g, blk, 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !pl.balanced) return e;
-  hipLaunchKernelGGL((kv4_join_kernel<D, BF16>), g, blk, 0, s, p);
+  hipLaunchKernelGGL((kv4_join_kernel<D, BF16, NT>), g, blk, 0, s, p);
   return hipGetLastError();
 }
 
 template <int D, bool BF16>
 hipError_t launch_d(const Kv4AttnParams& p, const Kv4Plan& pl, hipStream_t s) {
+  static_assert(kKv4MaxNT(true) == 4 && kKv4MaxNT(false) == 2, "one instance for each");
   switch (pl.NT) {
     case 1: return launch_nt<D, BF16, 1>(p, pl, s);
     case 2: return launch_nt<D, BF16, 2>(p, pl, s);
-    case 3: return launch_nt<D, BF16, 3>(p, pl, s);
-    default: return launch_nt<D, BF16, 4>(p, pl, s);
   }
+  if constexpr (BF16) {
+    switch (pl.NT) {
+      case 3: return launch_nt<D, BF16, 3>(p, pl, s);
+      case 4: return launch_nt<D, BF16, 4>(p, pl, s);
+    }
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace

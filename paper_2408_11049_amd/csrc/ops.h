@@ -15,6 +15,8 @@ namespace md {
 constexpr int kKv4Tile = 32;
 // Byte stride of a token row: a tile's rows are addressed with 32-bit offsets.
 constexpr int64_t kKv4MaxTokStride = int64_t{1} << 25;
+// Row tiles of 16 a pass over K and V takes: an fp32 query is three registers' worth of bf16.
+constexpr int kKv4MaxNT(bool bf16) { return bf16 ? 4 : 2; }
 // The balanced plan ranks every sequence's tiles in each workgroup.
 constexpr int kKv4BalMaxSeqs = 1024;
 
@@ -23,7 +25,8 @@ int validate_kv4_cache(const md_kv4_cache* c);
 int validate_kv4_buffers(const md_kv4_cache* c);
 
 struct Kv4Plan {
-  int32_t G = 0, R = 0, NT = 0;   // query heads a KV head, query rows a unit, 16-row tiles
+  int32_t G = 0, R = 0;           // query heads and rows a KV head
+  int32_t NT = 0, passes = 1;     // 16-row tiles of a pass over K and V, and passes
   bool balanced = false;
   int32_t n_blocks = 0;           // workgroups
   size_t part_o_bytes = 0, part_ml_bytes = 0, workspace_bytes = 0;

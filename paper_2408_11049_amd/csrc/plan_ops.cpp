@@ -43,7 +43,8 @@ int validate_kv4_cache(const md_kv4_cache* c) {
   if ((c->num_kv_heads > 1 && c->stride_head < row) || (toks > 1 && c->stride_tok < row))
     return MD_ERR_INVALID_ARG;
   if (c->stride_tok > kKv4MaxTokStride) return MD_ERR_UNSUPPORTED;
-  if (static_cast<int64_t>(c->num_seqs) * c->num_kv_heads > INT32_MAX) return MD_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(c->num_seqs) * c->num_kv_heads > INT32_MAX / 2)
+    return MD_ERR_UNSUPPORTED;  // workgroups: up to two a (sequence, head)
   return MD_OK;
 }
 
@@ -84,8 +85,10 @@ Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode
   Kv4Plan p;
   p.G = a->num_q_heads / c->num_kv_heads;
   p.R = p.G * a->q_len;
-  p.NT = (p.R + 15) / 16;
-  const int64_t units = static_cast<int64_t>(c->num_seqs) * c->num_kv_heads;
+  const int max_rows = 16 * kKv4MaxNT(a->dtype == MD_BF16);
+  p.passes = (p.R + max_rows - 1) / max_rows;
+  p.NT = (std::min(p.R, max_rows) + 15) / 16;
+  const int64_t units = static_cast<int64_t>(c->num_seqs) * c->num_kv_heads * p.passes;
   // Most tiles of any unit: the whole context, or sinks and the union of the windows,
   // each cut at tile boundaries.
   int64_t tiles = ceil_div(a->max_kv_len, kKv4Tile);
@@ -98,10 +101,11 @@ Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode
   if (tiles * kKv4Tile > kWholeTokens && c->num_seqs <= kKv4BalMaxSeqs &&
       tiles * units < (int64_t{1} << 30)) {
     p.balanced = true;
+    const size_t rows = 16 * static_cast<size_t>(p.NT);
     p.n_blocks = static_cast<int32_t>(std::min(slots, ceil_div(tiles * units, kWaves)));
     p.part_o_bytes =
-        align_up(static_cast<size_t>(2 * p.n_blocks) * p.R * c->head_dim * sizeof(float), 256);
-    p.part_ml_bytes = align_up(static_cast<size_t>(2 * p.n_blocks) * p.R * 2 * sizeof(float), 256);
+        align_up(static_cast<size_t>(2 * p.n_blocks) * rows * c->head_dim * sizeof(float), 256);
+    p.part_ml_bytes = align_up(static_cast<size_t>(2 * p.n_blocks) * rows * 2 * sizeof(float), 256);
     p.workspace_bytes = p.part_o_bytes + p.part_ml_bytes;
   }
   return p;
