@@ -91,9 +91,10 @@ int run_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int
   p.o = a->o;
   p.lse = a->lse;
   if (pl.balanced) {
-    p.part_o = static_cast<float*>(a->workspace);
-    p.part_ml =
-        reinterpret_cast<float*>(static_cast<unsigned char*>(a->workspace) + pl.part_o_bytes);
+    unsigned char* ws = static_cast<unsigned char*>(a->workspace);
+    p.part_o = reinterpret_cast<float*>(ws);
+    p.part_ml = reinterpret_cast<float*>(ws + pl.part_o_bytes);
+    p.joins = reinterpret_cast<Join*>(ws + pl.part_o_bytes + pl.part_ml_bytes);
   }
   return status(launch_kv4_attn(p, pl, c->head_dim, a->dtype == MD_BF16,
                                 static_cast<hipStream_t>(stream)));

@@ -44,6 +44,12 @@ hipError_t launch_kv4_append(const Kv4RowsParams& p, int head_dim, bool bf16, bo
 hipError_t launch_kv4_read(const Kv4RowsParams& p, int head_dim, bool bf16, bool paged,
                            hipStream_t s);
 
+// The unit (sequence b, unit j) that a range boundary cuts first: its pieces are those of ranges
+// w - 1 (partial slot `first`) .. `last`.  b < 0: none.
+struct Join {
+  int32_t b, j, last, first;
+};
+
 struct Kv4AttnParams {
   Kv4View c;
   const void* q;
@@ -58,6 +64,7 @@ struct Kv4AttnParams {
   float* lse;
   float* part_o;              // balanced: [2 * workgroups][16 NT][d], unnormalised
   float* part_ml;             // balanced: [2 * workgroups][16 NT][2]: running max (log2), sum
+  Join* joins;                // balanced: [workgroups]
 };
 
 hipError_t launch_kv4_attn(const Kv4AttnParams& p, const Kv4Plan& pl, int head_dim, bool bf16,

@@ -33,6 +33,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef const __attribute__((address_space(1))) unsigned char global_bytes;
 
 namespace {
 
@@ -57,15 +58,30 @@ __device__ __forceinline__ u32x4 values8(uint32_t codes, float scale) {
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
 }
 template <int N>
-__device__ __forceinline__ void load_words(const unsigned char* at, uint32_t (&w)[N]) {
+__device__ __forceinline__ void load_words(global_bytes* at, uint32_t (&w)[N]) {
   typedef uint32_t vec __attribute__((ext_vector_type(N)));
-  const vec x = __builtin_nontemporal_load(reinterpret_cast<const vec*>(at));
+  const vec x =
+      __builtin_nontemporal_load((const __attribute__((address_space(1))) vec*)(at));
 #pragma unroll
   for (int i = 0; i < N; ++i) w[i] = x[i];
+}
+// base + off, the same for the whole wave (but for small pages): kept in scalar registers, so
+// that a lane's own offset needs no 64-bit addition.  The empty asm hides the sum from the
+// compiler, which would otherwise add the lane's offset to the base outside the loop.
+template <int PG>
+__device__ __forceinline__ global_bytes* block_ptr(const unsigned char* base, int64_t off) {
+  uintptr_t at = reinterpret_cast<uintptr_t>(base) + static_cast<uintptr_t>(off);
+  if constexpr (PG != 2) asm("" : "+s"(at));
+  return reinterpret_cast<global_bytes*>(at);
 }
 // The scale's power of two; byte 255 becomes infinity's pattern with a mantissa bit: NaN.
 __device__ __forceinline__ float scale_of(uint32_t byte) {
   return __uint_as_float((byte << 23) | (byte == 255u ? 0x400000u : 0u));
+}
+
+// The bits below bit n: none for n <= 0, all from 32 on.
+__device__ __forceinline__ uint32_t below(int n) {
+  return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u);
 }
 
 // ---- the tiles of a sequence ----
@@ -180,21 +196,26 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 
 // PG: 0 contiguous, 1 pages of at least 16 tokens, 2 smaller pages.
 template <int D, bool BF16, int NT, int PG>
-__global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(NT <= 2 && BF16 ? 2 : 1)))
+__global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(kKv4Resident(BF16, NT))))
 kv4_attn_kernel(const Kv4AttnParams p) {
   constexpr int LB = D / 8;         // code bytes a lane loads of a token: D / 4 channels
   constexpr int LW = LB / 4;        // their dwords: MFMA steps over the channels
   constexpr int CB = D / 16;        // 16-channel blocks of O
   constexpr int PARTS = BF16 ? 1 : 3;
   constexpr int ROWS = NT * 16;
-  constexpr int DEPTH = 2;          // tiles in flight a wave
-  constexpr int VROW = D * 2 + 32;  // bytes of a staged V row
+  constexpr int DEPTH = 1;          // tiles in flight a wave
+  constexpr int kAhead = 4;         // channel blocks of V read ahead of their use
+  constexpr int VROW = D * 2 + 16;  // bytes of a staged V row
+  constexpr int QROW = D * 2 + 16;  // bytes of a staged row of Q (of one part)
   constexpr int MROW = D + 4;       // floats of a row in the waves' merge
-  constexpr int kMergeO = W * ROWS * MROW * 4;
-  constexpr int kMerge = kMergeO + 2 * W * ROWS * 4;
-  constexpr int kScan = kKv4BalMaxSeqs * 4;
+  // LDS: the scan of the lengths; then Q, the waves' V tiles, and over those their O of one
+  // row tile at a time.
+  constexpr int kQ = PARTS * ROWS * QROW;
   constexpr int kV = W * T * VROW;
-  constexpr int kLds = kV > kMerge ? (kV > kScan ? kV : kScan) : (kMerge > kScan ? kMerge : kScan);
+  constexpr int kMergeO = W * 16 * MROW * 4;
+  constexpr int kMl = 2 * W * ROWS * 4;
+  constexpr int kWork = kV > kMergeO ? kV : kMergeO;
+  constexpr int kLds = kQ + kMl + kWork > kKv4BalMaxSeqs * 4 ? kQ + kMl + kWork : kKv4BalMaxSeqs * 4;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kLds];
 
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
@@ -206,11 +227,19 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     c.TT = scan_tiles(p, sl);
     c.NW = ranges(static_cast<int>(gridDim.x), c.TT);
     const int w = static_cast<int>(blockIdx.x);
+    Join join{-1, 0, 0, 0};
+    if (w < c.NW) {
+      c.t = range_start(c, w);
+      c.hi = range_start(c, w + 1);
+      unit_at(p, sl, c.t, c);
+      // The boundary where this range begins cuts a unit, as its first?  Then join it later.
+      if (c.t != c.g0 && range_start(c, w - 1) <= c.g0)
+        join = Join{c.b, c.j, range_of(c, c.g0 + c.gt - 1),
+                    2 * (w - 1) + (range_start(c, w - 1) != c.g0)};
+    }
+    if (tid == 0) p.joins[w] = join;
     if (w >= c.NW) return;  // the whole workgroup
-    c.t = range_start(c, w);
-    c.hi = range_start(c, w + 1);
-    unit_at(p, sl, c.t, c);
-    __syncthreads();  // the LDS is reused
+    __syncthreads();        // the LDS is reused
   } else {
     c.b = static_cast<int>(blockIdx.x) / p.units;
     c.j = static_cast<int>(blockIdx.x) % p.units;
@@ -233,37 +262,11 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     const int n_tiles = min(lt1, u.n) - lt0;  // <= 0: nothing visible
 
     int row_pos[NT];  // position of this lane's query rows; padding rows see nothing
-    u32x4 q[NT][PARTS][LW];
 #pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
       const int r = rt * 16 + l16;
-      const bool live = r < rows;
-      row_pos[rt] = live ? S - p.L + (r0 + r) / p.G : -1;
-      const int64_t e = live ? out_row(p, b, hk, r0 + r) * D + grp * (D / 4) : 0;
-#pragma unroll
-      for (int w = 0; w < LW; ++w) {
-        if constexpr (BF16) {
-          q[rt][0][w] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + e + w * 8);
-        } else {
-          const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(p.q) + e + w * 8);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            f32x4 x = src[h];
-#pragma unroll
-            for (int k = 0; k < PARTS; ++k) {  // the leading 8 bits, then those of the rest
-              const uint32_t a0 = pack2(x[0], x[1]), a1 = pack2(x[2], x[3]);
-              q[rt][k][w][2 * h] = a0;
-              q[rt][k][w][2 * h + 1] = a1;
-              x = f32x4{x[0] - lo_f32(a0), x[1] - hi_f32(a0), x[2] - lo_f32(a1), x[3] - hi_f32(a1)};
-            }
-          }
-        }
-        if (!live)
-#pragma unroll
-          for (int k = 0; k < PARTS; ++k) q[rt][k][w] = u32x4{0, 0, 0, 0};
-      }
+      row_pos[rt] = r < rows ? S - p.L + (r0 + r) / p.G : -1;
     }
-
     // ---- loads ----
     struct TileRegs {
       uint32_t k[2][LW], v[2][LW];
@@ -271,7 +274,9 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     };
     const int pmask = (1 << p.c.page_shift) - 1;
     const int32_t* ptab = PG ? p.c.page_table + static_cast<int64_t>(b) * p.c.max_pages : nullptr;
-    const int64_t head_off = static_cast<int64_t>(hk) * p.c.s_head;
+    // Byte offset of the head's rows (contiguous: of the sequence's), added to every block's.
+    const int64_t unit_off = static_cast<int64_t>(hk) * p.c.s_head +
+                             (PG ? 0 : static_cast<int64_t>(b) * p.c.s_blk);
     const uint32_t s_tok = static_cast<uint32_t>(p.c.s_tok);
     const uint32_t sidx = grp * (D / 4) / 32;  // this lane's scale byte in its row
     auto real_tile = [&](int v) { return v < u.head ? v : v - u.head + u.tail0; };
@@ -306,8 +311,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
         int64_t base;
         uint32_t code = code_off, scale = scale_off;
         if constexpr (PG == 0) {
-          base = static_cast<int64_t>(b) * p.c.s_blk + head_off +
-                 static_cast<int64_t>(bt) * p.c.s_tok;
+          base = unit_off + static_cast<int64_t>(static_cast<uint64_t>(bt) * s_tok);
           if (bt + 16 > p.c.capacity) {  // the cache ends inside the block
             const uint32_t dt = static_cast<uint32_t>(min(l16, S - 1 - bt));
             code = dt * s_tok + grp * LB;
@@ -315,21 +319,70 @@ kv4_attn_kernel(const Kv4AttnParams p) {
           }
         } else if constexpr (PG == 1) {
           const int id = __builtin_amdgcn_readlane(ids, (k & 31) * 2 + tb);
-          base = static_cast<int64_t>(id) * p.c.s_blk + head_off +
-                 static_cast<int64_t>(bt & pmask) * p.c.s_tok;
+          base = unit_off + static_cast<int64_t>(id) * p.c.s_blk +
+                 static_cast<int64_t>(static_cast<uint64_t>(bt & pmask) * s_tok);
         } else {
           const int t = min(bt + l16, S - 1);
-          base = static_cast<int64_t>(page_ok(ptab[t >> p.c.page_shift])) * p.c.s_blk + head_off +
-                 static_cast<int64_t>(t & pmask) * p.c.s_tok;
+          base = unit_off + static_cast<int64_t>(page_ok(ptab[t >> p.c.page_shift])) * p.c.s_blk +
+                 static_cast<int64_t>(static_cast<uint64_t>(t & pmask) * s_tok);
           code = grp * LB;
           scale = sidx;
         }
-        load_words(p.c.k + base + code, r.k[tb]);
-        load_words(p.c.v + base + code, r.v[tb]);
-        r.ks[tb] = *(p.c.ks + (base >> 4) + scale);
-        r.vs[tb] = *(p.c.vs + (base >> 4) + scale);
+        asm("" : "+v"(code), "+v"(scale));  // 32 bits up to the load: see block_ptr
+        load_words(block_ptr<PG>(p.c.k, base) + code, r.k[tb]);
+        load_words(block_ptr<PG>(p.c.v, base) + code, r.v[tb]);
+        r.ks[tb] = *(block_ptr<PG>(p.c.ks, base >> 4) + scale);
+        r.vs[tb] = *(block_ptr<PG>(p.c.vs, base >> 4) + scale);
       }
     };
+
+    // The first tiles' loads, before anything waits.
+    const int mine = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // tiles of this wave
+    TileRegs ring[DEPTH];
+    if (mine > 0) {
+      ids = load_ids(0);
+      ids_next = load_ids(32);
+#pragma unroll
+      for (int s = 0; s < DEPTH; ++s) {
+        // In the order of the loop's refills: a wait for one tile leaves the later ones in flight.
+        __builtin_amdgcn_sched_barrier(0);
+        load_tile(ring[s], s);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    // Q into LDS (its registers are worth more: a third wave per SIMD), fp32 as three bf16 parts:
+    // the leading 8 bits, then those of what is left.
+    unsigned char* q_lds = lds;
+    for (int item = tid; item < ROWS * (D / 8); item += W * 64) {
+      const int r = item / (D / 8), c0 = item % (D / 8) * 8;
+      const int64_t e = r < rows ? out_row(p, b, hk, r0 + r) * D + c0 : 0;
+      if constexpr (BF16) {
+        u32x4 x = {0, 0, 0, 0};
+        if (r < rows) x = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + e);
+        *reinterpret_cast<u32x4*>(q_lds + r * QROW + c0 * 2) = x;
+      } else {
+        f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        if (r < rows) {
+          const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(p.q) + e);
+          x[0] = src[0];
+          x[1] = src[1];
+        }
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+          u32x4 w;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            w[2 * h] = pack2(x[h][0], x[h][1]);
+            w[2 * h + 1] = pack2(x[h][2], x[h][3]);
+            x[h] = f32x4{x[h][0] - lo_f32(w[2 * h]), x[h][1] - hi_f32(w[2 * h]),
+                         x[h][2] - lo_f32(w[2 * h + 1]), x[h][3] - hi_f32(w[2 * h + 1])};
+          }
+          *reinterpret_cast<u32x4*>(q_lds + (k * ROWS + r) * QROW + c0 * 2) = w;
+        }
+      }
+    }
+    __syncthreads();
 
     float m_run[NT], l_run[NT];  // log2; 0 and a threshold of -inf: no key seen yet
     float lazy[NT];
@@ -344,7 +397,8 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) acc[rt][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    unsigned char* vt = lds + wave * (T * VROW);
+    unsigned char* vt = lds + kQ + kMl + wave * (T * VROW);
+    const unsigned char* q_lane = q_lds + l16 * QROW + grp * (D / 2);
     constexpr float kLazy = 8.f;
 
     auto visible = [&](int t, int pos) {
@@ -389,24 +443,47 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       // S^T = K Q^T.
       f32x4 s[NT][2];
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb) {
+      for (int rt = 0; rt < NT; ++rt)
 #pragma unroll
-        for (int rt = 0; rt < NT; ++rt) s[rt][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const float ks = scale_of(r.ks[tb]);
+        for (int tb = 0; tb < 2; ++tb) s[rt][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const float ks[2] = {scale_of(r.ks[0]), scale_of(r.ks[1])};
 #pragma unroll
-        for (int w = 0; w < LW; ++w) {
-          const bf16x8 kk = __builtin_bit_cast(bf16x8, values8(r.k[tb][w], ks));
+      for (int w = 0; w < LW; ++w) {
+        bf16x8 kk[2];
 #pragma unroll
-          for (int rt = 0; rt < NT; ++rt)
+        for (int tb = 0; tb < 2; ++tb)
+          kk[tb] = __builtin_bit_cast(bf16x8, values8(r.k[tb][w], ks[tb]));
 #pragma unroll
-            for (int k = PARTS - 1; k >= 0; --k)
-              s[rt][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  kk, __builtin_bit_cast(bf16x8, q[rt][k][w]), s[rt][tb], 0, 0, 0);
-        }
+        for (int k = PARTS - 1; k >= 0; --k)
+#pragma unroll
+          for (int rt = 0; rt < NT; ++rt) {
+            const bf16x8 qq = *reinterpret_cast<const bf16x8*>(
+                q_lane + (k * ROWS + rt * 16) * QROW + w * 16);
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+              s[rt][tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk[tb], qq, s[rt][tb], 0, 0, 0);
+          }
       }
 
       __builtin_amdgcn_sched_barrier(0);
       refill();
+      // V^T for the first channel blocks, under way during the softmax.  Transposed reads:
+      // lane k of a 16-lane group supplies row 4 grp + k / 4 and channels cb*16 + 4 (k % 4)
+      // .. + 3, and lane i gets channel cb*16 + i of those rows.
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      auto read_v = [&](int cb) {
+        const unsigned char* src =
+            vt + (4 * grp + (l16 >> 2)) * VROW + (cb * 16 + 4 * (l16 & 3)) * 2;
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src));
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * VROW));
+        const u32x2 a = __builtin_bit_cast(u32x2, lo), d = __builtin_bit_cast(u32x2, hi);
+        return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], d[0], d[1]});
+      };
+      bf16x8 va[kAhead];
+#pragma unroll
+      for (int cb = 0; cb < kAhead; ++cb) va[cb] = read_v(cb);
       __builtin_amdgcn_sched_barrier(0);
 
       // Softmax weights 2^y, y = c s - m, c = scale * log2 e: lane's row l16, tokens tb*16 + 4
@@ -417,17 +494,16 @@ kv4_attn_kernel(const Kv4AttnParams p) {
         const int first = t0 + 4 * grp;
 #pragma unroll
         for (int rt = 0; rt < NT; ++rt) {
-          // visible() of this lane's tokens, relative to its first: up to `last`, and above
-          // `gone` or below `sinks`.  (Padding rows see none: their `last` is below 0.)
-          const int last = row_pos[rt] - first, sinks = p.n_sink - first;
-          const int gone = p.mode == MD_MODE_DRAFT
-                               ? static_cast<int>(static_cast<uint32_t>(last) - p.window)
-                               : INT32_MIN;
+          // visible() of this lane's tokens as bits, relative to its first.
+          // (Padding rows see none: their `last` is below 0.)
+          const int last = row_pos[rt] - first;
+          uint32_t seen = below(last + 1);
+          if (p.mode == MD_MODE_DRAFT)
+            seen &= ~below(static_cast<int>(static_cast<uint32_t>(last) - p.window + 1u)) |
+                    below(p.n_sink - first);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int t = j / 4 * 16 + j % 4;
-            if (!(t <= last && (t > gone || t < sinks))) s[rt][j / 4][j % 4] = -INFINITY;
-          }
+          for (int j = 0; j < 8; ++j)
+            if (!((seen >> (j / 4 * 16 + j % 4)) & 1u)) s[rt][j / 4][j % 4] = -INFINITY;
         }
       }
       u32x4 pb[NT][PARTS];
@@ -472,44 +548,24 @@ kv4_attn_kernel(const Kv4AttnParams p) {
           }
       }
 
-      // O^T += V^T P^T.  Transposed reads: lane k of a 16-lane group supplies row 4 grp + k / 4
-      // and channels cb*16 + 4 (k % 4) .. + 3, and lane i gets channel cb*16 + i of those rows.
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      // O^T += V^T P^T.
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
-        const unsigned char* src =
-            vt + (4 * grp + (l16 >> 2)) * VROW + (cb * 16 + 4 * (l16 & 3)) * 2;
-        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src));
-        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + 16 * VROW));
-        const u32x2 a = __builtin_bit_cast(u32x2, lo), d = __builtin_bit_cast(u32x2, hi);
-        const bf16x8 va = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], d[0], d[1]});
+        const bf16x8 v_now = va[cb % kAhead];
+        if (cb + kAhead < CB) va[cb % kAhead] = read_v(cb + kAhead);
 #pragma unroll
         for (int rt = 0; rt < NT; ++rt)
 #pragma unroll
           for (int k = PARTS - 1; k >= 0; --k)
             acc[rt][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                va, __builtin_bit_cast(bf16x8, pb[rt][k]), acc[rt][cb], 0, 0, 0);
+                v_now, __builtin_bit_cast(bf16x8, pb[rt][k]), acc[rt][cb], 0, 0, 0);
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
 
-    // Tiles of this wave.
-    const int mine = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;
     if (mine > 0) {
-      TileRegs ring[DEPTH];
-      ids = load_ids(0);
-      ids_next = load_ids(32);
-#pragma unroll
-      for (int s = 0; s < DEPTH; ++s) {
-        // In the order of the loop's refills: a wait for one tile leaves the later ones in flight.
-        __builtin_amdgcn_sched_barrier(0);
-        load_tile(ring[s], s);
-      }
-      __builtin_amdgcn_sched_barrier(0);
       auto one = [&](TileRegs& r, int k, auto refill) {
         const int t0 = real_tile(lt0 + wave + k * W) * T;
         bool masked = t0 + T - 1 > S - p.L;
@@ -551,49 +607,52 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       l_run[rt] += __shfl_xor(l_run[rt], 16);
       l_run[rt] += __shfl_xor(l_run[rt], 32);
     }
-    __syncthreads();
-    float* mo = reinterpret_cast<float*>(lds);
-    float* sm = reinterpret_cast<float*>(lds + kMergeO);
+    float* sm = reinterpret_cast<float*>(lds + kQ);
     float* sl = sm + W * ROWS;
+    float* mo = sl + W * ROWS;
+    if (grp == 0) {
 #pragma unroll
-    for (int rt = 0; rt < NT; ++rt) {
-      if (grp == 0) {
+      for (int rt = 0; rt < NT; ++rt) {
         sm[wave * ROWS + rt * 16 + l16] = lazy[rt] == -INFINITY ? -INFINITY : m_run[rt];
         sl[wave * ROWS + rt * 16 + l16] = l_run[rt];
       }
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb)
-        *reinterpret_cast<f32x4*>(mo + (wave * ROWS + rt * 16 + l16) * MROW + cb * 16 + grp * 4) =
-            acc[rt][cb];
     }
-    __syncthreads();
     // A cut unit's piece: slot 2w for the first piece of range w, 2w + 1 for its last.
     const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) +
                          (p.balanced && c.t != range_start(c, static_cast<int>(blockIdx.x)));
-    constexpr int kQuads = D / 4;
-    for (int item = tid; item < rows * kQuads; item += W * 64) {
-      const int r = item / kQuads, c0 = item % kQuads * 4;
-      float M = -INFINITY;
-      for (int w = 0; w < W; ++w) M = fmaxf(M, sm[w * ROWS + r]);
-      const float m_use = M == -INFINITY ? 0.f : M;
-      float L = 0.f;
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      for (int w = 0; w < W; ++w) {
-        const float f = exp2_fast(sm[w * ROWS + r] - m_use);
-        L += f * sl[w * ROWS + r];
-        const f32x4 x = *reinterpret_cast<const f32x4*>(mo + (w * ROWS + r) * MROW + c0);
-        for (int j = 0; j < 4; ++j) o[j] += f * x[j];
-      }
-      if (whole) {
-        const int64_t row = out_row(p, b, hk, r0 + r);
-        const float inv = inverse(L);
-        for (int j = 0; j < 4; ++j) o[j] *= inv;
-        store4<BF16>(p, row * D + c0, o);
-        if (c0 == 0 && p.lse) p.lse[row] = lse_of(M, L);
-      } else {
-        *reinterpret_cast<f32x4*>(p.part_o + (slot * ROWS + r) * D + c0) = o;
-        if (c0 == 0)
-          *reinterpret_cast<f32x2*>(p.part_ml + (slot * ROWS + r) * 2) = f32x2{M, L};
+#pragma unroll
+    for (int rt = 0; rt < NT; ++rt) {
+      __syncthreads();  // the V tiles, or the last row tile's O, are done with
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+        *reinterpret_cast<f32x4*>(mo + (wave * 16 + l16) * MROW + cb * 16 + grp * 4) = acc[rt][cb];
+      __syncthreads();
+      constexpr int kQuads = D / 4;
+      for (int item = tid; item < 16 * kQuads; item += W * 64) {
+        const int rr = item / kQuads, r = rt * 16 + rr, c0 = item % kQuads * 4;
+        if (r >= rows) break;
+        float M = -INFINITY;
+        for (int w = 0; w < W; ++w) M = fmaxf(M, sm[w * ROWS + r]);
+        const float m_use = M == -INFINITY ? 0.f : M;
+        float L = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < W; ++w) {
+          const float f = exp2_fast(sm[w * ROWS + r] - m_use);
+          L += f * sl[w * ROWS + r];
+          const f32x4 x = *reinterpret_cast<const f32x4*>(mo + (w * 16 + rr) * MROW + c0);
+          for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+        }
+        if (whole) {
+          const int64_t row = out_row(p, b, hk, r0 + r);
+          const float inv = inverse(L);
+          for (int j = 0; j < 4; ++j) o[j] *= inv;
+          store4<BF16>(p, row * D + c0, o);
+          if (c0 == 0 && p.lse) p.lse[row] = lse_of(M, L);
+        } else {
+          *reinterpret_cast<f32x4*>(p.part_o + (slot * ROWS + r) * D + c0) = o;
+          if (c0 == 0)
+            *reinterpret_cast<f32x2*>(p.part_ml + (slot * ROWS + r) * 2) = f32x2{M, L};
+        }
       }
     }
 
@@ -610,41 +669,63 @@ kv4_attn_kernel(const Kv4AttnParams p) {
   }
 }
 
-// Joins the pieces of the units that range boundaries cut: workgroup w takes the unit
-// that boundary w crosses, if it is the unit's first.
+// Joins the pieces of the units that range boundaries cut: workgroup (w, y) takes rows
+// 4 y .. of the unit whose first cut is where range w begins, if it is one.  The waves take the
+// pieces in turn (fixed order), then their sums are joined through LDS.
 template <int D, bool BF16, int NT>
-__global__ void __launch_bounds__(W * 64) kv4_join_kernel(const Kv4AttnParams p) {
-  __shared__ int sl[kKv4BalMaxSeqs];
-  Cursor c{};
-  c.TT = scan_tiles(p, sl);
-  c.NW = ranges(static_cast<int>(gridDim.x), c.TT);
+__global__ void __launch_bounds__(W * 64) kv4_join_kernel(const Kv4AttnParams p, int rows_per_wg) {
+  constexpr int kQuads = D / 4, ROWS = NT * 16, kRows = 64 / kQuads;  // rows a wave takes at once
+  __shared__ __attribute__((aligned(16))) float so[W][64][4];
+  __shared__ float sm[W][64], sl[W][64];
   const int w = static_cast<int>(blockIdx.x);
-  if (w == 0 || w >= c.NW) return;
-  const int t = range_start(c, w);
-  unit_at(p, sl, t, c);
-  if (t == c.g0 || range_start(c, w - 1) > c.g0) return;  // no cut, or not the first
-  const int w0 = w - 1, w1 = range_of(c, c.g0 + c.gt - 1);
-  const int first = 2 * w0 + (range_start(c, w0) != c.g0);
-  constexpr int kQuads = D / 4, ROWS = NT * 16;
-  const int hk = c.j / p.passes, r0 = c.j % p.passes * ROWS;
+  const Join join = p.joins[w];
+  if (join.b < 0) return;  // the whole workgroup
+  const int hk = join.j / p.passes, r0 = join.j % p.passes * ROWS;
   const int rows = min(p.R - r0, ROWS);
-  for (int item = threadIdx.x; item < rows * kQuads; item += W * 64) {
-    const int r = item / kQuads, c0 = item % kQuads * 4;
-    float M = -INFINITY;
-    for (int k = w0; k <= w1; ++k)
-      M = fmaxf(M, p.part_ml[(static_cast<int64_t>(k == w0 ? first : 2 * k) * ROWS + r) * 2]);
-    const float m_use = M == -INFINITY ? 0.f : M;
-    float L = 0.f;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c0 = lane % kQuads * 4;
+  const int n = join.last - w + 2;  // pieces: ranges w - 1 .. last
+  // With few pieces each wave takes rows of its own instead.
+  const bool split = n > W;
+  const int first = static_cast<int>(blockIdx.y) * rows_per_wg;
+  const int end = min(rows, first + rows_per_wg);
+  for (int rb = first + (split ? 0 : wave * kRows); rb < end; rb += split ? kRows : W * kRows) {
+    const int r = rb + lane / kQuads;
+    const bool live = r < end;
+    float M = -INFINITY, L = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k = w0; k <= w1; ++k) {
-      const int64_t row = static_cast<int64_t>(k == w0 ? first : 2 * k) * ROWS + r;
+#pragma unroll 4
+    for (int k = split ? wave : 0; k < n; k += split ? W : 1) {
+      const int64_t row =
+          static_cast<int64_t>(k == 0 ? join.first : 2 * (w - 1 + k)) * ROWS + (live ? r : first);
       const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + row * 2);
       const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + row * D + c0);
-      const float f = exp2_fast(ml[0] - m_use);
-      L += f * ml[1];
-      for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+      const float m_new = fmaxf(M, ml[0]);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float f = exp2_fast(M - m_use), g = exp2_fast(ml[0] - m_use);
+      L = L * f + ml[1] * g;
+      for (int j = 0; j < 4; ++j) o[j] = o[j] * f + x[j] * g;
+      M = m_new;
     }
-    const int64_t row = out_row(p, c.b, hk, r0 + r);
+    if (split) {
+      __syncthreads();  // the last rows' sums are read
+      *reinterpret_cast<f32x4*>(so[wave][lane]) = o;
+      sm[wave][lane] = M;
+      sl[wave][lane] = L;
+      __syncthreads();
+      if (wave != 0) continue;
+      for (int k = 1; k < W; ++k) M = fmaxf(M, sm[k][lane]);
+      const float m_use = M == -INFINITY ? 0.f : M;
+      L = 0.f;
+      o = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int k = 0; k < W; ++k) {
+        const float f = exp2_fast(sm[k][lane] - m_use);
+        L += f * sl[k][lane];
+        for (int j = 0; j < 4; ++j) o[j] += f * so[k][lane][j];
+      }
+    }
+    if (!live) continue;
+    const int64_t row = out_row(p, join.b, hk, r0 + r);
     const float inv = inverse(L);
     for (int j = 0; j < 4; ++j) o[j] *= inv;
     store4<BF16>(p, row * D + c0, o);
@@ -663,7 +744,12 @@ hipError_t launch_nt(const Kv4AttnParams& p, const Kv4Plan& pl, hipStream_t s) {
     hipLaunchKernelGGL((kv4_attn_kernel<D, BF16, NT, 2>), g, blk, 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !pl.balanced) return e;
-  hipLaunchKernelGGL((kv4_join_kernel<D, BF16, NT>), g, blk, 0, s, p);
+  // Units cut in many pieces are few: their rows go to several workgroups, four each.
+  const int rows = NT * 16 < p.R ? NT * 16 : p.R;
+  const bool many = pl.n_blocks > 4 * static_cast<int64_t>(p.B) * p.units;
+  const int per_wg = many && rows > 4 ? 4 : rows;
+  const dim3 gj(g.x, static_cast<uint32_t>((rows + per_wg - 1) / per_wg));
+  hipLaunchKernelGGL((kv4_join_kernel<D, BF16, NT>), gj, blk, 0, s, p, per_wg);
   return hipGetLastError();
 }
 

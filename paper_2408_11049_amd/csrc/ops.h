@@ -17,6 +17,8 @@ constexpr int kKv4Tile = 32;
 constexpr int64_t kKv4MaxTokStride = int64_t{1} << 25;
 // Row tiles of 16 a pass over K and V takes: an fp32 query is three registers' worth of bf16.
 constexpr int kKv4MaxNT(bool bf16) { return bf16 ? 4 : 2; }
+// Workgroups a compute unit holds, a wave per SIMD each (their instances' registers).
+constexpr int kKv4Resident(bool bf16, int NT) { return bf16 && NT <= 2 ? 3 : 2; }
 // The balanced plan ranks every sequence's tiles in each workgroup.
 constexpr int kKv4BalMaxSeqs = 1024;
 
@@ -29,7 +31,7 @@ struct Kv4Plan {
   int32_t NT = 0, passes = 1;     // 16-row tiles of a pass over K and V, and passes
   bool balanced = false;
   int32_t n_blocks = 0;           // workgroups
-  size_t part_o_bytes = 0, part_ml_bytes = 0, workspace_bytes = 0;
+  size_t part_o_bytes = 0, part_ml_bytes = 0, workspace_bytes = 0;  // then 16 bytes a workgroup
 };
 int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
                          int window);

@@ -96,7 +96,7 @@ Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode
     tiles = std::min(tiles, ceil_div(n_sink, kKv4Tile) +
                                 ceil_div(int64_t{window} + a->q_len - 1, kKv4Tile) + 1);
   const int64_t cus = num_cus > 0 ? num_cus : 256;
-  const int64_t slots = cus * (p.NT <= 2 ? 2 : 1);
+  const int64_t slots = cus * kKv4Resident(a->dtype == MD_BF16, p.NT);
   p.n_blocks = static_cast<int32_t>(units);
   if (tiles * kKv4Tile > kWholeTokens && c->num_seqs <= kKv4BalMaxSeqs &&
       tiles * units < (int64_t{1} << 30)) {
@@ -106,7 +106,8 @@ Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode
     p.part_o_bytes =
         align_up(static_cast<size_t>(2 * p.n_blocks) * rows * c->head_dim * sizeof(float), 256);
     p.part_ml_bytes = align_up(static_cast<size_t>(2 * p.n_blocks) * rows * 2 * sizeof(float), 256);
-    p.workspace_bytes = p.part_o_bytes + p.part_ml_bytes;
+    p.workspace_bytes =
+        p.part_o_bytes + p.part_ml_bytes + align_up(static_cast<size_t>(p.n_blocks) * 16, 256);
   }
   return p;
 }
