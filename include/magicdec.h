@@ -597,7 +597,8 @@ size_t md_kv4_workspace_bytes(const md_kv4_cache* c, const md_kv4_attn_args* a, 
  *   u             device fp32 [B, L], uniform in [0, 1): entry n_draft draws t
  *   accepted      device int32 [B] out
  *   tokens        device int32 [B, L] out
- *   workspace     >= md_spec_accept_workspace_bytes(), 256-byte aligned, any contents
+ *   workspace     >= md_spec_accept_workspace_bytes() (0: none), 256-byte aligned, any
+ *                 contents
  * Only the rows p_a and q_a are read whole.  Errors: MD_ERR_INVALID_ARG for NULL or
  * misaligned pointers (probabilities: their element size), n_draft outside [0, 1023],
  * vocab outside [1, 2^30], a bad dtype; MD_ERR_UNSUPPORTED for num_seqs > 2^25 - 1;

@@ -283,19 +283,18 @@ def _device_scoped(fn):
     scoped = _stream_scoped(fn)
 
     @functools.wraps(fn)
-    def wrapped(first, *args, **kw):
-        t = first[0] if isinstance(first, tuple) else first
+    def wrapped(first, *args, stream=None, **kw):
+        t = first.k if type(first) is Kv4Cache else first
         dev = t.get_device()
+        torch = _torch_module or _torch()
         if dev < 0:
             raise ValueError(f"tensors must be on a GPU, not {t.device}")
-        stream = kw.get("stream")
+        if stream is None and torch._C._cuda_getDevice() == dev:
+            return fn(first, *args, stream=None, **kw)
         if stream is not None and stream.device.index != dev:
             raise ValueError(f"stream is on {stream.device}; the call runs on {t.device}")
-        torch = _torch()
-        if torch.cuda.current_device() == dev:
-            return scoped(first, *args, **kw)
         with torch.cuda.device(dev):
-            return scoped(first, *args, **kw)
+            return scoped(first, *args, stream=stream, **kw)
     return wrapped
 
 
@@ -328,6 +327,14 @@ def _on_gpu(ref, **tensors):
     for name, t in tensors.items():
         if t is not None and t.device != ref.device:
             raise ValueError(f"{name} is on {t.device}; the call runs on {ref.device}")
+
+
+def _same_gpu(ref, **tensors):
+    """_on_gpu, at the cost of a comparison for each tensor."""
+    gpu = ref.get_device()
+    for t in tensors.values():
+        if gpu < 0 or (t is not None and t.get_device() != gpu):
+            _on_gpu(ref, **tensors)
 
 
 def _ints(name, t, n):
@@ -853,47 +860,57 @@ def kv4_empty(blocks, tokens, num_kv_heads, head_dim, device="cuda") -> Kv4Cache
                     empty(head_dim // 32))
 
 
+def _kv4_scales(shape, st, ks, vs):
+    """Raise unless the scale tensors' strides are the codes' / 16, where a dimension has one."""
+    for t in (ks, vs):
+        for n, a, b in zip(shape[:3], st, t.stride()):
+            if n > 1 and a != 16 * b:
+                raise ValueError("the scales' strides must be the codes' / 16")
+        if t.shape[3] > 1 and t.stride(3) != 1:
+            raise ValueError("the scales of a row must be contiguous")
+
+
 def make_kv4_cache(cache, *, num_seqs=None, page_table=None) -> MdKv4Cache:
     """Fill md_kv4_cache from the cache's tensors (no data is read or moved)."""
-    torch = _torch()
     k, v, ks, vs = cache
-    shape, st, u8 = k.shape, k.stride(), torch.uint8
+    shape, st = k.shape, k.stride()
     if len(shape) != 4 or v.shape != shape or v.stride() != st or st[3] != 1:
         raise ValueError("cache k and v must be 4-D with equal shapes and strides, codes unit-stride")
+    u8 = (_torch_module or _torch()).uint8
     if k.dtype != u8 or v.dtype != u8 or ks.dtype != u8 or vs.dtype != u8:
         raise ValueError("a 4-bit cache's tensors are uint8")
-    half = shape[3]
-    if half % 16 or ks.shape != shape[:3] + (half // 16,) or vs.shape != ks.shape:
+    blocks, toks, heads, half = shape
+    if half % 16 or ks.shape != (blocks, toks, heads, half // 16) or vs.shape != ks.shape:
         raise ValueError("k_scale and v_scale must be [.., d / 32] for codes [.., d / 2]")
     gpu = k.get_device()
     if gpu < 0 or v.get_device() != gpu or ks.get_device() != gpu or vs.get_device() != gpu or (
             page_table is not None and page_table.get_device() != gpu):
         _on_gpu(k, v=v, k_scale=ks, v_scale=vs, page_table=page_table)
-    # A dimension of size one has no stride of its own; every other one is the codes' / 16.
-    for t in (ks, vs):
-        for n, a, b in zip(shape, st, t.stride()[:3]):
-            if n > 1 and a != 16 * b:
-                raise ValueError("the scales' strides must be the codes' / 16")
-        if half > 16 and t.stride(3) != 1:
-            raise ValueError("the scales of a row must be contiguous")
-    page = max_pages = pages = cap = 0
-    pt = None
-    if page_table is None:
-        B, cap = shape[0] if num_seqs is None else num_seqs, shape[1]
-        if B > shape[0]:
-            raise ValueError("a contiguous cache must hold num_seqs sequences")
-    else:
-        if page_table.dtype != torch.int32 or not page_table.is_contiguous() or page_table.dim() != 2:
-            raise ValueError("page_table must be contiguous int32 [B, max_pages]")
-        B = page_table.shape[0] if num_seqs is None else num_seqs
-        if page_table.shape[0] < B:
-            raise ValueError("page_table must have a row per sequence")
-        page, max_pages, pages = shape[1], page_table.shape[1], shape[0]
-        pt = page_table.data_ptr()
+    sb, stok, sh, _ = st
+    want = (sb // 16, stok // 16, sh // 16, 1)
+    if ks.stride() != want or vs.stride() != want:
+        _kv4_scales(shape, st, ks, vs)
     # The stride of a dimension of size one is never used, but must be a whole row's.
-    sb, stok, sh = (x if n > 1 else half for n, x in zip(shape[:3], st))
-    return MdKv4Cache(B, shape[2], 2 * half, k.data_ptr(), v.data_ptr(), ks.data_ptr(),
-                      vs.data_ptr(), sb, stok, sh, page, max_pages, pages, pt, cap)
+    if blocks == 1 or toks == 1 or heads == 1:
+        sb, stok, sh = (x if n > 1 else half for n, x in zip(shape[:3], st))
+    if page_table is None:
+        if num_seqs is None:
+            num_seqs = blocks
+        elif num_seqs > blocks:
+            raise ValueError("a contiguous cache must hold num_seqs sequences")
+        return MdKv4Cache(num_seqs, heads, 2 * half, k.data_ptr(), v.data_ptr(), ks.data_ptr(),
+                          vs.data_ptr(), sb, stok, sh, 0, 0, 0, None, toks)
+    if (page_table.dtype != _torch_module.int32 or not page_table.is_contiguous()
+            or page_table.dim() != 2):
+        raise ValueError("page_table must be contiguous int32 [B, max_pages]")
+    rows, max_pages = page_table.shape
+    if num_seqs is None:
+        num_seqs = rows
+    elif rows < num_seqs:
+        raise ValueError("page_table must have a row per sequence")
+    return MdKv4Cache(num_seqs, heads, 2 * half, k.data_ptr(), v.data_ptr(), ks.data_ptr(),
+                      vs.data_ptr(), sb, stok, sh, toks, max_pages, blocks,
+                      page_table.data_ptr(), 0)
 
 
 @_device_scoped
@@ -909,11 +926,12 @@ def md_kv4_append(cache, k_new, v_new, pos0, *, page_table=None, lens_out=None, 
     c = make_kv4_cache(cache, num_seqs=B, page_table=page_table)
     if B and k_new.shape[2:] != (c.num_kv_heads, c.head_dim):
         raise ValueError("appended rows must have the cache's heads and head_dim")
-    _on_gpu(cache.k, k_new=k_new, v_new=v_new, pos0=pos0, lens_out=lens_out)
+    _same_gpu(cache.k, k_new=k_new, v_new=v_new, pos0=pos0, lens_out=lens_out)
     _ints("pos0", pos0, B)
     if lens_out is None:
         lens_out = pos0.new_empty((B,))
-    _ints("lens_out", lens_out, B)
+    else:
+        _ints("lens_out", lens_out, B)
     _check(lib.md_kv4_append(ctypes.byref(c), n_new, _dtype_code(k_new), k_new.data_ptr(),
                              v_new.data_ptr(), pos0.data_ptr(), lens_out.data_ptr(),
                              _stream_handle(cache.k, stream)))
@@ -931,17 +949,17 @@ def md_kv4_read(cache, pos0, n, *, page_table=None, dtype=None, k_out=None, v_ou
     B = pos0.shape[0]
     c = make_kv4_cache(cache, num_seqs=B, page_table=page_table)
     shape = (B, n, c.num_kv_heads, c.head_dim)
-    _on_gpu(cache.k, pos0=pos0, k_out=k_out, v_out=v_out)
+    _same_gpu(cache.k, pos0=pos0, k_out=k_out, v_out=v_out)
     _ints("pos0", pos0, B)
     if dtype is None:
         dtype = torch.bfloat16 if k_out is None else k_out.dtype
-    if k_out is None:
-        k_out = torch.empty(shape, dtype=dtype, device=cache.k.device)
-    if v_out is None:
-        v_out = torch.empty(shape, dtype=dtype, device=cache.k.device)
     for t in (k_out, v_out):
-        if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
             raise ValueError("k_out and v_out must be contiguous [B, n, Hkv, d] of one dtype")
+    if k_out is None:
+        k_out = pos0.new_empty(shape, dtype=dtype)
+    if v_out is None:
+        v_out = torch.empty_like(k_out)
     _check(lib.md_kv4_read(ctypes.byref(c), n, _dtype_code(k_out), pos0.data_ptr(),
                            k_out.data_ptr(), v_out.data_ptr(), _stream_handle(cache.k, stream)))
     return k_out, v_out
@@ -1040,8 +1058,8 @@ def md_spec_accept(target_probs, draft_probs, draft, u, *, accepted=None, tokens
         raise ValueError("draft must be contiguous int32 [B, gamma]")
     if u.shape != (B, L) or u.dtype != torch.float32 or not u.is_contiguous():
         raise ValueError("u must be contiguous float32 [B, gamma + 1]")
-    _on_gpu(target_probs, draft_probs=draft_probs, draft=draft, u=u, accepted=accepted,
-            tokens=tokens, workspace=workspace)
+    _same_gpu(target_probs, draft_probs=draft_probs, draft=draft, u=u, accepted=accepted,
+              tokens=tokens, workspace=workspace)
     if accepted is None:
         accepted = draft.new_empty((B,))
     else:
@@ -1052,12 +1070,12 @@ def md_spec_accept(target_probs, draft_probs, draft, u, *, accepted=None, tokens
         _ints("tokens", tokens, B * L)
     if workspace is None:
         need = lib.md_spec_accept_workspace_bytes(B, L - 1, vocab)
-        workspace = torch.empty((max(need, 1),), dtype=torch.uint8, device=target_probs.device)
+        workspace = target_probs.new_empty((need,), dtype=torch.uint8) if need else None
     _check(lib.md_spec_accept(B, L - 1, vocab, _dtype_code(target_probs), target_probs.data_ptr(),
                               None if draft_probs is None or L == 1 else draft_probs.data_ptr(),
                               draft.data_ptr() if L > 1 else None, u.data_ptr(),
-                              accepted.data_ptr(), tokens.data_ptr(), workspace.data_ptr(),
-                              workspace.numel() * workspace.element_size(),
+                              accepted.data_ptr(), tokens.data_ptr(), _addr(workspace),
+                              0 if workspace is None else workspace.numel() * workspace.element_size(),
                               _stream_handle(target_probs, stream)))
     return accepted, tokens
 
@@ -1102,24 +1120,25 @@ def md_qk_norm_rope(q, k_new, pos0, inv_freq, *, norm=True, q_weight=None, k_wei
         raise ValueError("page_table without a cache")
     if k_new.dtype != dt:
         raise ValueError("q and k_new must share a dtype")
-    _on_gpu(q, k_new=k_new, v_new=v_new, pos0=pos0, inv_freq=inv_freq, q_weight=q_weight,
-            k_weight=k_weight, q_out=q_out, k_out=k_out, lens_out=lens_out)
+    _same_gpu(q, k_new=k_new, v_new=v_new, pos0=pos0, inv_freq=inv_freq, q_weight=q_weight,
+              k_weight=k_weight, q_out=q_out, k_out=k_out, lens_out=lens_out)
     _ints("pos0", pos0, B)
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None and (w.dtype != dt or w.shape != (d,) or not w.is_contiguous()):
             raise ValueError(f"{name} must be contiguous [d] in q's dtype")
     if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq must be contiguous float32 [rot_dim / 2]")
-    if q_out is None:
-        q_out = torch.empty((B, n, Hq, d), dtype=dt, device=q.device)
-    if k_out is None and c is None:
-        k_out = torch.empty((B, n, Hkv, d), dtype=dt, device=q.device)
     for name, t, h in (("q_out", q_out, Hq), ("k_out", k_out, Hkv)):
         if t is not None and (t.shape != (B, n, h, d) or t.dtype != dt or not t.is_contiguous()):
             raise ValueError(f"{name} must be contiguous [B, n, heads, d] in q's dtype")
+    if q_out is None:
+        q_out = q.new_empty((B, n, Hq, d))
+    if k_out is None and c is None:
+        k_out = q.new_empty((B, n, Hkv, d))
     if lens_out is None:
         lens_out = pos0.new_empty((B,))
-    _ints("lens_out", lens_out, B)
+    else:
+        _ints("lens_out", lens_out, B)
     a = MdQkNormRopeArgs(B, n, Hq, Hkv, d, _dtype_code(q), int(bool(norm)), float(eps),
                          _addr(q_weight), _addr(k_weight), 2 * inv_freq.numel(), int(bool(interleaved)),
                          _addr(inv_freq), q.data_ptr(), k_new.data_ptr(), _addr(v_new), *qs, *ks, *vs,

@@ -165,7 +165,8 @@ int md_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dty
       md::misaligned(tokens, 4))
     return MD_ERR_INVALID_ARG;
   const md::SpecPlan pl = md::make_spec_plan(num_seqs, vocab, md::device_cu_count());
-  if (!workspace || workspace_bytes < pl.workspace_bytes || md::misaligned(workspace, 256))
+  if (pl.workspace_bytes && (!workspace || workspace_bytes < pl.workspace_bytes ||
+                             md::misaligned(workspace, 256)))
     return MD_ERR_WORKSPACE;
   md::SpecAcceptParams p{};
   p.p = target_probs;
@@ -175,9 +176,10 @@ int md_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dty
   p.B = num_seqs;
   p.n_draft = n_draft;
   p.vocab = vocab;
-  p.n_chunks = pl.n_chunks;
-  p.chunk_len = pl.chunk_len;
-  p.part_sum = static_cast<double*>(workspace);
+  p.n_segs = pl.n_segs;
+  p.seg_len = pl.seg_len;
+  p.wgs = pl.wgs;
+  p.seg_sum = static_cast<double*>(workspace);
   p.accepted = accepted;
   p.tokens = tokens;
   return md::status(

@@ -75,8 +75,9 @@ struct SpecAcceptParams {
   const void* q;              // [B, n_draft, vocab], or nullptr: drafts without probabilities
   const int32_t* draft;       // [B, n_draft]
   const float* u;             // [B, n_draft + 1]
-  int32_t B, n_draft, vocab, n_chunks, chunk_len;
-  double* part_sum;           // [B, n_chunks]
+  int32_t B, n_draft, vocab, n_segs, seg_len;
+  int32_t wgs;                // workgroups a sequence, or 0: one does all (spec_fused)
+  double* seg_sum;            // [B, n_segs] (wgs > 0)
   int32_t* accepted;
   int32_t* tokens;            // [B, n_draft + 1]
 };

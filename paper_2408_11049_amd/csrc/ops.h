@@ -40,11 +40,13 @@ Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode
 int validate_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
                       int window, Kv4Plan* plan);
 
+// Sampled acceptance: a row in segments, a wave each at a time.
+constexpr int kSpecMaxSegs = 1024;
 struct SpecPlan {
-  int32_t n_chunks = 0, chunk_len = 0;
+  int32_t n_segs = 0, seg_len = 0;
+  int32_t wgs = 0;                // workgroups of four waves a sequence; 0: one of sixteen does all
   size_t workspace_bytes = 0;
 };
-constexpr int kSpecMaxChunks = 64;
 int validate_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype);
 SpecPlan make_spec_plan(int32_t num_seqs, int32_t vocab, int num_cus);
 

@@ -133,20 +133,22 @@ int validate_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32
   if (num_seqs < 0 || n_draft < 0 || n_draft > 1023 || vocab < 1 || vocab > (1 << 30))
     return MD_ERR_INVALID_ARG;
   if (dtype != MD_F32 && dtype != MD_BF16) return MD_ERR_INVALID_ARG;
-  if (num_seqs > (1 << 25) - 1) return MD_ERR_UNSUPPORTED;  // num_seqs * kSpecMaxChunks workgroups
+  if (num_seqs > (1 << 25) - 1) return MD_ERR_UNSUPPORTED;
   return MD_OK;
 }
 
 SpecPlan make_spec_plan(int32_t num_seqs, int32_t vocab, int num_cus) {
   SpecPlan pl;
   const int64_t cus = num_cus > 0 ? num_cus : 256;
-  constexpr int64_t kMinChunk = 2048;
-  int64_t n = ceil_div(8 * cus, std::max(num_seqs, 1));
-  n = std::max<int64_t>(1, std::min({n, ceil_div(vocab, kMinChunk), int64_t{kSpecMaxChunks}}));
-  const int64_t len = ceil_div(ceil_div(vocab, n), 8) * 8;  // whole 16-byte vectors
-  pl.chunk_len = static_cast<int32_t>(len);
-  pl.n_chunks = static_cast<int32_t>(ceil_div(vocab, len));
-  pl.workspace_bytes = static_cast<size_t>(num_seqs) * pl.n_chunks * sizeof(double);
+  // Segments of 1024 tokens (four 16-byte loads a lane and row in fp32), more in long rows.
+  const int64_t len = std::max<int64_t>(1024, ceil_div(ceil_div(vocab, kSpecMaxSegs), 512) * 512);
+  pl.seg_len = static_cast<int32_t>(len);
+  pl.n_segs = static_cast<int32_t>(ceil_div(vocab, len));
+  const int64_t wgs = std::min(ceil_div(4 * cus, std::max(num_seqs, 1)), ceil_div(pl.n_segs, 4));
+  if (num_seqs > 0 && wgs > 1 && pl.n_segs > 32) {
+    pl.wgs = static_cast<int32_t>(wgs);
+    pl.workspace_bytes = static_cast<size_t>(num_seqs) * pl.n_segs * sizeof(double);
+  }
   return pl;
 }
 

@@ -1,13 +1,15 @@
 // spec.hip -- sampled acceptance: drafted tokens kept or refused by the target's
 // probabilities, and the token drawn after the kept ones.
 //
-//   spec_sum   one workgroup per (sequence, chunk of the vocabulary): finds the
-//              sequence's accepted count a (a comparison per draft) and sums r =
-//              max(p_a - q_a, 0) over its chunk;
-//   spec_pick  one workgroup per sequence: finds the chunk, the span of it and the
-//              token in which the running sum of r passes u * sum r.
+// The row is cut into segments, a wave each.  A wave finds the sequence's accepted count
+// a (a comparison per draft) and sums r = max(p_a - q_a, 0) over its segments; then one
+// wave finds the segment, the span of it and the token in which the running sum of r
+// passes u * sum r.
 //
-// Bound by HBM: the rows p_a and q_a are read once (spec_pick reads one chunk of
+//   spec_fused  one workgroup per sequence does both, the segment sums in LDS;
+//   spec_sum, spec_pick  the same in two launches, the segments over many workgroups.
+//
+// Bound by HBM: the rows p_a and q_a are read once (the search reads one segment of
 // them again, from the caches).  Sums are 64-bit: r is exact there, and a sum's
 // error, some 1e-15 of it, is far below the share of a token that 32-bit sums of
 // 10^5 terms would misplace.  Every sum has a fixed order.
@@ -87,70 +89,21 @@ __device__ __forceinline__ double weight(const SpecAcceptParams& p, const Residu
   return w > 0.0 ? w : 0.0;
 }
 
-template <bool BF16, bool VEC>
-__global__ void __launch_bounds__(256) spec_sum_kernel(const SpecAcceptParams p) {
-  constexpr int N = Vec<BF16>::N, U = 4;
-  const int b = static_cast<int>(blockIdx.x) / p.n_chunks;
-  const int chunk = static_cast<int>(blockIdx.x) % p.n_chunks;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int a = accepted_count<BF16>(p, b, lane);
-  if (chunk == 0 && tid == 0) p.accepted[b] = a;
-  const Residual r = residual(p, b, a);
-  const int c0 = chunk * p.chunk_len, c1 = min(p.vocab, c0 + p.chunk_len);
+// The sum of r over one vector of each row (zeros for no draft row), tokens t ..
+template <bool BF16>
+__device__ __forceinline__ double vec_sum(const u32x4& x, const u32x4& y, int t, int one_at) {
+  constexpr int N = Vec<BF16>::N;
+  float fp[N], fq[N];
+  Vec<BF16>::get(x, fp);
+  Vec<BF16>::get(y, fq);
   double sum = 0.0;
-  if constexpr (VEC) {
-    constexpr int ES = BF16 ? 2 : 4;
-    const u32x4* pv = reinterpret_cast<const u32x4*>(static_cast<const char*>(p.p) + r.prow * ES);
-    const u32x4* qv =
-        reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (r.qrow < 0 ? 0 : r.qrow) * ES);
-    const int v0 = c0 / N, v1 = c1 / N;
-    for (int v = v0 + tid; v < v1; v += 256 * U) {
-      u32x4 x[U], y[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int vv = v + u * 256 < v1 ? v + u * 256 : v0;  // in bounds, not counted below
-        x[u] = pv[vv];
-        y[u] = r.qrow >= 0 ? qv[vv] : u32x4{0u, 0u, 0u, 0u};
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (v + u * 256 >= v1) continue;
-        float fp[N], fq[N];
-        Vec<BF16>::get(x[u], fp);
-        Vec<BF16>::get(y[u], fq);
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          double w = static_cast<double>(fp[j]) - static_cast<double>(fq[j]);
-          if ((v + u * 256) * N + j == r.one_at) w -= 1.0;
-          sum += w > 0.0 ? w : 0.0;
-        }
-      }
-    }
-  } else {
-    for (int t = c0 + tid; t < c1; t += 256) sum += weight<BF16>(p, r, t);
+  for (int j = 0; j < N; ++j) {
+    double w = static_cast<double>(fp[j]) - static_cast<double>(fq[j]);
+    if (t + j == one_at) w -= 1.0;
+    sum += w > 0.0 ? w : 0.0;
   }
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  __shared__ double s[4];
-  if (lane == 0) s[tid >> 6] = sum;
-  __syncthreads();
-  if (tid == 0)
-    p.part_sum[static_cast<int64_t>(b) * p.n_chunks + chunk] = (s[0] + s[1]) + (s[2] + s[3]);
-}
-
-// Inclusive sum over the workgroup's threads in thread order; `total` its last.
-__device__ __forceinline__ double block_scan(double x, double* s, double& total) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) s[tid >> 6] = x;
-  __syncthreads();
-  double base = 0.0;
-  for (int w = 0; w < (tid >> 6); ++w) base += s[w];
-  total = ((s[0] + s[1]) + s[2]) + s[3];
-  return base + x;
+  return sum;
 }
 
 // The sum of r over tokens [t0, t1), in order.
@@ -160,20 +113,13 @@ __device__ __forceinline__ double span_sum(const SpecAcceptParams& p, const Resi
   double sum = 0.0;
   if constexpr (VEC) {  // t0 and t1 are multiples of the vector's width
     constexpr int N = Vec<BF16>::N, ES = BF16 ? 2 : 4;
+#pragma unroll 4
     for (int t = t0; t < t1; t += N) {
       const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.p) + (r.prow + t) * ES);
       u32x4 y = {0u, 0u, 0u, 0u};
       if (r.qrow >= 0)
         y = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (r.qrow + t) * ES);
-      float fp[N], fq[N];
-      Vec<BF16>::get(x, fp);
-      Vec<BF16>::get(y, fq);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        double w = static_cast<double>(fp[j]) - static_cast<double>(fq[j]);
-        if (t + j == r.one_at) w -= 1.0;
-        sum += w > 0.0 ? w : 0.0;
-      }
+      sum += vec_sum<BF16>(x, y, t, r.one_at);
     }
   } else {
     for (int t = t0; t < t1; ++t) sum += weight<BF16>(p, r, t);
@@ -181,103 +127,186 @@ __device__ __forceinline__ double span_sum(const SpecAcceptParams& p, const Resi
   return sum;
 }
 
+// The sum of r over segment `seg`, by one wave (every lane gets it).
 template <bool BF16, bool VEC>
-__global__ void __launch_bounds__(256) spec_pick_kernel(const SpecAcceptParams p) {
-  __shared__ double s[4];
-  __shared__ double span_before;
-  __shared__ int first_span, last_span;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
-  const int n = p.n_draft;
-  const int a = p.accepted[b];
-  Residual r = residual(p, b, a);
-  const double* part = p.part_sum + static_cast<int64_t>(b) * p.n_chunks;
-  const double u = p.u[static_cast<int64_t>(b) * (n + 1) + n];
-  double total = 0.0;
-  for (int k = 0; k < p.n_chunks; ++k) total += part[k];
-  int c0 = 0, c1 = p.vocab;
-  double before = 0.0, want = u * total;
+__device__ __forceinline__ double segment_sum(const SpecAcceptParams& p, const Residual& r, int seg,
+                                              int lane) {
+  const int t0 = seg * p.seg_len, t1 = min(p.vocab, t0 + p.seg_len);
+  double sum = 0.0;
+  if constexpr (VEC) {
+    constexpr int N = Vec<BF16>::N, ES = BF16 ? 2 : 4, U = 4;
+    const char* pp = static_cast<const char*>(p.p) + r.prow * ES;
+    const char* qp = static_cast<const char*>(p.q) + r.qrow * ES;
+    for (int t = t0 + lane * N; t < t1; t += 64 * N * U) {
+      u32x4 x[U], y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = t + u * 64 * N < t1 ? t + u * 64 * N : t;  // in bounds, not counted below
+        x[u] = *reinterpret_cast<const u32x4*>(pp + static_cast<int64_t>(at) * ES);
+        y[u] = u32x4{0u, 0u, 0u, 0u};
+        if (r.qrow >= 0)
+          y[u] = *reinterpret_cast<const u32x4*>(qp + static_cast<int64_t>(at) * ES);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (t + u * 64 * N < t1) sum += vec_sum<BF16>(x[u], y[u], t + u * 64 * N, r.one_at);
+    }
+  } else {
+#pragma unroll 4
+    for (int t = t0 + lane; t < t1; t += 64) sum += weight<BF16>(p, r, t);
+  }
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  return sum;
+}
+
+__device__ __forceinline__ double wave_scan(double x, int lane) {  // inclusive
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+// Where a running sum that starts at `before` passes `want`: the first lane, in order, whose
+// own weight w > 0 brings it past, else the last lane with any weight (-1: none has).
+// before becomes the sum ahead of that lane; `all`: only a lane that passes counts.
+__device__ __forceinline__ int find_lane(double w, double want, bool all, int lane, double& before,
+                                         double& total) {
+  const double incl = before + wave_scan(w, lane);
+  const unsigned long long some = __ballot(w > 0.0), pass = __ballot(w > 0.0 && incl > want);
+  total = __shfl(incl, 63);
+  if (!pass && (all || !some)) return -1;
+  const int at = pass ? __ffsll(static_cast<long long>(pass)) - 1
+                      : 63 - __clzll(static_cast<long long>(some));
+  before = __shfl(incl - w, at);
+  return at;
+}
+
+// The drawn token, by one wave; sums: the segments' (LDS or global).
+template <bool BF16, bool VEC>
+__device__ int draw_token(const SpecAcceptParams& p, int b, Residual r, const double* sums, int lane) {
+  const double u = p.u[static_cast<int64_t>(b) * (p.n_draft + 1) + p.n_draft];
+  // A lane takes `per` consecutive segments.
+  const int per = (p.n_segs + 63) / 64;
+  const int s0 = min(p.n_segs, lane * per), s1 = min(p.n_segs, s0 + per);
+  double mine = 0.0;
+  for (int k = s0; k < s1; ++k) mine += sums[k];
+  double total = __shfl(wave_scan(mine, lane), 63);
+  int c0 = 0, c1 = p.vocab;  // the tokens in which it is
+  double before = 0.0, want = u * total, end;
   if (total > 0.0) {
-    // The chunk in which the sum passes; the last one with any weight if none.
-    int at = -1;
-    double run = 0.0;
-    for (int k = 0; k < p.n_chunks; ++k) {
-      const double w = part[k];
+    const int at = find_lane(mine, want, false, lane, before, end);
+    int seg = -1, last = 0;
+    double run = before;
+    for (int k = min(p.n_segs, at * per); k < min(p.n_segs, (at + 1) * per); ++k) {
+      const double w = sums[k];
       if (w > 0.0) {
-        at = k;
+        last = k;
         before = run;
-        if (run + w > want) break;
+        if (run + w > want) {
+          seg = k;
+          break;
+        }
       }
       run += w;
     }
-    c0 = at * p.chunk_len;
-    c1 = min(p.vocab, c0 + p.chunk_len);
+    if (seg < 0) seg = last;
+    c0 = seg * p.seg_len;
+    c1 = min(p.vocab, c0 + p.seg_len);
   } else {  // nothing of p_a is above q_a: the target's own row, whole
     r.qrow = -1;
     r.one_at = -1;
   }
-  if (tid == 0) {
-    first_span = 256;
-    last_span = 0;
-  }
-  // The span of the chunk (consecutive tokens of one thread) in which it passes.
-  const int span = ((c1 - c0 + 255) / 256 + 7) / 8 * 8;
-  const int t0 = min(c1, c0 + tid * span), t1 = min(c1, t0 + span);
+  // The span of them, consecutive tokens of a lane.
+  const int span = ((c1 - c0 + 63) / 64 + 7) / 8 * 8;
+  const int t0 = min(c1, c0 + lane * span), t1 = min(c1, t0 + span);
   const double w = span_sum<BF16, VEC>(p, r, t0, t1);
-  double sum;
-  const double run = before + block_scan(w, s, sum);
-  if (!(total > 0.0)) want = u * sum;
-  if (w > 0.0) {
-    if (run > want) atomicMin(&first_span, tid);
-    atomicMax(&last_span, tid);
-  }
-  __syncthreads();
-  const int at = first_span < 256 ? first_span : last_span;
-  if (tid == at) span_before = run - w;
-  __syncthreads();
-  if (tid >= 64) return;
-  // Its token, 64 at a time.
-  const int s0 = min(c1, c0 + at * span), s1 = min(c1, s0 + span);
-  double acc = span_before;
-  int tok = -1, last = 0;
-  for (int t = s0; t < s1 && tok < 0; t += 64) {
-    const double wt = t + lane < s1 ? weight<BF16>(p, r, t + lane) : 0.0;
-    double x = wt;
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(x, o);
-      if (lane >= o) x += y;
-    }
-    const unsigned long long pass = __ballot(wt > 0.0 && acc + x > want);
+  if (!(total > 0.0)) want = u * __shfl(wave_scan(w, lane), 63);
+  const int at = find_lane(w, want, false, lane, before, end);
+  if (at < 0) return 0;  // p_a is all 0
+  // The token, 64 at a time.
+  const int e0 = c0 + at * span, e1 = min(c1, e0 + span);
+  int tok = 0;
+  for (int t = e0; t < e1; t += 64) {
+    const double wt = t + lane < e1 ? weight<BF16>(p, r, t + lane) : 0.0;
     const unsigned long long some = __ballot(wt > 0.0);
-    if (pass) tok = t + __ffsll(static_cast<long long>(pass)) - 1;
-    if (some) last = t + 63 - __clzll(static_cast<long long>(some));
-    acc += __shfl(x, 63);
+    if (some) tok = t + 63 - __clzll(static_cast<long long>(some));
+    const int found = find_lane(wt, want, true, lane, before, end);
+    if (found >= 0) return t + found;
+    before = end;
   }
-  if (tok < 0) tok = last;
-  for (int i = tid; i <= n; i += 64)
+  return tok;
+}
+
+__device__ __forceinline__ void store_tokens(const SpecAcceptParams& p, int b, int a, int tok, int lane) {
+  const int n = p.n_draft;
+  for (int i = lane; i <= n; i += 64)
     p.tokens[static_cast<int64_t>(b) * (n + 1) + i] =
         i < a ? p.draft[static_cast<int64_t>(b) * n + i] : (i == a ? tok : -1);
 }
 
-template <bool BF16>
-static void launch_spec(const SpecAcceptParams& p, hipStream_t s) {
-  const dim3 g(static_cast<uint32_t>(p.B) * static_cast<uint32_t>(p.n_chunks)), blk(256);
-  // Whole 16-byte vectors where every row starts on one.
-  const bool vec = p.vocab % Vec<BF16>::N == 0 && (reinterpret_cast<uintptr_t>(p.p) & 15u) == 0 &&
-                   (reinterpret_cast<uintptr_t>(p.q) & 15u) == 0;
-  if (vec) {
-    hipLaunchKernelGGL((spec_sum_kernel<BF16, true>), g, blk, 0, s, p);
-    hipLaunchKernelGGL((spec_pick_kernel<BF16, true>), dim3(p.B), blk, 0, s, p);
-  } else {
-    hipLaunchKernelGGL((spec_sum_kernel<BF16, false>), g, blk, 0, s, p);
-    hipLaunchKernelGGL((spec_pick_kernel<BF16, false>), dim3(p.B), blk, 0, s, p);
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(256) spec_sum_kernel(const SpecAcceptParams p) {
+  const int b = static_cast<int>(blockIdx.x) / p.wgs;
+  const int lane = threadIdx.x & 63;
+  const int first = static_cast<int>(blockIdx.x) % p.wgs * 4 + (static_cast<int>(threadIdx.x) >> 6);
+  const int a = accepted_count<BF16>(p, b, lane);
+  if (first == 0 && lane == 0) p.accepted[b] = a;
+  const Residual r = residual(p, b, a);
+  for (int seg = first; seg < p.n_segs; seg += 4 * p.wgs) {
+    const double sum = segment_sum<BF16, VEC>(p, r, seg, lane);
+    if (lane == 0) p.seg_sum[static_cast<int64_t>(b) * p.n_segs + seg] = sum;
   }
 }
 
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(64) spec_pick_kernel(const SpecAcceptParams p) {
+  const int b = blockIdx.x, lane = threadIdx.x;
+  const int a = p.accepted[b];
+  const int tok = draw_token<BF16, VEC>(p, b, residual(p, b, a),
+                                        p.seg_sum + static_cast<int64_t>(b) * p.n_segs, lane);
+  store_tokens(p, b, a, tok, lane);
+}
+
+template <bool BF16, bool VEC>
+__global__ void __launch_bounds__(1024) spec_fused_kernel(const SpecAcceptParams p) {
+  __shared__ double sums[kSpecMaxSegs];
+  const int b = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = static_cast<int>(threadIdx.x) >> 6;
+  const int a = accepted_count<BF16>(p, b, lane);
+  const Residual r = residual(p, b, a);
+  for (int seg = wave; seg < p.n_segs; seg += 16) {
+    const double sum = segment_sum<BF16, VEC>(p, r, seg, lane);
+    if (lane == 0) sums[seg] = sum;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  if (lane == 0) p.accepted[b] = a;
+  store_tokens(p, b, a, draw_token<BF16, VEC>(p, b, r, sums, lane), lane);
+}
+
+template <bool BF16, bool VEC>
+static void launch_spec(const SpecAcceptParams& p, hipStream_t s) {
+  if (p.wgs == 0) {
+    hipLaunchKernelGGL((spec_fused_kernel<BF16, VEC>), dim3(p.B), dim3(1024), 0, s, p);
+    return;
+  }
+  const dim3 g(static_cast<uint32_t>(p.B) * static_cast<uint32_t>(p.wgs));
+  hipLaunchKernelGGL((spec_sum_kernel<BF16, VEC>), g, dim3(256), 0, s, p);
+  hipLaunchKernelGGL((spec_pick_kernel<BF16, VEC>), dim3(p.B), dim3(64), 0, s, p);
+}
+
 hipError_t launch_spec_accept(const SpecAcceptParams& p, bool bf16, hipStream_t s) {
-  if (bf16)
-    launch_spec<true>(p, s);
-  else
-    launch_spec<false>(p, s);
+  // Whole 16-byte vectors where every row starts on one.
+  const bool vec = p.vocab % (bf16 ? 8 : 4) == 0 && (reinterpret_cast<uintptr_t>(p.p) & 15u) == 0 &&
+                   (reinterpret_cast<uintptr_t>(p.q) & 15u) == 0;
+  if (bf16) {
+    if (vec) launch_spec<true, true>(p, s);
+    else launch_spec<true, false>(p, s);
+  } else {
+    if (vec) launch_spec<false, true>(p, s);
+    else launch_spec<false, false>(p, s);
+  }
   return hipGetLastError();
 }
 

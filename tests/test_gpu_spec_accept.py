@@ -170,7 +170,9 @@ def test_binding_refusals():
             lambda: f(p.transpose(0, 1), q, draft, u),
             lambda: f(p, q, draft, u, accepted=torch.empty(1, dtype=torch.int32, device=DEV)),
             lambda: f(p, q, draft, u, tokens=torch.empty(5, dtype=torch.int32, device=DEV)),
-            lambda: f(p, q, draft, u, workspace=torch.empty(1, dtype=torch.uint8, device=DEV))]):
+            lambda: f(p, q, draft, u, workspace=torch.empty(1 << 20, dtype=torch.uint8)),
+            lambda: f(torch.ones((1, 1, 100000), device=DEV), None, draft[:1, :0], u[:1, :1],
+                      workspace=torch.empty(64, dtype=torch.uint8, device=DEV))]):
         with pytest.raises(ValueError):
             bad()
             pytest.fail(f"case {i} was accepted")
