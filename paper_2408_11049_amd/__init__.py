@@ -310,12 +310,26 @@ def _stream_handle(t, stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _raw_stream(dev, stream):
+    """_stream_handle as an integer, for a device index."""
+    if stream is not None:
+        return stream.cuda_stream
+    return _torch_module._C._cuda_getCurrentRawStream(dev)
+
+
+_codes = {}
+
+
+def _code(t):
+    """_dtype_code, looked up."""
+    code = _codes.get(t.dtype)
+    if code is None:
+        code = _codes[t.dtype] = _dtype_code(t)
+    return code
+
+
 def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
-
-
-def _addr(t):
-    return None if t is None else t.data_ptr()
 
 
 def _on_gpu(ref, **tensors):
@@ -327,14 +341,6 @@ def _on_gpu(ref, **tensors):
     for name, t in tensors.items():
         if t is not None and t.device != ref.device:
             raise ValueError(f"{name} is on {t.device}; the call runs on {ref.device}")
-
-
-def _same_gpu(ref, **tensors):
-    """_on_gpu, at the cost of a comparison for each tensor."""
-    gpu = ref.get_device()
-    for t in tensors.values():
-        if gpu < 0 or (t is not None and t.get_device() != gpu):
-            _on_gpu(ref, **tensors)
 
 
 def _ints(name, t, n):
@@ -917,24 +923,30 @@ def make_kv4_cache(cache, *, num_seqs=None, page_table=None) -> MdKv4Cache:
 def md_kv4_append(cache, k_new, v_new, pos0, *, page_table=None, lens_out=None, stream=None):
     """Round k_new/v_new [B, n_new, Hkv, d] into the 4-bit cache at positions pos0[b] + i
     (in place).  Returns lens_out [B] int32 = pos0 + n_new."""
-    lib = load_library()
-    B, n_new = k_new.shape[:2]
-    if k_new.shape != v_new.shape or not k_new.is_contiguous() or not v_new.is_contiguous():
+    shape = k_new.shape
+    if (len(shape) != 4 or v_new.shape != shape or not k_new.is_contiguous()
+            or not v_new.is_contiguous()):
         raise ValueError("k_new and v_new must be contiguous [B, n_new, Hkv, d] of equal shape")
+    B, n_new, heads, d = shape
     if k_new.dtype != v_new.dtype:
         raise ValueError("k_new and v_new must share a dtype")
     c = make_kv4_cache(cache, num_seqs=B, page_table=page_table)
-    if B and k_new.shape[2:] != (c.num_kv_heads, c.head_dim):
+    if heads != c.num_kv_heads or d != c.head_dim:
         raise ValueError("appended rows must have the cache's heads and head_dim")
-    _same_gpu(cache.k, k_new=k_new, v_new=v_new, pos0=pos0, lens_out=lens_out)
+    gpu = cache.k.get_device()
+    if k_new.get_device() != gpu or v_new.get_device() != gpu or pos0.get_device() != gpu or (
+            lens_out is not None and lens_out.get_device() != gpu):
+        _on_gpu(cache.k, k_new=k_new, v_new=v_new, pos0=pos0, lens_out=lens_out)
     _ints("pos0", pos0, B)
     if lens_out is None:
         lens_out = pos0.new_empty((B,))
     else:
         _ints("lens_out", lens_out, B)
-    _check(lib.md_kv4_append(ctypes.byref(c), n_new, _dtype_code(k_new), k_new.data_ptr(),
-                             v_new.data_ptr(), pos0.data_ptr(), lens_out.data_ptr(),
-                             _stream_handle(cache.k, stream)))
+    st = load_library().md_kv4_append(
+        ctypes.byref(c), n_new, _code(k_new), k_new.data_ptr(), v_new.data_ptr(), pos0.data_ptr(),
+        lens_out.data_ptr(), _raw_stream(gpu, stream))
+    if st:
+        _check(st)
     return lens_out
 
 
@@ -944,48 +956,55 @@ def md_kv4_read(cache, pos0, n, *, page_table=None, dtype=None, k_out=None, v_ou
     """The values of positions pos0[b] .. pos0[b] + n - 1 of the 4-bit cache: (k, v)
     [B, n, Hkv, d] in dtype (bfloat16 unless given; exact in float32 too), zeros
     outside the cache."""
-    torch = _torch()
-    lib = load_library()
     B = pos0.shape[0]
     c = make_kv4_cache(cache, num_seqs=B, page_table=page_table)
     shape = (B, n, c.num_kv_heads, c.head_dim)
-    _same_gpu(cache.k, pos0=pos0, k_out=k_out, v_out=v_out)
+    gpu = cache.k.get_device()
+    if pos0.get_device() != gpu or k_out is not None or v_out is not None:
+        _on_gpu(cache.k, pos0=pos0, k_out=k_out, v_out=v_out)
     _ints("pos0", pos0, B)
     if dtype is None:
-        dtype = torch.bfloat16 if k_out is None else k_out.dtype
+        dtype = _torch_module.bfloat16 if k_out is None else k_out.dtype
     for t in (k_out, v_out):
         if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
             raise ValueError("k_out and v_out must be contiguous [B, n, Hkv, d] of one dtype")
     if k_out is None:
         k_out = pos0.new_empty(shape, dtype=dtype)
     if v_out is None:
-        v_out = torch.empty_like(k_out)
-    _check(lib.md_kv4_read(ctypes.byref(c), n, _dtype_code(k_out), pos0.data_ptr(),
-                           k_out.data_ptr(), v_out.data_ptr(), _stream_handle(cache.k, stream)))
+        v_out = k_out.new_empty(shape)
+    st = load_library().md_kv4_read(
+        ctypes.byref(c), n, _code(k_out), pos0.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+        _raw_stream(gpu, stream))
+    if st:
+        _check(st)
     return k_out, v_out
 
 
 def _kv4_args(q, c, kv_lens, max_kv_len, sm_scale, out, lse, workspace):
-    B, L, Hq, d = q.shape
+    """md_kv4_attn_args of tensors on q's device.  out, lse and workspace are the caller's
+    or None; what is None is filled in by the caller of this."""
+    shape = q.shape
+    B, L, Hq, d = shape
     if d != c.head_dim:
         raise ValueError("q's head_dim must be the cache's")
-    if not q.is_contiguous() or (out is not None and not out.is_contiguous()):
-        raise ValueError("q and o must be contiguous [B, L, Hq, d]")
-    if out is not None and (out.shape != q.shape or out.dtype != q.dtype):
-        raise ValueError("o must have q's shape and dtype")
-    torch = _torch()
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
-                            or lse.numel() < B * L * Hq):
-        raise ValueError("lse must be contiguous float32 [B, L, Hq]")
     gpu = q.get_device()
-    for t in (kv_lens, out, lse, workspace):
-        if gpu < 0 or (t is not None and t.get_device() != gpu):
-            _on_gpu(q, kv_lens=kv_lens, out=out, lse=lse, workspace=workspace)
+    if gpu < 0 or kv_lens.get_device() != gpu:
+        _on_gpu(q, kv_lens=kv_lens)
+    if not q.is_contiguous():
+        raise ValueError("q must be contiguous [B, L, Hq, d]")
+    if out is not None or lse is not None or workspace is not None:
+        _on_gpu(q, out=out, lse=lse, workspace=workspace)
+        if out is not None and (out.shape != shape or out.dtype != q.dtype
+                                or not out.is_contiguous()):
+            raise ValueError("o must be contiguous, with q's shape and dtype")
+        if lse is not None and (lse.dtype != _torch_module.float32 or not lse.is_contiguous()
+                                or lse.numel() < B * L * Hq):
+            raise ValueError("lse must be contiguous float32 [B, L, Hq]")
     _ints("kv_lens", kv_lens, B)
     if max_kv_len is None:  # a bound that needs no device sync
         max_kv_len = c.max_pages_per_seq * c.page_size if c.page_size else c.capacity
-    return MdKv4AttnArgs(L, Hq, _dtype_code(q), float(sm_scale), q.data_ptr(), kv_lens.data_ptr(),
-                         int(max_kv_len), None if out is None else out.data_ptr(),
+    return MdKv4AttnArgs(L, Hq, _code(q), sm_scale, q.data_ptr(), kv_lens.data_ptr(), max_kv_len,
+                         None if out is None else out.data_ptr(),
                          None if lse is None else lse.data_ptr(),
                          None if workspace is None else workspace.data_ptr(),
                          0 if workspace is None else workspace.numel() * workspace.element_size())
@@ -1003,28 +1022,30 @@ def md_kv4_workspace_bytes(q, cache, kv_lens, *, mode=MD_MODE_VERIFY, n_sink=0, 
 @_device_scoped
 def _kv4_attention(q, cache, kv_lens, mode, n_sink, window, *, max_kv_len=None, page_table=None,
                    sm_scale=0.0, out=None, lse=None, return_lse=True, workspace=None, stream=None):
-    torch = _torch()
+    torch = _torch_module
     lib = load_library()
     c = make_kv4_cache(cache, num_seqs=q.shape[0], page_table=page_table)
-    if cache.k.get_device() != q.get_device():
+    gpu = q.get_device()
+    if cache.k.get_device() != gpu:
         _on_gpu(q, cache=cache.k)
+    a = _kv4_args(q, c, kv_lens, max_kv_len, sm_scale, out, lse, workspace)
     if out is None:
         out = torch.empty_like(q)
+        a.o = out.data_ptr()
     if lse is None and return_lse:
         lse = q.new_empty(q.shape[:3], dtype=torch.float32)
-    a = _kv4_args(q, c, kv_lens, max_kv_len, sm_scale, out, lse, workspace)
+        a.lse = lse.data_ptr()
     rc, ra = ctypes.byref(c), ctypes.byref(a)
     if workspace is None:
         need = lib.md_kv4_workspace_bytes(rc, ra, mode, n_sink, window)
         if need:
             workspace = q.new_empty((need,), dtype=torch.uint8)
             a.workspace, a.workspace_bytes = workspace.data_ptr(), need
-    s = _stream_handle(q, stream)
     if mode == MD_MODE_VERIFY:
-        st = lib.md_kv4_verify_attn(rc, ra, s)
+        st = lib.md_kv4_verify_attn(rc, ra, _raw_stream(gpu, stream))
     else:
-        st = lib.md_kv4_draft_attn(rc, ra, n_sink, window, s)
-    if st != MD_OK:
+        st = lib.md_kv4_draft_attn(rc, ra, n_sink, window, _raw_stream(gpu, stream))
+    if st:
         _check(st)
     return out, lse
 
@@ -1045,7 +1066,7 @@ def md_spec_accept(target_probs, draft_probs, draft, u, *, accepted=None, tokens
     """Sampled acceptance: target_probs [B, gamma + 1, vocab] and draft_probs [B, gamma,
     vocab] (or None: drafts chosen, not sampled), float32/bfloat16; draft [B, gamma]
     int32; u [B, gamma + 1] float32 in [0, 1) -> (accepted [B], tokens [B, gamma + 1]), int32."""
-    torch = _torch()
+    torch = _torch_module
     lib = load_library()
     B, L, vocab = target_probs.shape
     if not target_probs.is_contiguous():
@@ -1058,8 +1079,12 @@ def md_spec_accept(target_probs, draft_probs, draft, u, *, accepted=None, tokens
         raise ValueError("draft must be contiguous int32 [B, gamma]")
     if u.shape != (B, L) or u.dtype != torch.float32 or not u.is_contiguous():
         raise ValueError("u must be contiguous float32 [B, gamma + 1]")
-    _same_gpu(target_probs, draft_probs=draft_probs, draft=draft, u=u, accepted=accepted,
-              tokens=tokens, workspace=workspace)
+    gpu = target_probs.get_device()
+    if draft.get_device() != gpu or u.get_device() != gpu or (
+            draft_probs is not None and draft_probs.get_device() != gpu):
+        _on_gpu(target_probs, draft_probs=draft_probs, draft=draft, u=u)
+    if accepted is not None or tokens is not None or workspace is not None:
+        _on_gpu(target_probs, accepted=accepted, tokens=tokens, workspace=workspace)
     if accepted is None:
         accepted = draft.new_empty((B,))
     else:
@@ -1071,25 +1096,28 @@ def md_spec_accept(target_probs, draft_probs, draft, u, *, accepted=None, tokens
     if workspace is None:
         need = lib.md_spec_accept_workspace_bytes(B, L - 1, vocab)
         workspace = target_probs.new_empty((need,), dtype=torch.uint8) if need else None
-    _check(lib.md_spec_accept(B, L - 1, vocab, _dtype_code(target_probs), target_probs.data_ptr(),
-                              None if draft_probs is None or L == 1 else draft_probs.data_ptr(),
-                              draft.data_ptr() if L > 1 else None, u.data_ptr(),
-                              accepted.data_ptr(), tokens.data_ptr(), _addr(workspace),
-                              0 if workspace is None else workspace.numel() * workspace.element_size(),
-                              _stream_handle(target_probs, stream)))
+    st = lib.md_spec_accept(
+        B, L - 1, vocab, _code(target_probs), target_probs.data_ptr(),
+        None if draft_probs is None or L == 1 else draft_probs.data_ptr(),
+        draft.data_ptr() if L > 1 else None, u.data_ptr(), accepted.data_ptr(), tokens.data_ptr(),
+        None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _raw_stream(gpu, stream))
+    if st:
+        _check(st)
     return accepted, tokens
 
 
-def _token_rows(name, t, shape):
+def _token_rows(name, t, B, n, heads, d):
     """The (sequence, token) element strides of rows [B, n, heads, d] whose heads are dense."""
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
+    if t.shape != (B, n, heads, d):
+        raise ValueError(f"{name} must be {(B, n, heads, d)}, not {tuple(t.shape)}")
     sb, st, sh, sc = t.stride()
-    if (sc != 1 and shape[3] > 1) or (sh != shape[3] and shape[2] > 1):
+    if (sc != 1 and d > 1) or (sh != d and heads > 1):
         raise ValueError(f"the heads of a token of {name} must be contiguous")
-    if shape[1] == 1:  # a dimension of size one has no stride of its own
-        st = shape[2] * shape[3]
-    return (shape[1] * st if shape[0] == 1 else sb), st
+    if n == 1:  # a dimension of size one has no stride of its own
+        st = heads * d
+    return (n * st if B == 1 else sb), st
 
 
 @_device_scoped
@@ -1101,36 +1129,40 @@ def md_qk_norm_rope(q, k_new, pos0, inv_freq, *, norm=True, q_weight=None, k_wei
     With a cache k, v (contiguous, or paged with page_table) the K rows and v_new's
     rows are written into it.  q, k_new and v_new may be views of one projection.
     Returns (q_out, k_out, lens_out); k_out is None with a cache unless given."""
-    torch = _torch()
-    lib = load_library()
     B, n, Hq, d = q.shape
     Hkv = k_new.shape[2]
-    qs, ks = _token_rows("q", q, (B, n, Hq, d)), _token_rows("k_new", k_new, (B, n, Hkv, d))
-    vs = (0, 0)
-    c = None
-    dt = q.dtype
+    dt, gpu = q.dtype, q.get_device()
+    qs = _token_rows("q", q, B, n, Hq, d)
+    ks = _token_rows("k_new", k_new, B, n, Hkv, d)
     if (k is None) != (v is None) or (k is None) != (v_new is None):
         raise ValueError("a cache takes k, v and v_new together")
     if k is not None:
-        vs = _token_rows("v_new", v_new, (B, n, Hkv, d))
+        vs = _token_rows("v_new", v_new, B, n, Hkv, d)
         c = make_kv_cache(k, v, num_seqs=B, page_table=page_table)
-        if k.dtype != dt or v_new.dtype != dt or k.get_device() != q.get_device():
+        if k.dtype != dt or v_new.dtype != dt or k.get_device() != gpu or v_new.get_device() != gpu:
             raise ValueError("the cache and v_new must have q's dtype and device")
-    elif page_table is not None:
+        v_addr = v_new.data_ptr()
+    elif page_table is None:
+        vs, c, v_addr = (0, 0), None, None
+    else:
         raise ValueError("page_table without a cache")
     if k_new.dtype != dt:
         raise ValueError("q and k_new must share a dtype")
-    _same_gpu(q, k_new=k_new, v_new=v_new, pos0=pos0, inv_freq=inv_freq, q_weight=q_weight,
-              k_weight=k_weight, q_out=q_out, k_out=k_out, lens_out=lens_out)
+    if k_new.get_device() != gpu or pos0.get_device() != gpu or inv_freq.get_device() != gpu:
+        _on_gpu(q, k_new=k_new, pos0=pos0, inv_freq=inv_freq)
     _ints("pos0", pos0, B)
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None and (w.dtype != dt or w.shape != (d,) or not w.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous [d] in q's dtype")
-    if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+    qw = kw = None
+    if q_weight is not None:
+        qw = _row_weight("q_weight", q_weight, d, dt, gpu)
+    if k_weight is not None:
+        kw = _row_weight("k_weight", k_weight, d, dt, gpu)
+    if inv_freq.dtype != _torch_module.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq must be contiguous float32 [rot_dim / 2]")
-    for name, t, h in (("q_out", q_out, Hq), ("k_out", k_out, Hkv)):
-        if t is not None and (t.shape != (B, n, h, d) or t.dtype != dt or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous [B, n, heads, d] in q's dtype")
+    if q_out is not None or k_out is not None or lens_out is not None:
+        _on_gpu(q, q_out=q_out, k_out=k_out, lens_out=lens_out)
+        for name, t, h in (("q_out", q_out, Hq), ("k_out", k_out, Hkv)):
+            if t is not None and (t.shape != (B, n, h, d) or t.dtype != dt or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous [B, n, heads, d] in q's dtype")
     if q_out is None:
         q_out = q.new_empty((B, n, Hq, d))
     if k_out is None and c is None:
@@ -1139,13 +1171,22 @@ def md_qk_norm_rope(q, k_new, pos0, inv_freq, *, norm=True, q_weight=None, k_wei
         lens_out = pos0.new_empty((B,))
     else:
         _ints("lens_out", lens_out, B)
-    a = MdQkNormRopeArgs(B, n, Hq, Hkv, d, _dtype_code(q), int(bool(norm)), float(eps),
-                         _addr(q_weight), _addr(k_weight), 2 * inv_freq.numel(), int(bool(interleaved)),
-                         _addr(inv_freq), q.data_ptr(), k_new.data_ptr(), _addr(v_new), *qs, *ks, *vs,
-                         pos0.data_ptr(), q_out.data_ptr(), _addr(k_out), lens_out.data_ptr())
-    _check(lib.md_qk_norm_rope(ctypes.byref(a), None if c is None else ctypes.byref(c),
-                               _stream_handle(q, stream)))
+    a = MdQkNormRopeArgs(B, n, Hq, Hkv, d, _code(q), 1 if norm else 0, eps, qw, kw,
+                         2 * inv_freq.shape[0], 1 if interleaved else 0, inv_freq.data_ptr(),
+                         q.data_ptr(), k_new.data_ptr(), v_addr, *qs, *ks, *vs, pos0.data_ptr(),
+                         q_out.data_ptr(), None if k_out is None else k_out.data_ptr(),
+                         lens_out.data_ptr())
+    st = load_library().md_qk_norm_rope(ctypes.byref(a), None if c is None else ctypes.byref(c),
+                                        _raw_stream(gpu, stream))
+    if st:
+        _check(st)
     return q_out, k_out, lens_out
+
+
+def _row_weight(name, w, d, dtype, gpu):
+    if w.dtype != dtype or w.shape != (d,) or not w.is_contiguous() or w.get_device() != gpu:
+        raise ValueError(f"{name} must be contiguous [d] in q's dtype, on q's device")
+    return w.data_ptr()
 
 
 def md_sd_expected_tokens(gamma: int, alpha: float) -> float:

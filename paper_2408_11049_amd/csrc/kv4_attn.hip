@@ -93,9 +93,12 @@ struct Tiles {
   int n;      // tiles that hold a visible token
   int head, tail0;
 };
-__device__ __forceinline__ Tiles tiles_of(const Kv4AttnParams& p, int b) {
+__device__ __forceinline__ int length(const Kv4AttnParams& p, int b) {
+  return max(min(p.kv_lens[b], p.max_kv_len), 0);
+}
+__device__ __forceinline__ Tiles tiles_of(const Kv4AttnParams& p, int S) {
   Tiles t;
-  t.S = max(min(p.kv_lens[b], p.max_kv_len), 0);
+  t.S = S;
   const int end = (t.S + T - 1) / T;
   t.head = end;
   t.tail0 = end;
@@ -121,7 +124,8 @@ struct Cursor {
   int TT, NW;
 };
 
-// Inclusive tile counts of the sequences in sl[0..B); the total.  256 threads.
+// Inclusive tile counts of the sequences in sl[0..B), their lengths in sl[kKv4BalMaxSeqs ..);
+// the total.  256 threads.
 __device__ int scan_tiles(const Kv4AttnParams& p, int* sl) {
   constexpr int kPer = kKv4BalMaxSeqs / 256;
   __shared__ int wave_sum[W];
@@ -129,7 +133,12 @@ __device__ int scan_tiles(const Kv4AttnParams& p, int* sl) {
   int v[kPer], mine = 0;
   for (int e = 0; e < kPer; ++e) {
     const int b = tid * kPer + e;
-    v[e] = b < p.B ? max(tiles_of(p, b).n, 1) * p.units : 0;
+    v[e] = 0;
+    if (b < p.B) {
+      const int S = length(p, b);
+      sl[kKv4BalMaxSeqs + b] = S;
+      v[e] = max(tiles_of(p, S).n, 1) * p.units;
+    }
     mine += v[e];
   }
   int incl = mine;
@@ -215,13 +224,15 @@ kv4_attn_kernel(const Kv4AttnParams p) {
   constexpr int kMergeO = W * 16 * MROW * 4;
   constexpr int kMl = 2 * W * ROWS * 4;
   constexpr int kWork = kV > kMergeO ? kV : kMergeO;
-  constexpr int kLds = kQ + kMl + kWork > kKv4BalMaxSeqs * 4 ? kQ + kMl + kWork : kKv4BalMaxSeqs * 4;
+  constexpr int kScan = 2 * kKv4BalMaxSeqs * 4;
+  constexpr int kLds = kQ + kMl + kWork > kScan ? kQ + kMl + kWork : kScan;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kLds];
 
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
   const int wave = uniform(tid >> 6);
 
   Cursor c{};
+  int S_next;  // length of the next piece's sequence
   if (p.balanced) {
     int* sl = reinterpret_cast<int*>(lds);
     c.TT = scan_tiles(p, sl);
@@ -239,21 +250,19 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     }
     if (tid == 0) p.joins[w] = join;
     if (w >= c.NW) return;  // the whole workgroup
+    S_next = sl[kKv4BalMaxSeqs + c.b];
     __syncthreads();        // the LDS is reused
   } else {
     c.b = static_cast<int>(blockIdx.x) / p.units;
     c.j = static_cast<int>(blockIdx.x) % p.units;
+    S_next = length(p, c.b);
   }
 
   for (;;) {  // one pass a piece
     const int b = c.b, hk = c.j / p.passes;
     const int r0 = c.j % p.passes * ROWS;   // its rows of the head's R: r0 .. r0 + rows - 1
     const int rows = min(p.R - r0, ROWS);
-    Tiles u = tiles_of(p, b);
-    u.S = uniform(u.S);
-    u.n = uniform(u.n);
-    u.head = uniform(u.head);
-    u.tail0 = uniform(u.tail0);
+    const Tiles u = tiles_of(p, uniform(S_next));
     if (!p.balanced) c = Cursor{0, max(u.n, 1), b, c.j, 0, max(u.n, 1), max(u.n, 1), 1};
     const int S = u.S;
     const int lt0 = c.t - c.g0;
@@ -663,7 +672,8 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     if (++c.j == p.units) {
       c.j = 0;
       ++c.b;
-      c.gt = max(uniform(tiles_of(p, c.b).n), 1);
+      S_next = length(p, c.b);
+      c.gt = max(uniform(tiles_of(p, S_next).n), 1);
     }
     __syncthreads();  // the LDS is reused
   }

@@ -80,6 +80,27 @@ int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int m
   return MD_OK;
 }
 
+// Whether a workgroup for each unit is put at less than equal ranges of all units' tiles.
+// Ranges cost some 8 us more (the scan of the lengths, the pieces' partial results, the second
+// launch: 64 x 8 units of 1024 tokens 28.0 us against 19.9); whole units leave compute units
+// short of workgroups.  A compute unit with one of the three workgroups it can hold streams at
+// 0.62 of its rate, with two at 0.93: 32 x 8 units of 2048 tokens 26.5 us whole, 25.4 in
+// ranges; 64 x 8 of 2048 31.6 and 39.7, of 4096 56.9 and 61.0; 128 x 8 of 2048 62.7 and 66.1, of
+// 4096 114.6 and 108.1.  Lengths are not known here: from 4096 tokens on, unequal ones would
+// cost whole units more than that.
+static bool whole_units(int64_t tiles, int64_t units, int64_t cus, int64_t resident, int d) {
+  if (tiles <= 32) return true;
+  if (tiles > 128) return false;
+  const double round_us =  // of a workgroup in every place
+      static_cast<double>(cus * resident * tiles * kKv4Tile * (d + d / 16)) / 6.2e6;
+  const double share = static_cast<double>(units) / static_cast<double>(cus * resident);
+  const int64_t left = units % (cus * resident), per_cu = ceil_div(left, cus);
+  const double rate = per_cu >= resident ? 1.0 : (per_cu > 1 ? 0.93 : 0.62);
+  const double rounds = static_cast<double>(units / (cus * resident)) +
+                        static_cast<double>(per_cu) / static_cast<double>(resident) / rate;
+  return round_us * (rounds - share) < 8.0;
+}
+
 Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
                       int window, int num_cus) {
   Kv4Plan p;
@@ -96,9 +117,9 @@ Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode
     tiles = std::min(tiles, ceil_div(n_sink, kKv4Tile) +
                                 ceil_div(int64_t{window} + a->q_len - 1, kKv4Tile) + 1);
   const int64_t cus = num_cus > 0 ? num_cus : 256;
-  const int64_t slots = cus * kKv4Resident(a->dtype == MD_BF16, p.NT);
+  const int64_t resident = kKv4Resident(a->dtype == MD_BF16, p.NT), slots = cus * resident;
   p.n_blocks = static_cast<int32_t>(units);
-  if (tiles * kKv4Tile > kWholeTokens && c->num_seqs <= kKv4BalMaxSeqs &&
+  if (!whole_units(tiles, units, cus, resident, c->head_dim) && c->num_seqs <= kKv4BalMaxSeqs &&
       tiles * units < (int64_t{1} << 30)) {
     p.balanced = true;
     const size_t rows = 16 * static_cast<size_t>(p.NT);
