@@ -516,8 +516,8 @@ typedef struct {
  * are not written.
  * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers, bad sizes or strides,
  * a bad dtype, n_new < 0, lens_out overlapping pos0; MD_ERR_UNSUPPORTED for
- * head_dim not in {64,128}, a token stride over 2^25 bytes or B * n_new * Hkv >
- * 2^31 - 1; MD_ERR_HIP.
+ * head_dim not in {64,128}, a token stride over 2^25 bytes, B * Hkv > 2^30 - 1 or
+ * B * n_new * Hkv > 2^31 - 1; MD_ERR_HIP.
  */
 int md_kv4_append(const md_kv4_cache* c, int32_t n_new, int32_t dtype, const void* k_new,
                   const void* v_new, const int32_t* pos0, int32_t* lens_out, void* stream);

@@ -144,7 +144,7 @@ size_t md_kv4_workspace_bytes(const md_kv4_cache* c, const md_kv4_attn_args* a, 
                               int32_t n_sink, int32_t window) {
   if (!c || md::check_kv4_attn_sizes(c, a, mode, n_sink, window) != MD_OK || c->num_seqs == 0)
     return 0;
-  return md::make_kv4_plan(c, a, mode, n_sink, window, md::device_cu_count()).workspace_bytes;
+  return md::kv4_workspace_need(c, a, mode, n_sink, window, md::device_cu_count());
 }
 
 size_t md_spec_accept_workspace_bytes(int32_t num_seqs, int32_t n_draft, int32_t vocab) {

@@ -21,6 +21,8 @@ constexpr int kKv4MaxNT(bool bf16) { return bf16 ? 4 : 2; }
 constexpr int kKv4Resident(bool bf16, int NT) { return bf16 && NT <= 2 ? 3 : 2; }
 // The balanced plan ranks every sequence's tiles in each workgroup.
 constexpr int kKv4BalMaxSeqs = 1024;
+// A unit of at most so many tiles is never cut, one of more than the second always may be.
+constexpr int64_t kKv4WholeTiles = 32, kKv4RangeTiles = 128;
 
 int validate_kv4_cache(const md_kv4_cache* c);
 // The buffers of a call that touches the cache (B > 0).
@@ -37,6 +39,9 @@ int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int m
                          int window);
 Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
                       int window, int num_cus);
+// What md_kv4_workspace_bytes answers: enough for this max_kv_len and every smaller one.
+size_t kv4_workspace_need(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                          int window, int num_cus);
 int validate_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
                       int window, Kv4Plan* plan);
 

@@ -89,8 +89,8 @@ int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int m
 // 4096 114.6 and 108.1.  Lengths are not known here: from 4096 tokens on, unequal ones would
 // cost whole units more than that.
 static bool whole_units(int64_t tiles, int64_t units, int64_t cus, int64_t resident, int d) {
-  if (tiles <= 32) return true;
-  if (tiles > 128) return false;
+  if (tiles <= kKv4WholeTiles) return true;
+  if (tiles > kKv4RangeTiles) return false;
   const double round_us =  // of a workgroup in every place
       static_cast<double>(cus * resident * tiles * kKv4Tile * (d + d / 16)) / 6.2e6;
   const double share = static_cast<double>(units) / static_cast<double>(cus * resident);
@@ -101,36 +101,74 @@ static bool whole_units(int64_t tiles, int64_t units, int64_t cus, int64_t resid
   return round_us * (rounds - share) < 8.0;
 }
 
+namespace {
+
+// What the plans of all lengths share, and the most tiles any unit has: those of the whole
+// context, or of the sinks and of the union of the windows, each cut at tile boundaries.
+struct Kv4Sizes {
+  Kv4Plan p;
+  int64_t units, tiles, cus, resident;
+};
+
+Kv4Sizes kv4_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                   int window, int num_cus) {
+  Kv4Sizes s;
+  s.p.G = a->num_q_heads / c->num_kv_heads;
+  s.p.R = s.p.G * a->q_len;
+  const int max_rows = 16 * kKv4MaxNT(a->dtype == MD_BF16);
+  s.p.passes = (s.p.R + max_rows - 1) / max_rows;
+  s.p.NT = (std::min(s.p.R, max_rows) + 15) / 16;
+  s.units = static_cast<int64_t>(c->num_seqs) * c->num_kv_heads * s.p.passes;
+  s.tiles = ceil_div(a->max_kv_len, kKv4Tile);
+  if (mode == MD_MODE_DRAFT)
+    s.tiles = std::min(s.tiles, ceil_div(n_sink, kKv4Tile) +
+                                    ceil_div(int64_t{window} + a->q_len - 1, kKv4Tile) + 1);
+  s.cus = num_cus > 0 ? num_cus : 256;
+  s.resident = kKv4Resident(a->dtype == MD_BF16, s.p.NT);
+  return s;
+}
+
+bool kv4_whole(const Kv4Sizes& s, int64_t tiles, const md_kv4_cache* c) {
+  return c->num_seqs > kKv4BalMaxSeqs || tiles * s.units >= (int64_t{1} << 30) ||
+         whole_units(tiles, s.units, s.cus, s.resident, c->head_dim);
+}
+
+void kv4_balance(const Kv4Sizes& s, int64_t tiles, int head_dim, Kv4Plan* p) {
+  const size_t rows = 16 * static_cast<size_t>(p->NT);
+  p->balanced = true;
+  p->n_blocks = static_cast<int32_t>(
+      std::min(s.cus * s.resident, ceil_div(tiles * s.units, kWaves)));
+  p->part_o_bytes =
+      align_up(static_cast<size_t>(2 * p->n_blocks) * rows * head_dim * sizeof(float), 256);
+  p->part_ml_bytes = align_up(static_cast<size_t>(2 * p->n_blocks) * rows * 2 * sizeof(float), 256);
+  p->workspace_bytes =
+      p->part_o_bytes + p->part_ml_bytes + align_up(static_cast<size_t>(p->n_blocks) * 16, 256);
+}
+
+}  // namespace
+
 Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
                       int window, int num_cus) {
-  Kv4Plan p;
-  p.G = a->num_q_heads / c->num_kv_heads;
-  p.R = p.G * a->q_len;
-  const int max_rows = 16 * kKv4MaxNT(a->dtype == MD_BF16);
-  p.passes = (p.R + max_rows - 1) / max_rows;
-  p.NT = (std::min(p.R, max_rows) + 15) / 16;
-  const int64_t units = static_cast<int64_t>(c->num_seqs) * c->num_kv_heads * p.passes;
-  // Most tiles of any unit: the whole context, or sinks and the union of the windows,
-  // each cut at tile boundaries.
-  int64_t tiles = ceil_div(a->max_kv_len, kKv4Tile);
-  if (mode == MD_MODE_DRAFT)
-    tiles = std::min(tiles, ceil_div(n_sink, kKv4Tile) +
-                                ceil_div(int64_t{window} + a->q_len - 1, kKv4Tile) + 1);
-  const int64_t cus = num_cus > 0 ? num_cus : 256;
-  const int64_t resident = kKv4Resident(a->dtype == MD_BF16, p.NT), slots = cus * resident;
-  p.n_blocks = static_cast<int32_t>(units);
-  if (!whole_units(tiles, units, cus, resident, c->head_dim) && c->num_seqs <= kKv4BalMaxSeqs &&
-      tiles * units < (int64_t{1} << 30)) {
-    p.balanced = true;
-    const size_t rows = 16 * static_cast<size_t>(p.NT);
-    p.n_blocks = static_cast<int32_t>(std::min(slots, ceil_div(tiles * units, kWaves)));
-    p.part_o_bytes =
-        align_up(static_cast<size_t>(2 * p.n_blocks) * rows * c->head_dim * sizeof(float), 256);
-    p.part_ml_bytes = align_up(static_cast<size_t>(2 * p.n_blocks) * rows * 2 * sizeof(float), 256);
-    p.workspace_bytes =
-        p.part_o_bytes + p.part_ml_bytes + align_up(static_cast<size_t>(p.n_blocks) * 16, 256);
-  }
+  const Kv4Sizes s = kv4_sizes(c, a, mode, n_sink, window, num_cus);
+  Kv4Plan p = s.p;
+  if (kv4_whole(s, s.tiles, c))
+    p.n_blocks = static_cast<int32_t>(s.units);
+  else
+    kv4_balance(s, s.tiles, c->head_dim, &p);
   return p;
+}
+
+// A range's need grows with its length, but a longer one may run whole: the need is that of
+// the longest one that does not.
+size_t kv4_workspace_need(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
+                          int window, int num_cus) {
+  const Kv4Sizes s = kv4_sizes(c, a, mode, n_sink, window, num_cus);
+  if (c->num_seqs > kKv4BalMaxSeqs) return 0;
+  int64_t tiles = std::min(s.tiles, ((int64_t{1} << 30) - 1) / s.units);
+  while (tiles > kKv4WholeTiles && kv4_whole(s, tiles, c)) --tiles;
+  Kv4Plan p = s.p;
+  if (tiles > kKv4WholeTiles) kv4_balance(s, tiles, c->head_dim, &p);
+  return p.workspace_bytes;
 }
 
 int validate_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int n_sink,
