@@ -516,7 +516,7 @@ typedef struct {
  * are not written.
  * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers, bad sizes or strides,
  * a bad dtype, n_new < 0, lens_out overlapping pos0; MD_ERR_UNSUPPORTED for
- * head_dim not in {64,128}, a token stride over 2^25 bytes, B * Hkv > 2^30 - 1 or
+ * head_dim not in {64,128}, a token stride over 2^25 bytes, B * Hkv or
  * B * n_new * Hkv > 2^31 - 1; MD_ERR_HIP.
  */
 int md_kv4_append(const md_kv4_cache* c, int32_t n_new, int32_t dtype, const void* k_new,
@@ -554,12 +554,15 @@ typedef struct {
  * last `window` positions.  Scores are products with the cache's exact values;
  * softmax and sums are fp32, with fp32 queries throughout, with bf16 ones the
  * softmax weights are rounded to bf16 before they multiply V (lse is not).
- * A query that sees no key gets o = 0, lse = -inf.  A NaN or infinity in a row
- * of K or V reaches only the queries that see that row.  kv_lens[b] is clamped to
+ * A query that sees no key gets o = 0, lse = -inf.  A NaN in a row of K or V reaches
+ * only the queries that see that row; so does an infinite value of K, but one of V
+ * (under the scales 253 and 254, which md_kv4_append never writes) may make NaN of the
+ * others that see part of the same 32 tokens.  kv_lens[b] is clamped to
  * [0, max_kv_len]; tokens on pages outside [0, num_pages) are not dereferenced, and
  * the queries that see them get unspecified results.
  * Errors: MD_ERR_INVALID_ARG and MD_ERR_UNSUPPORTED as md_verify_attn,
- * md_draft_attn and md_kv4_append (a contiguous cache must hold max_kv_len tokens);
+ * md_draft_attn and md_kv4_append (a contiguous cache must hold max_kv_len tokens), also
+ * UNSUPPORTED for B * Hkv > 2^23 - 1;
  * MD_ERR_WORKSPACE; MD_ERR_HIP.
  */
 int md_kv4_verify_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, void* stream);
@@ -601,7 +604,7 @@ size_t md_kv4_workspace_bytes(const md_kv4_cache* c, const md_kv4_attn_args* a, 
  *                 contents
  * Only the rows p_a and q_a are read whole.  Errors: MD_ERR_INVALID_ARG for NULL or
  * misaligned pointers (probabilities: their element size), n_draft outside [0, 1023],
- * vocab outside [1, 2^30], a bad dtype; MD_ERR_UNSUPPORTED for num_seqs > 2^25 - 1;
+ * vocab outside [1, 2^30], a bad dtype; MD_ERR_UNSUPPORTED for num_seqs > 2^22 - 1;
  * MD_ERR_WORKSPACE; MD_ERR_HIP.
  */
 int md_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype,
@@ -655,7 +658,8 @@ typedef struct {
  * and 4 bytes), bad sizes or strides, neither cache nor k_out, a v_new without or a cache
  * without a v_new, a cache of other sizes, q_out or k_out that overlaps an input in any other way
  * than being q or k_new itself, lens_out overlapping pos0; MD_ERR_UNSUPPORTED
- * for head_dim not in {64,128} or B * n_new > 2^31 - 1; MD_ERR_HIP.
+ * for head_dim not in {64,128}, B * n_new > 2^31 - 1 or more than 65536 heads of a kind;
+ * MD_ERR_HIP.
  */
 int md_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* cache, void* stream);
 

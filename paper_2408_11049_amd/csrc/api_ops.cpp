@@ -76,7 +76,6 @@ int run_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int
   p.B = c->num_seqs;
   p.L = a->q_len;
   p.Hq = a->num_q_heads;
-  p.Hkv = c->num_kv_heads;
   p.G = pl.G;
   p.R = pl.R;
   p.passes = pl.passes;
@@ -110,13 +109,18 @@ int md_kv4_append(const md_kv4_cache* c, int32_t n_new, int32_t dtype, const voi
                   const void* v_new, const int32_t* pos0, int32_t* lens_out, void* stream) {
   md::Kv4RowsParams p{};
   const int st = md::kv4_rows(c, n_new, dtype, k_new, v_new, pos0, &p);
-  if (st != MD_OK || p.rows == 0) return st;
+  if (st != MD_OK || c->num_seqs == 0) return st;
   if (lens_out) {  // one thread writes lens_out[b] while others still read pos0[b]
+    if (!pos0 || md::misaligned(pos0, 4)) return MD_ERR_INVALID_ARG;
     const uintptr_t lo = reinterpret_cast<uintptr_t>(lens_out);
     const uintptr_t po = reinterpret_cast<uintptr_t>(pos0);
     const uintptr_t nb = static_cast<uintptr_t>(c->num_seqs) * 4;
     if (lo % 4 || (lo < po + nb && po < lo + nb)) return MD_ERR_INVALID_ARG;
   }
+  if (p.rows == 0)  // no token: the lengths alone
+    return lens_out ? md::status(md::launch_copy_lens(c->num_seqs, pos0, lens_out,
+                                                      static_cast<hipStream_t>(stream)))
+                    : MD_OK;
   p.lens_out = lens_out;
   return md::status(md::launch_kv4_append(p, c->head_dim, dtype == MD_BF16, c->page_size != 0,
                                           static_cast<hipStream_t>(stream)));
@@ -188,7 +192,11 @@ int md_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dty
 
 int md_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* c, void* stream) {
   const int st = md::validate_qk_norm_rope(a, c);
-  if (st != MD_OK || a->num_seqs == 0 || a->n_new == 0) return st;
+  if (st != MD_OK || a->num_seqs == 0) return st;
+  if (a->n_new == 0)  // no token: the lengths alone
+    return a->lens_out ? md::status(md::launch_copy_lens(a->num_seqs, a->pos0, a->lens_out,
+                                                         static_cast<hipStream_t>(stream)))
+                       : MD_OK;
   md::NormRopeParams p{};
   p.q = a->q;
   p.k = a->k_new;

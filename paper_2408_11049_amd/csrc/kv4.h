@@ -41,6 +41,8 @@ struct Kv4RowsParams {
 
 hipError_t launch_kv4_append(const Kv4RowsParams& p, int head_dim, bool bf16, bool paged,
                              hipStream_t s);
+// lens_out = pos0: a call with no new token.
+hipError_t launch_copy_lens(int B, const int32_t* pos0, int32_t* lens_out, hipStream_t s);
 hipError_t launch_kv4_read(const Kv4RowsParams& p, int head_dim, bool bf16, bool paged,
                            hipStream_t s);
 
@@ -55,7 +57,7 @@ struct Kv4AttnParams {
   const void* q;
   const int32_t* kv_lens;
   int32_t max_kv_len;
-  int32_t B, L, Hq, Hkv, G, R;
+  int32_t B, L, Hq, G, R;
   int32_t passes, units;      // passes over a head's K and V; units of a sequence: Hkv * passes
   float scale_log2;           // softmax scale * log2(e)
   int32_t mode, n_sink, window;

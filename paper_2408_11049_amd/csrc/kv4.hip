@@ -120,6 +120,19 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Kv4RowsParams p) 
   }
 }
 
+__global__ void __launch_bounds__(256) copy_lens_kernel(int B, const int32_t* pos0, int32_t* lens_out) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t b = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; b < B; b += step)
+    lens_out[b] = pos0[b];
+}
+
+hipError_t launch_copy_lens(int B, const int32_t* pos0, int32_t* lens_out, hipStream_t s) {
+  const int wgs = B / 256 + 1;
+  hipLaunchKernelGGL(copy_lens_kernel, dim3(wgs < 1024 ? wgs : 1024), dim3(256), 0, s, B, pos0,
+                     lens_out);
+  return hipGetLastError();
+}
+
 // 8 values of a row: codes * scale.  v_cvt_scalef32_pk_{bf16,f32}_fp4 multiply by
 // the scale's power of two (exactly, subnormals too) and give NaN for a NaN scale.
 template <bool BF16>

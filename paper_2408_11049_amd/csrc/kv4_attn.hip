@@ -212,7 +212,6 @@ kv4_attn_kernel(const Kv4AttnParams p) {
   constexpr int CB = D / 16;        // 16-channel blocks of O
   constexpr int PARTS = BF16 ? 1 : 3;
   constexpr int ROWS = NT * 16;
-  constexpr int DEPTH = 1;          // tiles in flight a wave
   constexpr int kAhead = 4;         // channel blocks of V read ahead of their use
   constexpr int VROW = D * 2 + 16;  // bytes of a staged V row
   constexpr int QROW = D * 2 + 16;  // bytes of a staged row of Q (of one part)
@@ -347,16 +346,11 @@ kv4_attn_kernel(const Kv4AttnParams p) {
 
     // The first tiles' loads, before anything waits.
     const int mine = n_tiles > wave ? (n_tiles - wave + W - 1) / W : 0;  // tiles of this wave
-    TileRegs ring[DEPTH];
+    TileRegs tile;
     if (mine > 0) {
       ids = load_ids(0);
       ids_next = load_ids(32);
-#pragma unroll
-      for (int s = 0; s < DEPTH; ++s) {
-        // In the order of the loop's refills: a wait for one tile leaves the later ones in flight.
-        __builtin_amdgcn_sched_barrier(0);
-        load_tile(ring[s], s);
-      }
+      load_tile(tile, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
 
@@ -574,33 +568,20 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     };
 
-    if (mine > 0) {
-      auto one = [&](TileRegs& r, int k, auto refill) {
-        const int t0 = real_tile(lt0 + wave + k * W) * T;
-        bool masked = t0 + T - 1 > S - p.L;
-        if (p.mode == MD_MODE_DRAFT)
-          masked = masked || !(t0 + T <= p.n_sink || t0 > S - 1 - p.window);
-        process(masked, r, t0, refill);
-      };
-      // No slot of the ring is skipped inside the loop: one that was filled on some paths only
-      // would be copied at the loop's end, and the copy would wait for its loads.
-      int k0 = 0;
-      for (; k0 + DEPTH <= mine; k0 += DEPTH) {
-#pragma unroll
-        for (int s = 0; s < DEPTH; ++s) {
-          const int k = k0 + s;
-          one(ring[s], k, [&]() {
-            if (PG == 1 && ((k + DEPTH) & 31) == 0) {
-              ids = ids_next;
-              ids_next = load_ids(k + DEPTH + 32);
-            }
-            load_tile(ring[s], k + DEPTH);
-          });
+    for (int k = 0; k < mine; ++k) {
+      const int t0 = real_tile(lt0 + wave + k * W) * T;
+      bool masked = t0 + T - 1 > S - p.L;
+      if (p.mode == MD_MODE_DRAFT)
+        masked = masked || !(t0 + T <= p.n_sink || t0 > S - 1 - p.window);
+      // The next tile is loaded in any case (behind the last: the last again).  Registers filled
+      // on some paths only would be copied at the loop's end, and the copy would wait for them.
+      process(masked, tile, t0, [&]() {
+        if (PG == 1 && ((k + 1) & 31) == 0) {
+          ids = ids_next;
+          ids_next = load_ids(k + 33);
         }
-      }
-#pragma unroll
-      for (int s = 0; s + 1 < DEPTH; ++s)
-        if (k0 + s < mine) one(ring[s], k0 + s, []() {});
+        load_tile(tile, k + 1);
+      });
     }
 #pragma unroll
     for (int rt = 0; rt < NT; ++rt)

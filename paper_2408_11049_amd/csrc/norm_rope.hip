@@ -72,6 +72,8 @@ __device__ __forceinline__ Raw<BF16> narrow(const float (&x)[8]) {
   return r;
 }
 
+constexpr int64_t kTokensX = kMaxWgs256 / 2;
+
 // Row `row` of a token: Hq query heads, Hkv key heads, then (with a cache) Hkv value heads.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeParams p) {
@@ -81,13 +83,22 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeParams 
   __shared__ float cs[D / 2], sn[D / 2];
   const int tid = threadIdx.x;
   const int c = tid % LPR, rr = tid / LPR;
-  const int token = blockIdx.x;
+  const uint32_t at_token = blockIdx.x + blockIdx.z * gridDim.x;
+  if (at_token >= static_cast<uint32_t>(p.B * p.n)) return;  // the whole workgroup
+  const int token = static_cast<int>(at_token);
   const int b = token / p.n, i = token - b * p.n;
   const int rows = p.Hq + p.Hkv * (p.has_cache ? 2 : 1);
   const int32_t base = p.pos0[b];
   const int64_t pos = static_cast<int64_t>(base) + i;
   const int64_t qoff = b * p.q_seq + i * p.q_tok, koff = b * p.k_seq + i * p.k_tok,
                 voff = b * p.v_seq + i * p.v_tok;
+
+  // Whatever does not depend on another load comes first: the weights and the frequencies
+  // are not waited for one after the other.
+  Raw<BF16> wq, wk;
+  if (p.q_weight) wq = load_raw<BF16>(p.q_weight, c * 8);
+  if (p.k_weight) wk = load_raw<BF16>(p.k_weight, c * 8);
+  const float freq = tid < p.rot / 2 ? p.inv_freq[tid] : 0.f;  // rot / 2 <= 64 threads' angles
 
   const int first = static_cast<int>(blockIdx.y) * RPP;
   const int step = static_cast<int>(gridDim.y) * RPP;
@@ -105,13 +116,13 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeParams 
       raw[u] = load_raw<BF16>(src, at + c * 8);
     }
     if (!angles) {
-      for (int j = tid; j < p.rot / 2; j += 256) {
+      if (tid < p.rot / 2) {
         constexpr double kInv2Pi = 0.15915494309189533577;
         constexpr double k2PiHi = 6.283185307179586232, k2PiLo = 2.4492935982947064e-16;
-        const double t = static_cast<double>(pos) * static_cast<double>(p.inv_freq[j]);
+        const double t = static_cast<double>(pos) * static_cast<double>(freq);
         const double n = rint(t * kInv2Pi);
         const float f = static_cast<float>(fma(-n, k2PiLo, fma(-n, k2PiHi, t)));
-        sincosf(f, &sn[j], &cs[j]);
+        sincosf(f, &sn[tid], &cs[tid]);
       }
       __syncthreads();
       angles = true;
@@ -152,10 +163,9 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeParams 
         for (int j = 0; j < 8; ++j) ss += x[j] * x[j];
         for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o);
         const float rs = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
-        const void* w = is_q ? p.q_weight : p.k_weight;
         float wt[8];
-        if (w && live) {
-          widen<BF16>(load_raw<BF16>(w, c * 8), wt);
+        if (is_q ? p.q_weight != nullptr : p.k_weight != nullptr) {
+          widen<BF16>(is_q ? wq : wk, wt);
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) wt[j] = 1.f;
@@ -213,7 +223,10 @@ hipError_t launch_qk_norm_rope(const NormRopeParams& p, int head_dim, bool bf16,
   // Few tokens: a workgroup for each pass of a token's rows instead of one for all.
   const int64_t cus = device_cu_count();
   const int split = static_cast<int>(tokens * 2 <= cus ? passes : 1);
-  const dim3 g(static_cast<uint32_t>(tokens), static_cast<uint32_t>(split)), b(256);
+  // Tokens over x and, past the threads that one dimension counts, z.
+  const int64_t layers = (tokens + kTokensX - 1) / kTokensX;
+  const dim3 g(static_cast<uint32_t>((tokens + layers - 1) / layers),
+               static_cast<uint32_t>(split), static_cast<uint32_t>(layers)), b(256);
   if (head_dim == 128) {
     if (bf16) hipLaunchKernelGGL((qk_norm_rope_kernel<128, true>), g, b, 0, s, p);
     else hipLaunchKernelGGL((qk_norm_rope_kernel<128, false>), g, b, 0, s, p);

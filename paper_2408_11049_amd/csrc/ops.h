@@ -19,6 +19,8 @@ constexpr int64_t kKv4MaxTokStride = int64_t{1} << 25;
 constexpr int kKv4MaxNT(bool bf16) { return bf16 ? 4 : 2; }
 // Workgroups a compute unit holds, a wave per SIMD each (their instances' registers).
 constexpr int kKv4Resident(bool bf16, int NT) { return bf16 && NT <= 2 ? 3 : 2; }
+// Workgroups of 256 and of 1024 threads a launch may have: its threads are counted in 32 bits.
+constexpr int64_t kMaxWgs256 = (int64_t{1} << 24) - 1, kMaxWgs1024 = (int64_t{1} << 22) - 1;
 // The balanced plan ranks every sequence's tiles in each workgroup.
 constexpr int kKv4BalMaxSeqs = 1024;
 // A unit of at most so many tiles is never cut, one of more than the second always may be.

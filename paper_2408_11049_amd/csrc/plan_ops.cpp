@@ -43,8 +43,7 @@ int validate_kv4_cache(const md_kv4_cache* c) {
   if ((c->num_kv_heads > 1 && c->stride_head < row) || (toks > 1 && c->stride_tok < row))
     return MD_ERR_INVALID_ARG;
   if (c->stride_tok > kKv4MaxTokStride) return MD_ERR_UNSUPPORTED;
-  if (static_cast<int64_t>(c->num_seqs) * c->num_kv_heads > INT32_MAX / 2)
-    return MD_ERR_UNSUPPORTED;  // workgroups: up to two a (sequence, head)
+  if (static_cast<int64_t>(c->num_seqs) * c->num_kv_heads > INT32_MAX) return MD_ERR_UNSUPPORTED;
   return MD_OK;
 }
 
@@ -73,6 +72,9 @@ int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int m
     return MD_ERR_INVALID_ARG;
   if (st != MD_OK) return st;
   if (static_cast<int64_t>(a->num_q_heads / c->num_kv_heads) * a->q_len > kMaxRows)
+    return MD_ERR_UNSUPPORTED;
+  // Up to two passes, a workgroup each, a (sequence, head).
+  if (static_cast<int64_t>(c->num_seqs) * c->num_kv_heads > kMaxWgs256 / 2)
     return MD_ERR_UNSUPPORTED;
   if (a->max_kv_len > kMaxPosition) return MD_ERR_UNSUPPORTED;
   if (mode == MD_MODE_DRAFT && (window > kMaxPosition || n_sink > kMaxPosition))
@@ -192,7 +194,7 @@ int validate_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32
   if (num_seqs < 0 || n_draft < 0 || n_draft > 1023 || vocab < 1 || vocab > (1 << 30))
     return MD_ERR_INVALID_ARG;
   if (dtype != MD_F32 && dtype != MD_BF16) return MD_ERR_INVALID_ARG;
-  if (num_seqs > (1 << 25) - 1) return MD_ERR_UNSUPPORTED;
+  if (num_seqs > kMaxWgs1024) return MD_ERR_UNSUPPORTED;
   return MD_OK;
 }
 
@@ -233,8 +235,16 @@ int validate_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* c) {
   }
   if (a->head_dim != 64 && a->head_dim != 128) return MD_ERR_UNSUPPORTED;
   const int64_t tokens = static_cast<int64_t>(a->num_seqs) * a->n_new;
-  if (tokens > INT32_MAX) return MD_ERR_UNSUPPORTED;
-  if (tokens == 0) return MD_OK;
+  if (tokens > INT32_MAX || a->num_q_heads > 65536 || a->num_kv_heads > 65536)
+    return MD_ERR_UNSUPPORTED;
+  if (tokens == 0) {  // lens_out alone
+    const wide n4 = static_cast<wide>(a->num_seqs) * 4;
+    return a->num_seqs && a->lens_out &&
+                   (!a->pos0 || !aligned(a->pos0, 4) || !aligned(a->lens_out, 4) ||
+                    overlap(a->lens_out, n4, a->pos0, n4))
+               ? MD_ERR_INVALID_ARG
+               : MD_OK;
+  }
   if (!a->q || !a->k_new || !a->pos0 || !a->q_out || (!c && !a->k_out) || (c != nullptr) != (a->v_new != nullptr))
     return MD_ERR_INVALID_ARG;
   if (a->rot_dim && !a->inv_freq) return MD_ERR_INVALID_ARG;

@@ -172,6 +172,12 @@ def test_append_of_nothing_and_of_one():
     assert np.array_equal(host(k), plain.kv4_values(*plain.kv4_round(host(x))))
 
 
+def test_append_of_nothing_gives_the_lengths():
+    cache, _ = make_cache(3, 8, 1, 64)
+    none = randn((3, 0, 1, 64), "bf16", 0)
+    assert md.md_kv4_append(cache, none, none, ints([5, 0, 8])).tolist() == [5, 0, 8]
+
+
 # -------------------------------------------------------------- attention --
 
 def filled(B, cap, Hkv, d, page=0, layout="head", seed=0):
@@ -262,6 +268,21 @@ def test_attention_many_sequences(B):
     lens = rng.integers(0, 600, B).tolist()
     cache, pt = filled(B, 600, 1, 64, seed=B)
     check(randn((B, 1, 2, 64), "bf16", 10), cache, pt, lens, "bf16")
+
+
+def test_attention_of_millions_of_sequences():
+    """One token each: O is its value, exactly, and lse its score."""
+    B = 1 << 22
+    c = md.kv4_empty(B, 1, 1, 64, device=DEV)
+    c.k.fill_(0x22)
+    c.k_scale.fill_(127)
+    c.v.random_(0, 256)
+    c.v_scale.fill_(126)
+    q = torch.full((B, 1, 1, 64), 0.5, dtype=torch.bfloat16, device=DEV)
+    o, lse = md.md_kv4_verify_attn(q, c, torch.ones(B, dtype=torch.int32, device=DEV))
+    _, v = md.md_kv4_read(c, torch.zeros(B, dtype=torch.int32, device=DEV), 1)
+    assert torch.equal(o, v)
+    assert bool(((lse - 4.0).abs() <= 4 * 4 * 2.0 ** -22).all())  # 64 * 0.5 / 8
 
 
 def test_attention_lengths_past_the_bound_and_below_the_queries():

@@ -196,3 +196,22 @@ def test_binding_refusals():
         with pytest.raises(ValueError):
             bad()
             pytest.fail(f"case {i} was accepted")
+
+
+def test_no_new_token_still_gives_the_lengths():
+    q, k = randn((3, 0, 4, 64), "bf16", 0), randn((3, 0, 2, 64), "bf16", 1)
+    a, b, lens = md.md_qk_norm_rope(q, k, ints([4, 0, 9]), inv_freq(64))
+    assert a.shape == q.shape and b.shape == k.shape and lens.tolist() == [4, 0, 9]
+
+
+def test_more_tokens_than_one_grid_dimension_counts():
+    """Rows of the ends and of the middle against the same rows in a small call."""
+    n = (1 << 23) + 77
+    q = torch.randn((1, n, 1, 64), dtype=torch.bfloat16, device=DEV)
+    k = torch.randn((1, n, 1, 64), dtype=torch.bfloat16, device=DEV)
+    a, b, lens = md.md_qk_norm_rope(q, k, ints([3]), inv_freq(64))
+    assert lens.tolist() == [n + 3]
+    for at in (0, (1 << 22) - 40, (1 << 23) - 60, n - 70):
+        s = slice(at, at + 70)
+        ra, rb, _ = md.md_qk_norm_rope(q[:, s], k[:, s], ints([3 + at]), inv_freq(64))
+        assert torch.equal(a[:, s], ra) and torch.equal(b[:, s], rb)

@@ -112,6 +112,16 @@ def test_sums_of_many_small_terms():
     check(p, None, torch.empty((B, 0), dtype=torch.int32, device=DEV), u)
 
 
+def test_millions_of_sequences():
+    B = (1 << 22) - 1
+    p = torch.ones((B, 1, 2), device=DEV)
+    u = torch.zeros((B, 1), device=DEV)
+    u[1::2] = 0.75
+    acc, tok = md.md_spec_accept(p, None, torch.empty((B, 0), dtype=torch.int32, device=DEV), u)
+    assert int(acc.abs().sum()) == 0
+    assert torch.equal(tok[:, 0], (torch.arange(B, device=DEV) % 2).to(torch.int32))
+
+
 def test_unaligned_rows_and_given_buffers():
     p, q, draft, u = make(3, 2, 4096, "bf16", 9)
     flat = torch.empty(p.numel() + 1, dtype=p.dtype, device=DEV)

@@ -55,7 +55,7 @@ BAD_CACHE = [
     ("table misaligned", dict(PAGED, page_table=FAKE + 2), INV), ("no pages", dict(PAGED, num_pages=0), INV),
     ("page ids past int32", dict(PAGED, num_pages=1 << 31), INV),
     ("no table columns", dict(PAGED, max_pages_per_seq=0), INV),
-    ("units past 2^30", dict(num_seqs=1 << 30), UNS),
+    ("units past 2^31 - 1", dict(num_seqs=1 << 30), UNS),
 ]
 
 
@@ -86,6 +86,9 @@ def test_bad_rows(lib):  # noqa: F811
     assert r(c, 2, 1, FAKE, FAKE, FAKE + 4, None) == INV
     assert r(c, 2, 1, None, FAKE, FAKE, None) == INV
     assert f(c, 0, 1, None, None, None, None, None) == OK            # nothing to do
+    assert f(c, 0, 1, None, None, None, FAKE, None) == INV           # lengths alone, of what?
+    assert f(c, 0, 1, None, None, FAKE, FAKE + 4, None) == INV
+    assert f(ctypes.byref(cache(num_seqs=0)), 2, 1, None, None, None, FAKE, None) == OK
     assert r(ctypes.byref(cache(num_seqs=0, k=None)), 5, 1, None, None, None, None) == OK
 
 
@@ -128,6 +131,7 @@ def test_attention_windows_and_workspaces(lib):  # noqa: F811
     for ws, size in ((None, need[3]), (FAKE, need[3] - 1), (FAKE + 16, need[3])):
         big = attn(max_kv_len=1 << 20, workspace=ws, workspace_bytes=size)
         assert lib.md_kv4_verify_attn(ctypes.byref(cache(**long)), ctypes.byref(big), None) == WS
+    assert lib.md_kv4_verify_attn(ctypes.byref(cache(num_seqs=1 << 22)), a, None) == UNS
     assert lib.md_kv4_verify_attn(ctypes.byref(cache(num_seqs=0, k=None)), ctypes.byref(attn(q=None)),
                                   None) == OK
 
@@ -154,7 +158,7 @@ def test_bad_sampled_acceptance(lib):  # noqa: F811
                 dict(q=FAKE + 1, dt=1), dict(d=FAKE + 2), dict(u=FAKE + 2), dict(a=FAKE + 1),
                 dict(t=FAKE + 3)):
         assert f(**bad) == INV, bad
-    assert f(B=1 << 25) == UNS
+    assert f(B=1 << 22) == UNS
     assert f(B=0, p=None) == OK
     need = lib.md_spec_accept_workspace_bytes(2, 3, 128256)
     assert need > 0 and lib.md_spec_accept_workspace_bytes(2, 3, 1000) == 0
@@ -206,7 +210,11 @@ def test_bad_norm_caches_and_sizes(lib):  # noqa: F811
     assert f(None, None, None) == INV
     assert f(ctypes.byref(norm(head_dim=96, rot_dim=0)), None, None) == UNS
     assert f(ctypes.byref(norm(num_seqs=1 << 20, n_new=1 << 12)), None, None) == UNS
+    assert f(ctypes.byref(norm(num_q_heads=65537)), None, None) == UNS
     assert f(ctypes.byref(norm(n_new=0, q=None)), None, None) == OK
+    assert f(ctypes.byref(norm(n_new=0, lens_out=FAKE + 4)), None, None) == INV
+    assert f(ctypes.byref(norm(n_new=0, lens_out=FAKE, pos0=None)), None, None) == INV
+    assert f(ctypes.byref(norm(num_seqs=0, lens_out=FAKE, pos0=None)), None, None) == OK
     with_v = norm(v_new=FAKE + 0x40000, v_stride_tok=128, v_stride_seq=384)
     for over in (dict(num_seqs=3), dict(num_kv_heads=1), dict(head_dim=128), dict(dtype=0), dict(k=None),
                  dict(v=FAKE + 8), dict(capacity=0), dict(kv_stride_tok=4)):
