@@ -8,8 +8,13 @@
 // sum of squares is reduced over 8 or 16 neighbouring lanes and a pair's other half is
 // one lane exchange away.  A workgroup takes one token: the rot / 2 angles are turned
 // into cosines and sines once (64-bit product and reduction, so far positions keep
-// their fraction of a turn) and serve all the token's heads from LDS, while the
-// rows' loads are in flight.
+// their fraction of a turn) and serve all the token's heads from LDS.
+//
+// What keeps the memory busy is many small workgroups, each with two passes' rows loaded and
+// the next two under way: 4 x 4096 tokens of 32 + 8 heads of 128 in bf16 80 us, 5.0 TB/s read
+// and written (a large copy: 4.9).  Against that, on one card: one pass at a time 97 to 93, three
+// 98, four tokens a workgroup 104, no rows ahead 100.  A step of 64 x 5 tokens takes 6.1 us, of
+// which the bytes would need 1.6.
 #include "kv4.h"
 
 namespace md {
@@ -38,8 +43,8 @@ __device__ __forceinline__ Raw<BF16> load_raw(const void* base, int64_t e) {
 template <bool BF16>
 __device__ __forceinline__ void store_raw(void* base, int64_t e, const Raw<BF16>& r) {
   u32x4* p = reinterpret_cast<u32x4*>(static_cast<char*>(base) + e * (BF16 ? 2 : 4));
-  p[0] = r.w[0];
-  if constexpr (!BF16) p[1] = r.w[1];
+  __builtin_nontemporal_store(r.w[0], p);
+  if constexpr (!BF16) __builtin_nontemporal_store(r.w[1], p + 1);
 }
 
 template <bool BF16>
@@ -74,75 +79,86 @@ __device__ __forceinline__ Raw<BF16> narrow(const float (&x)[8]) {
 
 constexpr int64_t kTokensX = kMaxWgs256 / 2;
 
+// Where a token is: its sequence, its place in it, its position.
+struct At {
+  int token, b, i;
+  int64_t pos;
+};
+__device__ __forceinline__ At at_token(const NormRopeParams& p, int token) {
+  At t;
+  t.token = token;
+  t.b = token / p.n;
+  t.i = token - t.b * p.n;
+  t.pos = static_cast<int64_t>(p.pos0[t.b]) + t.i;
+  return t;
+}
+// Element offset of the token's rows in the cache, -1: not in it.
+__device__ __forceinline__ int64_t cache_offset(const NormRopeParams& p, const At& t) {
+  if (!p.has_cache || t.pos < 0) return -1;
+  if (!p.paged) return t.pos < p.c.capacity ? t.b * p.c.s_blk + t.pos * p.c.s_tok : -1;
+  const int64_t pg = t.pos >> p.c.page_shift;
+  if (pg >= p.c.max_pages) return -1;
+  const int64_t id = p.c.page_table[static_cast<int64_t>(t.b) * p.c.max_pages + pg];
+  if (id < 0 || id >= p.c.num_pages) return -1;
+  return id * p.c.s_blk + (t.pos & ((int64_t{1} << p.c.page_shift) - 1)) * p.c.s_tok;
+}
+
 // Row `row` of a token: Hq query heads, Hkv key heads, then (with a cache) Hkv value heads.
+// A workgroup takes one token (blockIdx.x, blockIdx.z) and its share of the passes over its rows.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeParams p) {
   constexpr int LPR = D / 8;       // threads a row
   constexpr int RPP = 256 / LPR;   // rows a pass
-  constexpr int U = 4;             // passes whose loads are in flight together
+  constexpr int U = 2;             // passes whose loads are in flight together
   __shared__ float cs[D / 2], sn[D / 2];
   const int tid = threadIdx.x;
   const int c = tid % LPR, rr = tid / LPR;
-  const uint32_t at_token = blockIdx.x + blockIdx.z * gridDim.x;
-  if (at_token >= static_cast<uint32_t>(p.B * p.n)) return;  // the whole workgroup
-  const int token = static_cast<int>(at_token);
-  const int b = token / p.n, i = token - b * p.n;
+  const uint32_t token = blockIdx.x + blockIdx.z * gridDim.x;
+  if (token >= static_cast<uint32_t>(p.B * p.n)) return;  // the whole workgroup
   const int rows = p.Hq + p.Hkv * (p.has_cache ? 2 : 1);
-  const int32_t base = p.pos0[b];
-  const int64_t pos = static_cast<int64_t>(base) + i;
-  const int64_t qoff = b * p.q_seq + i * p.q_tok, koff = b * p.k_seq + i * p.k_tok,
-                voff = b * p.v_seq + i * p.v_tok;
-
-  // Whatever does not depend on another load comes first: the weights and the frequencies
-  // are not waited for one after the other.
-  Raw<BF16> wq, wk;
-  if (p.q_weight) wq = load_raw<BF16>(p.q_weight, c * 8);
-  if (p.k_weight) wk = load_raw<BF16>(p.k_weight, c * 8);
-  const float freq = tid < p.rot / 2 ? p.inv_freq[tid] : 0.f;  // rot / 2 <= 64 threads' angles
-
+  const At here = at_token(p, static_cast<int>(token));
   const int first = static_cast<int>(blockIdx.y) * RPP;
   const int step = static_cast<int>(gridDim.y) * RPP;
-  bool angles = false;
-  for (int r0 = first; r0 < rows; r0 += U * step) {
-    Raw<BF16> raw[U];
+
+  // Whatever does not depend on another load comes first.
+  auto load = [&](Raw<BF16> (&raw)[U], int r0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int row = r0 + u * step + rr;
       if (row >= rows) continue;
-      const void* src = row < p.Hq ? p.q : (row < p.Hq + p.Hkv ? p.k : p.v);
-      const int64_t at = row < p.Hq ? qoff + static_cast<int64_t>(row) * D
-                         : row < p.Hq + p.Hkv ? koff + static_cast<int64_t>(row - p.Hq) * D
-                                              : voff + static_cast<int64_t>(row - p.Hq - p.Hkv) * D;
+      const int64_t b = here.b, i = here.i;
+      const bool is_q = row < p.Hq, is_k = !is_q && row < p.Hq + p.Hkv;
+      const void* src = is_q ? p.q : (is_k ? p.k : p.v);
+      const int64_t at = is_q ? b * p.q_seq + i * p.q_tok + static_cast<int64_t>(row) * D
+                         : is_k ? b * p.k_seq + i * p.k_tok + static_cast<int64_t>(row - p.Hq) * D
+                                : b * p.v_seq + i * p.v_tok +
+                                      static_cast<int64_t>(row - p.Hq - p.Hkv) * D;
       raw[u] = load_raw<BF16>(src, at + c * 8);
     }
-    if (!angles) {
-      if (tid < p.rot / 2) {
-        constexpr double kInv2Pi = 0.15915494309189533577;
-        constexpr double k2PiHi = 6.283185307179586232, k2PiLo = 2.4492935982947064e-16;
-        const double t = static_cast<double>(pos) * static_cast<double>(freq);
-        const double n = rint(t * kInv2Pi);
-        const float f = static_cast<float>(fma(-n, k2PiLo, fma(-n, k2PiHi, t)));
-        sincosf(f, &sn[tid], &cs[tid]);
-      }
-      __syncthreads();
-      angles = true;
-    }
-    // Where position pos lives in the cache (uniform over the workgroup).
-    bool in = p.has_cache && pos >= 0;
-    int64_t cache_at = 0;
-    if (in) {
-      int64_t blk = b, tok = pos;
-      if (p.paged) {
-        const int64_t pg = pos >> p.c.page_shift;
-        in = pg < p.c.max_pages;
-        blk = in ? p.c.page_table[static_cast<int64_t>(b) * p.c.max_pages + pg] : 0;
-        in = in && blk >= 0 && blk < p.c.num_pages;
-        tok = pos & ((int64_t{1} << p.c.page_shift) - 1);
-      } else {
-        in = pos < p.c.capacity;
-      }
-      cache_at = blk * p.c.s_blk + tok * p.c.s_tok;
-    }
+  };
+  Raw<BF16> raw[U];
+  load(raw, first);
+  Raw<BF16> wq, wk;
+  if (p.q_weight) wq = load_raw<BF16>(p.q_weight, c * 8);
+  if (p.k_weight) wk = load_raw<BF16>(p.k_weight, c * 8);
+  const float freq = tid < p.rot / 2 ? p.inv_freq[tid] : 0.f;
+  const int64_t cache_at = cache_offset(p, here);
+
+  if (tid < p.rot / 2) {  // an angle a thread
+    constexpr double kInv2Pi = 0.15915494309189533577;
+    constexpr double k2PiHi = 6.283185307179586232, k2PiLo = 2.4492935982947064e-16;
+    const double t = static_cast<double>(here.pos) * static_cast<double>(freq);
+    const double n = rint(t * kInv2Pi);
+    const float f = static_cast<float>(fma(-n, k2PiLo, fma(-n, k2PiHi, t)));
+    sincosf(f, &sn[tid], &cs[tid]);
+  }
+  if (here.i == 0 && tid == 0 && blockIdx.y == 0 && p.lens_out)
+    p.lens_out[here.b] = static_cast<int32_t>(here.pos + p.n);
+  __syncthreads();
+
+  for (int r0 = first; r0 < rows; r0 += U * step) {
+    Raw<BF16> raw_next[U];
+    load(raw_next, r0 + U * step);  // none behind the last row
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int row = r0 + u * step + rr;
@@ -200,39 +216,45 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeParams 
       }
       if (!live) continue;
       if (is_q) {
-        store_raw<BF16>(p.q_out, (static_cast<int64_t>(token) * p.Hq + head) * D + c * 8,
+        store_raw<BF16>(p.q_out, (static_cast<int64_t>(here.token) * p.Hq + head) * D + c * 8,
                         narrow<BF16>(x));
         continue;
       }
       // A value row moves as it is.
       const Raw<BF16> out = is_k ? narrow<BF16>(x) : raw[u];
       if (is_k && p.k_out)
-        store_raw<BF16>(p.k_out, (static_cast<int64_t>(token) * p.Hkv + head) * D + c * 8, out);
-      if (in) store_raw<BF16>(is_k ? p.c.k : p.c.v, cache_at + head * p.c.s_head + c * 8, out);
+        store_raw<BF16>(p.k_out, (static_cast<int64_t>(here.token) * p.Hkv + head) * D + c * 8, out);
+      if (cache_at >= 0)
+        store_raw<BF16>(is_k ? p.c.k : p.c.v, cache_at + head * p.c.s_head + c * 8, out);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = raw_next[u];
   }
-  if (blockIdx.y == 0 && i == 0 && tid == 0 && p.lens_out) p.lens_out[b] = base + p.n;
+}
+
+template <int D, bool BF16>
+void launch_norm(const NormRopeParams& p, hipStream_t s) {
+  const int64_t tokens = static_cast<int64_t>(p.B) * p.n;
+  const int rows = p.Hq + p.Hkv * (p.has_cache ? 2 : 1);
+  const int rpp = 256 / (D / 8), passes = (rows + rpp - 1) / rpp;
+  // Few tokens: a workgroup for each pass of a token's rows instead of one for all.
+  const int split = static_cast<int>(tokens <= 4 * device_cu_count() ? passes : 1);
+  // Tokens over x and, past the threads that one dimension counts, z.
+  const int64_t layers = (tokens + kTokensX - 1) / kTokensX;
+  const dim3 g(static_cast<uint32_t>((tokens + layers - 1) / layers),
+               static_cast<uint32_t>(split), static_cast<uint32_t>(layers));
+  hipLaunchKernelGGL((qk_norm_rope_kernel<D, BF16>), g, dim3(256), 0, s, p);
 }
 
 }  // namespace
 
 hipError_t launch_qk_norm_rope(const NormRopeParams& p, int head_dim, bool bf16, hipStream_t s) {
-  const int64_t tokens = static_cast<int64_t>(p.B) * p.n;
-  const int rows = p.Hq + p.Hkv * (p.has_cache ? 2 : 1);
-  const int passes = (rows + 256 / (head_dim / 8) - 1) / (256 / (head_dim / 8));
-  // Few tokens: a workgroup for each pass of a token's rows instead of one for all.
-  const int64_t cus = device_cu_count();
-  const int split = static_cast<int>(tokens * 2 <= cus ? passes : 1);
-  // Tokens over x and, past the threads that one dimension counts, z.
-  const int64_t layers = (tokens + kTokensX - 1) / kTokensX;
-  const dim3 g(static_cast<uint32_t>((tokens + layers - 1) / layers),
-               static_cast<uint32_t>(split), static_cast<uint32_t>(layers)), b(256);
   if (head_dim == 128) {
-    if (bf16) hipLaunchKernelGGL((qk_norm_rope_kernel<128, true>), g, b, 0, s, p);
-    else hipLaunchKernelGGL((qk_norm_rope_kernel<128, false>), g, b, 0, s, p);
+    if (bf16) launch_norm<128, true>(p, s);
+    else launch_norm<128, false>(p, s);
   } else {
-    if (bf16) hipLaunchKernelGGL((qk_norm_rope_kernel<64, true>), g, b, 0, s, p);
-    else hipLaunchKernelGGL((qk_norm_rope_kernel<64, false>), g, b, 0, s, p);
+    if (bf16) launch_norm<64, true>(p, s);
+    else launch_norm<64, false>(p, s);
   }
   return hipGetLastError();
 }
