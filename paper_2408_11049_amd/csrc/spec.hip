@@ -9,10 +9,15 @@
 //   spec_fused  one workgroup per sequence does both, the segment sums in LDS;
 //   spec_sum, spec_pick  the same in two launches, the segments over many workgroups.
 //
-// Bound by HBM: the rows p_a and q_a are read once (the search reads one segment of
-// them again, from the caches).  Sums are 64-bit: r is exact there, and a sum's
-// error, some 1e-15 of it, is far below the share of a token that 32-bit sums of
-// 10^5 terms would misplace.  Every sum has a fixed order.
+// Bound by HBM where many rows are long: p_a and q_a are read once (the search reads one
+// segment of them again, from the caches); otherwise by the chain of loads, each of which needs
+// the one before: the drafts, their probabilities, the row, the segment.  64 sequences of
+// 128256 tokens in fp32: 13.2 us for 66 MB (5.0 TB/s; the first two loads of the chain are some
+// 3 us of it) and 3.9 us for the search.  One sequence of 32000 in one launch: 8.5 us; in two
+// 5.5 and 4, and a launch more.
+// Lanes exchange by DPP moves; with LDS shuffles the search took 4.6 us.
+// Sums are 64-bit: r is exact there, and a sum's error, some 1e-15 of it, is far below the
+// share of a token that 32-bit sums of 10^5 terms would misplace.  Every sum has a fixed order.
 #include "kv4.h"
 
 namespace md {
@@ -106,79 +111,114 @@ __device__ __forceinline__ double vec_sum(const u32x4& x, const u32x4& y, int t,
   return sum;
 }
 
-// The sum of r over tokens [t0, t1), in order.
-template <bool BF16, bool VEC>
-__device__ __forceinline__ double span_sum(const SpecAcceptParams& p, const Residual& r, int t0,
-                                           int t1) {
-  double sum = 0.0;
-  if constexpr (VEC) {  // t0 and t1 are multiples of the vector's width
-    constexpr int N = Vec<BF16>::N, ES = BF16 ? 2 : 4;
-#pragma unroll 4
-    for (int t = t0; t < t1; t += N) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.p) + (r.prow + t) * ES);
-      u32x4 y = {0u, 0u, 0u, 0u};
-      if (r.qrow >= 0)
-        y = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (r.qrow + t) * ES);
-      sum += vec_sum<BF16>(x, y, t, r.one_at);
-    }
-  } else {
-    for (int t = t0; t < t1; ++t) sum += weight<BF16>(p, r, t);
-  }
-  return sum;
+// One step of the wave's scans and broadcasts: no LDS exchange, no latency to wait for.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp(double x) {  // zeros where there is no such lane
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(b), CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(b >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
 }
-
-// The sum of r over segment `seg`, by one wave (every lane gets it).
-template <bool BF16, bool VEC>
-__device__ __forceinline__ double segment_sum(const SpecAcceptParams& p, const Residual& r, int seg,
-                                              int lane) {
-  const int t0 = seg * p.seg_len, t1 = min(p.vocab, t0 + p.seg_len);
-  double sum = 0.0;
-  if constexpr (VEC) {
-    constexpr int N = Vec<BF16>::N, ES = BF16 ? 2 : 4, U = 4;
-    const char* pp = static_cast<const char*>(p.p) + r.prow * ES;
-    const char* qp = static_cast<const char*>(p.q) + r.qrow * ES;
-    for (int t = t0 + lane * N; t < t1; t += 64 * N * U) {
-      u32x4 x[U], y[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = t + u * 64 * N < t1 ? t + u * 64 * N : t;  // in bounds, not counted below
-        x[u] = *reinterpret_cast<const u32x4*>(pp + static_cast<int64_t>(at) * ES);
-        y[u] = u32x4{0u, 0u, 0u, 0u};
-        if (r.qrow >= 0)
-          y[u] = *reinterpret_cast<const u32x4*>(qp + static_cast<int64_t>(at) * ES);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (t + u * 64 * N < t1) sum += vec_sum<BF16>(x[u], y[u], t + u * 64 * N, r.one_at);
-    }
-  } else {
-#pragma unroll 4
-    for (int t = t0 + lane; t < t1; t += 64) sum += weight<BF16>(p, r, t);
-  }
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  return sum;
+__device__ __forceinline__ double lane_value(double x, int lane) {  // lane: uniform
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(b), lane);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(b >> 32), lane);
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
 }
-
-__device__ __forceinline__ double wave_scan(double x, int lane) {  // inclusive
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
+// Inclusive sums over the lanes: within rows of 16, then over the rows.
+__device__ __forceinline__ double wave_scan(double x) {
+  x += dpp<0x111, 0xf>(x);  // from 1, 2, 4, 8 lanes below in the row
+  x += dpp<0x112, 0xf>(x);
+  x += dpp<0x114, 0xf>(x);
+  x += dpp<0x118, 0xf>(x);
+  x += dpp<0x142, 0xa>(x);  // rows 1 and 3: the last lane of the row before
+  x += dpp<0x143, 0xc>(x);  // rows 2 and 3: lane 31
   return x;
+}
+__device__ __forceinline__ double wave_sum(double x) { return lane_value(wave_scan(x), 63); }
+
+// Segment `seg` by one wave: its loads, then (every lane gets it) the sum of r.
+template <bool BF16>
+struct SegVecs {
+  static constexpr int U = 4;
+  u32x4 x[U], y[U];
+};
+template <bool BF16>
+__device__ __forceinline__ void load_vecs(const SpecAcceptParams& p, const Residual& r, int t, int t1,
+                                          SegVecs<BF16>& v) {
+  constexpr int N = Vec<BF16>::N, ES = BF16 ? 2 : 4;
+  const char* pp = static_cast<const char*>(p.p) + r.prow * ES;
+  const char* qp = static_cast<const char*>(p.q) + r.qrow * ES;
+#pragma unroll
+  for (int u = 0; u < v.U; ++u) {
+    const int at = t + u * 64 * N;
+    v.x[u] = v.y[u] = u32x4{0u, 0u, 0u, 0u};
+    if (at < t1) {
+      v.x[u] = *reinterpret_cast<const u32x4*>(pp + static_cast<int64_t>(at) * ES);
+      if (r.qrow >= 0) v.y[u] = *reinterpret_cast<const u32x4*>(qp + static_cast<int64_t>(at) * ES);
+    }
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ double sum_vecs(const Residual& r, int t, const SegVecs<BF16>& v) {
+  double sum = 0.0;
+#pragma unroll
+  for (int u = 0; u < v.U; ++u)  // what is behind the end is 0
+    sum += vec_sum<BF16>(v.x[u], v.y[u], t + u * 64 * Vec<BF16>::N, r.one_at);
+  return sum;
+}
+// Segments seg and seg + next (that one: where there is one): both are loaded before either is
+// summed.
+template <bool BF16, bool VEC>
+__device__ __forceinline__ void segment_sums(const SpecAcceptParams& p, const Residual& r, int seg,
+                                             int next, int lane, double* out) {
+  constexpr int N = Vec<BF16>::N, kStep = 64 * N * SegVecs<BF16>::U;
+  const bool two = seg + next < p.n_segs;
+  double sum[2] = {0.0, 0.0};
+  for (int c = 0; c < p.seg_len; c += kStep) {
+    if constexpr (VEC) {
+      SegVecs<BF16> v[2];
+      int t[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int s0 = (seg + k * next) * p.seg_len;
+        t[k] = s0 + c + lane * N;
+        if (k == 0 || two) load_vecs<BF16>(p, r, t[k], min(p.vocab, s0 + p.seg_len), v[k]);
+      }
+      sum[0] += sum_vecs<BF16>(r, t[0], v[0]);
+      if (two) sum[1] += sum_vecs<BF16>(r, t[1], v[1]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (k == 1 && !two) break;
+        const int s0 = (seg + k * next) * p.seg_len;
+        const int t1 = min(min(p.vocab, s0 + p.seg_len), s0 + c + kStep);
+#pragma unroll 4
+        for (int t = s0 + c + lane; t < t1; t += 64) sum[k] += weight<BF16>(p, r, t);
+      }
+    }
+  }
+  const double a = wave_sum(sum[0]), b = wave_sum(sum[1]);
+  if (lane == 0) {
+    out[seg] = a;
+    if (two) out[seg + next] = b;
+  }
 }
 
 // Where a running sum that starts at `before` passes `want`: the first lane, in order, whose
 // own weight w > 0 brings it past, else the last lane with any weight (-1: none has).
-// before becomes the sum ahead of that lane; `all`: only a lane that passes counts.
-__device__ __forceinline__ int find_lane(double w, double want, bool all, int lane, double& before,
-                                         double& total) {
-  const double incl = before + wave_scan(w, lane);
+// before becomes the sum ahead of that lane; `all`: only a lane that passes counts, and without
+// one before becomes the whole sum.
+__device__ __forceinline__ int find_lane(double w, double want, bool all, double& before) {
+  const double incl = before + wave_scan(w);
   const unsigned long long some = __ballot(w > 0.0), pass = __ballot(w > 0.0 && incl > want);
-  total = __shfl(incl, 63);
-  if (!pass && (all || !some)) return -1;
+  if (!pass && (all || !some)) {
+    before = lane_value(incl, 63);
+    return -1;
+  }
   const int at = pass ? __ffsll(static_cast<long long>(pass)) - 1
                       : 63 - __clzll(static_cast<long long>(some));
-  before = __shfl(incl - w, at);
+  if (at) before = lane_value(incl, at - 1);
   return at;
 }
 
@@ -191,11 +231,11 @@ __device__ int draw_token(const SpecAcceptParams& p, int b, Residual r, const do
   const int s0 = min(p.n_segs, lane * per), s1 = min(p.n_segs, s0 + per);
   double mine = 0.0;
   for (int k = s0; k < s1; ++k) mine += sums[k];
-  double total = __shfl(wave_scan(mine, lane), 63);
+  const double total = wave_sum(mine);
   int c0 = 0, c1 = p.vocab;  // the tokens in which it is
-  double before = 0.0, want = u * total, end;
+  double before = 0.0, want = u * total;
   if (total > 0.0) {
-    const int at = find_lane(mine, want, false, lane, before, end);
+    const int at = find_lane(mine, want, false, before);
     int seg = -1, last = 0;
     double run = before;
     for (int k = min(p.n_segs, at * per); k < min(p.n_segs, (at + 1) * per); ++k) {
@@ -218,11 +258,74 @@ __device__ int draw_token(const SpecAcceptParams& p, int b, Residual r, const do
     r.one_at = -1;
   }
   // The span of them, consecutive tokens of a lane.
+  constexpr int kSpan = 16;  // tokens a lane can hold
   const int span = ((c1 - c0 + 63) / 64 + 7) / 8 * 8;
   const int t0 = min(c1, c0 + lane * span), t1 = min(c1, t0 + span);
-  const double w = span_sum<BF16, VEC>(p, r, t0, t1);
-  if (!(total > 0.0)) want = u * __shfl(wave_scan(w, lane), 63);
-  const int at = find_lane(w, want, false, lane, before, end);
+  if (total > 0.0 && span <= kSpan) {  // every segment of rows up to 2^20 tokens
+    float fp[kSpan], fq[kSpan];
+    constexpr int N = VEC ? Vec<BF16>::N : 1, ES = BF16 ? 2 : 4;
+#pragma unroll
+    for (int j = 0; j < kSpan; j += N) {
+      const bool in = t0 + j < t1;
+      if constexpr (VEC) {
+        u32x4 x = {0u, 0u, 0u, 0u}, y = {0u, 0u, 0u, 0u};
+        if (in) {
+          x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.p) + (r.prow + t0 + j) * ES);
+          if (r.qrow >= 0)
+            y = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (r.qrow + t0 + j) * ES);
+        }
+        float a[N], c[N];
+        Vec<BF16>::get(x, a);
+        Vec<BF16>::get(y, c);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          fp[j + k] = a[k];
+          fq[j + k] = c[k];
+        }
+      } else {
+        fp[j] = in ? load_prob<BF16>(p.p, r.prow + t0 + j) : 0.f;
+        fq[j] = in && r.qrow >= 0 ? load_prob<BF16>(p.q, r.qrow + t0 + j) : 0.f;
+      }
+    }
+    auto held = [&](int j) {
+      double w = static_cast<double>(fp[j]) - static_cast<double>(fq[j]);
+      if (t0 + j == r.one_at) w -= 1.0;
+      return w > 0.0 ? w : 0.0;
+    };
+    double w = 0.0;
+#pragma unroll
+    for (int j = 0; j < kSpan; ++j) w += held(j);
+    const int at = find_lane(w, want, false, before);
+    // Each lane looks among its own as if it were that one.
+    int past = -1, last = 0;
+    double run = before;
+#pragma unroll
+    for (int j = 0; j < kSpan; ++j) {
+      const double x = held(j);
+      run += x;
+      if (x > 0.0) {
+        last = j;
+        if (past < 0 && run > want) past = j;
+      }
+    }
+    return __builtin_amdgcn_readlane(t0 + (past >= 0 ? past : last), at);
+  }
+  double w = 0.0;
+  if constexpr (VEC) {  // t0 and t1 are multiples of the vector's width
+    constexpr int N = Vec<BF16>::N, ES = BF16 ? 2 : 4;
+#pragma unroll 4
+    for (int t = t0; t < t1; t += N) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.p) + (r.prow + t) * ES);
+      u32x4 y = {0u, 0u, 0u, 0u};
+      if (r.qrow >= 0)
+        y = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (r.qrow + t) * ES);
+      w += vec_sum<BF16>(x, y, t, r.one_at);
+    }
+  } else {
+    for (int t = t0; t < t1; ++t) w += weight<BF16>(p, r, t);
+  }
+  if (!(total > 0.0)) want = u * wave_sum(w);
+  const int at = find_lane(w, want, false, before);
   if (at < 0) return 0;  // p_a is all 0
   // The token, 64 at a time.
   const int e0 = c0 + at * span, e1 = min(c1, e0 + span);
@@ -231,9 +334,8 @@ __device__ int draw_token(const SpecAcceptParams& p, int b, Residual r, const do
     const double wt = t + lane < e1 ? weight<BF16>(p, r, t + lane) : 0.0;
     const unsigned long long some = __ballot(wt > 0.0);
     if (some) tok = t + 63 - __clzll(static_cast<long long>(some));
-    const int found = find_lane(wt, want, true, lane, before, end);
+    const int found = find_lane(wt, want, true, before);
     if (found >= 0) return t + found;
-    before = end;
   }
   return tok;
 }
@@ -253,10 +355,9 @@ __global__ void __launch_bounds__(256) spec_sum_kernel(const SpecAcceptParams p)
   const int a = accepted_count<BF16>(p, b, lane);
   if (first == 0 && lane == 0) p.accepted[b] = a;
   const Residual r = residual(p, b, a);
-  for (int seg = first; seg < p.n_segs; seg += 4 * p.wgs) {
-    const double sum = segment_sum<BF16, VEC>(p, r, seg, lane);
-    if (lane == 0) p.seg_sum[static_cast<int64_t>(b) * p.n_segs + seg] = sum;
-  }
+  for (int seg = first; seg < p.n_segs; seg += 8 * p.wgs)
+    segment_sums<BF16, VEC>(p, r, seg, 4 * p.wgs, lane,
+                            p.seg_sum + static_cast<int64_t>(b) * p.n_segs);
 }
 
 template <bool BF16, bool VEC>
@@ -275,10 +376,8 @@ __global__ void __launch_bounds__(1024) spec_fused_kernel(const SpecAcceptParams
   const int wave = static_cast<int>(threadIdx.x) >> 6;
   const int a = accepted_count<BF16>(p, b, lane);
   const Residual r = residual(p, b, a);
-  for (int seg = wave; seg < p.n_segs; seg += 16) {
-    const double sum = segment_sum<BF16, VEC>(p, r, seg, lane);
-    if (lane == 0) sums[seg] = sum;
-  }
+  for (int seg = wave; seg < p.n_segs; seg += 32)
+    segment_sums<BF16, VEC>(p, r, seg, 16, lane, sums);
   __syncthreads();
   if (wave != 0) return;
   if (lane == 0) p.accepted[b] = a;
