@@ -205,7 +205,7 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 
 // PG: 0 contiguous, 1 pages of at least 16 tokens, 2 smaller pages.
 template <int D, bool BF16, int NT, int PG>
-__global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(kKv4Resident(BF16, NT))))
+__global__ void __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(kKv4Resident(BF16, NT, D))))
 kv4_attn_kernel(const Kv4AttnParams p) {
   constexpr int LB = D / 8;         // code bytes a lane loads of a token: D / 4 channels
   constexpr int LW = LB / 4;        // their dwords: MFMA steps over the channels

@@ -17,8 +17,14 @@ constexpr int kKv4Tile = 32;
 constexpr int64_t kKv4MaxTokStride = int64_t{1} << 25;
 // Row tiles of 16 a pass over K and V takes: an fp32 query is three registers' worth of bf16.
 constexpr int kKv4MaxNT(bool bf16) { return bf16 ? 4 : 2; }
-// Workgroups a compute unit holds, a wave per SIMD each (their instances' registers).
-constexpr int kKv4Resident(bool bf16, int NT) { return bf16 && NT <= 2 ? 3 : 2; }
+// Workgroups a compute unit holds, a wave per SIMD each: as many as the registers of their
+// instances allow.  32 x 8 units of 16384 .. 32768 tokens against one less (fp32: against two):
+// bf16 d = 64, one row tile 99 us and 103, three 152 and 155; fp32 d = 64, one 113 and 133, two
+// 179 and 183, d = 128, one 181 and 190.  (bf16, two row tiles of d = 64: 124 with three or four.)
+constexpr int kKv4Resident(bool bf16, int NT, int d) {
+  if (d == 64) return bf16 ? (NT == 1 ? 4 : NT <= 3 ? 3 : 2) : (NT == 1 ? 4 : 3);
+  return bf16 ? (NT <= 2 ? 3 : 2) : (NT == 1 ? 3 : 2);
+}
 // Workgroups of 256 and of 1024 threads a launch may have: its threads are counted in 32 bits.
 constexpr int64_t kMaxWgs256 = (int64_t{1} << 24) - 1, kMaxWgs1024 = (int64_t{1} << 22) - 1;
 // The balanced plan ranks every sequence's tiles in each workgroup.

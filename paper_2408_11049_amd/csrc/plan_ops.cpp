@@ -126,7 +126,7 @@ Kv4Sizes kv4_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, i
     s.tiles = std::min(s.tiles, ceil_div(n_sink, kKv4Tile) +
                                     ceil_div(int64_t{window} + a->q_len - 1, kKv4Tile) + 1);
   s.cus = num_cus > 0 ? num_cus : 256;
-  s.resident = kKv4Resident(a->dtype == MD_BF16, s.p.NT);
+  s.resident = kKv4Resident(a->dtype == MD_BF16, s.p.NT, c->head_dim);
   return s;
 }
 

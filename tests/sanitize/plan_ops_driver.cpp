@@ -92,7 +92,7 @@ int main() {
                     check(p.NT * 16 * p.passes >= p.R && p.NT * 16 * (p.passes - 1) < p.R, "passes", p.passes, p.R);
                     check(p.n_blocks >= 1 && (p.balanced || p.n_blocks == units), "workgroups", p.n_blocks, units);
                     if (p.balanced) {
-                      check(B <= md::kKv4BalMaxSeqs && p.n_blocks <= 256 * 3, "ranges", B, p.n_blocks);
+                      check(B <= md::kKv4BalMaxSeqs && p.n_blocks <= 256 * 4, "ranges", B, p.n_blocks);
                       check(p.part_o_bytes >= size_t(2) * p.n_blocks * p.NT * 16 * d * 4, "partials");
                       check(p.workspace_bytes >= p.part_o_bytes + p.part_ml_bytes + size_t(16) * p.n_blocks,
                             "workspace");
