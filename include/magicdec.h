@@ -562,7 +562,7 @@ typedef struct {
  * the queries that see them get unspecified results.
  * Errors: MD_ERR_INVALID_ARG and MD_ERR_UNSUPPORTED as md_verify_attn,
  * md_draft_attn and md_kv4_append (a contiguous cache must hold max_kv_len tokens), also
- * UNSUPPORTED for B * Hkv > 2^23 - 1;
+ * UNSUPPORTED for B * Hkv > 2^22 - 1;
  * MD_ERR_WORKSPACE; MD_ERR_HIP.
  */
 int md_kv4_verify_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, void* stream);

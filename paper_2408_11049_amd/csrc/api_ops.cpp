@@ -80,6 +80,8 @@ int run_kv4_attn(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, int
   p.R = pl.R;
   p.passes = pl.passes;
   p.units = c->num_kv_heads * pl.passes;
+  p.share = pl.share;
+  p.groups = p.units / pl.share;
   const float scale =
       a->sm_scale > 0.f ? a->sm_scale : 1.0f / sqrtf(static_cast<float>(c->head_dim));
   p.scale_log2 = scale * 1.44269504088896340736f;

@@ -46,8 +46,8 @@ hipError_t launch_copy_lens(int B, const int32_t* pos0, int32_t* lens_out, hipSt
 hipError_t launch_kv4_read(const Kv4RowsParams& p, int head_dim, bool bf16, bool paged,
                            hipStream_t s);
 
-// The unit (sequence b, unit j) that a range boundary cuts first: its pieces are those of ranges
-// w - 1 (partial slot `first`) .. `last`.  b < 0: none.
+// The unit (a member of group j of sequence b) that the boundary where range w begins cuts as
+// its first: its pieces are those of ranges w - 1 (partial slot `first`) .. `last`.  b < 0: none.
 struct Join {
   int32_t b, j, last, first;
 };
@@ -59,6 +59,7 @@ struct Kv4AttnParams {
   int32_t max_kv_len;
   int32_t B, L, Hq, G, R;
   int32_t passes, units;      // passes over a head's K and V; units of a sequence: Hkv * passes
+  int32_t share, groups;      // units of a group (see kv4_attn.hip); groups of a sequence
   float scale_log2;           // softmax scale * log2(e)
   int32_t mode, n_sink, window;
   int32_t balanced;           // 1: workgroups share all units' tiles equally

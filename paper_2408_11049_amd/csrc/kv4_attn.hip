@@ -115,11 +115,23 @@ __device__ __forceinline__ Tiles tiles_of(const Kv4AttnParams& p, int S) {
   return t;
 }
 
-// Balanced plan: units in order (sequence, unit), max(1, tiles) stream tiles each; range w
+// Neighbouring units share memory lines: two passes the whole of K and V, heads of a 16-token
+// page the lines of its scales (64 bytes a head, d = 128), heads of a token-major cache those of
+// its codes too.  So `share` consecutive units form a group, and its units' workgroups run side
+// by side on one XCD, whose L2 then reads each line once.  Workgroups go to the eight XCDs in
+// turn: workgroup w has member w / 8 % share of range (or group) place(w).  32 x 8 units of 16384
+// tokens, alone and in groups: token-major 203 us and 177, fp32 206 and 168; 16-token pages of the
+// head-major layout 103 and 101; two fp32 passes 366 and 354.  (Groups of eight: 180 and 175.)
+__device__ __forceinline__ int member(const Kv4AttnParams& p, int w) { return w / 8 % p.share; }
+__device__ __forceinline__ int place(const Kv4AttnParams& p, int w) {
+  return w / (8 * p.share) * 8 + w % 8;
+}
+
+// Balanced plan: groups in order (sequence, group), max(1, tiles) stream tiles each; range w
 // of NW is [w TT / NW, (w + 1) TT / NW).
 struct Cursor {
   int t, hi;       // next stream tile, end of the range
-  int b, j;        // the current unit: unit j of sequence b
+  int b, j;        // the current group: group j of sequence b
   int g0, gt;      // its first stream tile and its number of tiles
   int TT, NW;
 };
@@ -137,7 +149,7 @@ __device__ int scan_tiles(const Kv4AttnParams& p, int* sl) {
     if (b < p.B) {
       const int S = length(p, b);
       sl[kKv4BalMaxSeqs + b] = S;
-      v[e] = max(tiles_of(p, S).n, 1) * p.units;
+      v[e] = max(tiles_of(p, S).n, 1) * p.groups;
     }
     mine += v[e];
   }
@@ -158,8 +170,8 @@ __device__ int scan_tiles(const Kv4AttnParams& p, int* sl) {
   return uniform(sl[p.B - 1]);
 }
 
-// The unit that holds stream tile t.  sl as scan_tiles leaves it.
-__device__ void unit_at(const Kv4AttnParams& p, const int* sl, int t, Cursor& c) {
+// The group that holds stream tile t.  sl as scan_tiles leaves it.
+__device__ void group_at(const Kv4AttnParams& p, const int* sl, int t, Cursor& c) {
   int lo = 0, hi = p.B - 1;  // the first sequence whose inclusive count passes t
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
@@ -168,7 +180,7 @@ __device__ void unit_at(const Kv4AttnParams& p, const int* sl, int t, Cursor& c)
   }
   c.b = uniform(lo);
   const int ex = c.b ? uniform(sl[c.b - 1]) : 0;
-  c.gt = (uniform(sl[c.b]) - ex) / p.units;
+  c.gt = (uniform(sl[c.b]) - ex) / p.groups;
   c.j = (t - ex) / c.gt;
   c.g0 = ex + c.j * c.gt;
 }
@@ -230,36 +242,38 @@ kv4_attn_kernel(const Kv4AttnParams p) {
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, grp = lane >> 4;
   const int wave = uniform(tid >> 6);
 
+  const int range = place(p, static_cast<int>(blockIdx.x));
+  const int mem = member(p, static_cast<int>(blockIdx.x));
   Cursor c{};
   int S_next;  // length of the next piece's sequence
   if (p.balanced) {
     int* sl = reinterpret_cast<int*>(lds);
     c.TT = scan_tiles(p, sl);
-    c.NW = ranges(static_cast<int>(gridDim.x), c.TT);
-    const int w = static_cast<int>(blockIdx.x);
+    c.NW = ranges(static_cast<int>(gridDim.x) / p.share, c.TT);
     Join join{-1, 0, 0, 0};
-    if (w < c.NW) {
-      c.t = range_start(c, w);
-      c.hi = range_start(c, w + 1);
-      unit_at(p, sl, c.t, c);
+    if (range < c.NW) {
+      c.t = range_start(c, range);
+      c.hi = range_start(c, range + 1);
+      group_at(p, sl, c.t, c);
       // The boundary where this range begins cuts a unit, as its first?  Then join it later.
-      if (c.t != c.g0 && range_start(c, w - 1) <= c.g0)
+      if (c.t != c.g0 && range_start(c, range - 1) <= c.g0)
         join = Join{c.b, c.j, range_of(c, c.g0 + c.gt - 1),
-                    2 * (w - 1) + (range_start(c, w - 1) != c.g0)};
+                    2 * ((range - 1) * p.share + mem) + (range_start(c, range - 1) != c.g0)};
     }
-    if (tid == 0) p.joins[w] = join;
-    if (w >= c.NW) return;  // the whole workgroup
+    if (tid == 0) p.joins[blockIdx.x] = join;
+    if (range >= c.NW) return;  // the whole workgroup
     S_next = sl[kKv4BalMaxSeqs + c.b];
     __syncthreads();        // the LDS is reused
   } else {
-    c.b = static_cast<int>(blockIdx.x) / p.units;
-    c.j = static_cast<int>(blockIdx.x) % p.units;
+    if (range >= p.B * p.groups) return;  // the whole workgroup
+    c.b = range / p.groups;
+    c.j = range % p.groups;
     S_next = length(p, c.b);
   }
 
   for (;;) {  // one pass a piece
-    const int b = c.b, hk = c.j / p.passes;
-    const int r0 = c.j % p.passes * ROWS;   // its rows of the head's R: r0 .. r0 + rows - 1
+    const int b = c.b, unit = c.j * p.share + mem, hk = unit / p.passes;
+    const int r0 = unit % p.passes * ROWS;  // its rows of the head's R: r0 .. r0 + rows - 1
     const int rows = min(p.R - r0, ROWS);
     const Tiles u = tiles_of(p, uniform(S_next));
     if (!p.balanced) c = Cursor{0, max(u.n, 1), b, c.j, 0, max(u.n, 1), max(u.n, 1), 1};
@@ -607,9 +621,9 @@ kv4_attn_kernel(const Kv4AttnParams p) {
         sl[wave * ROWS + rt * 16 + l16] = l_run[rt];
       }
     }
-    // A cut unit's piece: slot 2w for the first piece of range w, 2w + 1 for its last.
-    const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) +
-                         (p.balanced && c.t != range_start(c, static_cast<int>(blockIdx.x)));
+    // A cut unit's piece: two slots for each range of each member, its first piece's and its last's.
+    const int64_t slot = 2 * (static_cast<int64_t>(range) * p.share + mem) +
+                         (p.balanced && c.t != range_start(c, range));
 #pragma unroll
     for (int rt = 0; rt < NT; ++rt) {
       __syncthreads();  // the V tiles, or the last row tile's O, are done with
@@ -650,7 +664,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     c.t = min(c.hi, c.g0 + c.gt);
     if (c.t >= c.hi) return;
     c.g0 += c.gt;
-    if (++c.j == p.units) {
+    if (++c.j == p.groups) {
       c.j = 0;
       ++c.b;
       S_next = length(p, c.b);
@@ -660,18 +674,18 @@ kv4_attn_kernel(const Kv4AttnParams p) {
   }
 }
 
-// Joins the pieces of the units that range boundaries cut: workgroup (w, y) takes rows
-// 4 y .. of the unit whose first cut is where range w begins, if it is one.  The waves take the
+// Joins the pieces of the units that range boundaries cut: workgroup (x, y) takes rows
+// 4 y .. of the unit whose first cut is where the range of workgroup x begins, if it is one.  The waves take the
 // pieces in turn (fixed order), then their sums are joined through LDS.
 template <int D, bool BF16, int NT>
 __global__ void __launch_bounds__(W * 64) kv4_join_kernel(const Kv4AttnParams p, int rows_per_wg) {
   constexpr int kQuads = D / 4, ROWS = NT * 16, kRows = 64 / kQuads;  // rows a wave takes at once
   __shared__ __attribute__((aligned(16))) float so[W][64][4];
   __shared__ float sm[W][64], sl[W][64];
-  const int w = static_cast<int>(blockIdx.x);
-  const Join join = p.joins[w];
+  const Join join = p.joins[blockIdx.x];
   if (join.b < 0) return;  // the whole workgroup
-  const int hk = join.j / p.passes, r0 = join.j % p.passes * ROWS;
+  const int w = place(p, static_cast<int>(blockIdx.x)), mem = member(p, static_cast<int>(blockIdx.x));
+  const int unit = join.j * p.share + mem, hk = unit / p.passes, r0 = unit % p.passes * ROWS;
   const int rows = min(p.R - r0, ROWS);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c0 = lane % kQuads * 4;
@@ -688,7 +702,8 @@ __global__ void __launch_bounds__(W * 64) kv4_join_kernel(const Kv4AttnParams p,
 #pragma unroll 4
     for (int k = split ? wave : 0; k < n; k += split ? W : 1) {
       const int64_t row =
-          static_cast<int64_t>(k == 0 ? join.first : 2 * (w - 1 + k)) * ROWS + (live ? r : first);
+          static_cast<int64_t>(k == 0 ? join.first : 2 * ((w - 1 + k) * p.share + mem)) * ROWS +
+          (live ? r : first);
       const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + row * 2);
       const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + row * D + c0);
       const float m_new = fmaxf(M, ml[0]);

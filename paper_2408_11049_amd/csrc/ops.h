@@ -39,6 +39,7 @@ int validate_kv4_buffers(const md_kv4_cache* c);
 struct Kv4Plan {
   int32_t G = 0, R = 0;           // query heads and rows a KV head
   int32_t NT = 0, passes = 1;     // 16-row tiles of a pass over K and V, and passes
+  int32_t share = 1;              // units whose workgroups run side by side (kv4_attn.hip)
   bool balanced = false;
   int32_t n_blocks = 0;           // workgroups
   size_t part_o_bytes = 0, part_ml_bytes = 0, workspace_bytes = 0;  // then 16 bytes a workgroup

@@ -74,7 +74,7 @@ int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int m
   if (static_cast<int64_t>(a->num_q_heads / c->num_kv_heads) * a->q_len > kMaxRows)
     return MD_ERR_UNSUPPORTED;
   // Up to two passes, a workgroup each, a (sequence, head).
-  if (static_cast<int64_t>(c->num_seqs) * c->num_kv_heads > kMaxWgs256 / 2)
+  if (static_cast<int64_t>(c->num_seqs) * c->num_kv_heads > kMaxWgs256 / 4)
     return MD_ERR_UNSUPPORTED;
   if (a->max_kv_len > kMaxPosition) return MD_ERR_UNSUPPORTED;
   if (mode == MD_MODE_DRAFT && (window > kMaxPosition || n_sink > kMaxPosition))
@@ -121,6 +121,13 @@ Kv4Sizes kv4_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, i
   s.p.passes = (s.p.R + max_rows - 1) / max_rows;
   s.p.NT = (std::min(s.p.R, max_rows) + 15) / 16;
   s.units = static_cast<int64_t>(c->num_seqs) * c->num_kv_heads * s.p.passes;
+  // How many neighbouring units share memory lines: the passes of a head, and the heads whose
+  // scales of a token (16-token page) are within a line of 128 bytes.
+  const int64_t apart = c->stride_head / 16;  // bytes between two heads' scales
+  const int64_t heads = apart <= 32 ? 4 : (apart < 128 ? 2 : 1);
+  for (int64_t n : {int64_t{2}, int64_t{4}})
+    if (n <= heads * s.p.passes && c->num_kv_heads * s.p.passes % n == 0)
+      s.p.share = static_cast<int32_t>(n);
   s.tiles = ceil_div(a->max_kv_len, kKv4Tile);
   if (mode == MD_MODE_DRAFT)
     s.tiles = std::min(s.tiles, ceil_div(n_sink, kKv4Tile) +
@@ -128,6 +135,11 @@ Kv4Sizes kv4_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode, i
   s.cus = num_cus > 0 ? num_cus : 256;
   s.resident = kKv4Resident(a->dtype == MD_BF16, s.p.NT, c->head_dim);
   return s;
+}
+
+// Workgroups for n of them in groups, each group's on one XCD of eight.
+int32_t whole_groups(int64_t n, int32_t share) {
+  return static_cast<int32_t>(share == 1 ? n : ceil_div(n, 8 * share) * 8 * share);
 }
 
 bool kv4_whole(const Kv4Sizes& s, int64_t tiles, const md_kv4_cache* c) {
@@ -138,8 +150,8 @@ bool kv4_whole(const Kv4Sizes& s, int64_t tiles, const md_kv4_cache* c) {
 void kv4_balance(const Kv4Sizes& s, int64_t tiles, int head_dim, Kv4Plan* p) {
   const size_t rows = 16 * static_cast<size_t>(p->NT);
   p->balanced = true;
-  p->n_blocks = static_cast<int32_t>(
-      std::min(s.cus * s.resident, ceil_div(tiles * s.units, kWaves)));
+  p->n_blocks = whole_groups(std::min(s.cus * s.resident, ceil_div(tiles * s.units, kWaves)),
+                             p->share);
   p->part_o_bytes =
       align_up(static_cast<size_t>(2 * p->n_blocks) * rows * head_dim * sizeof(float), 256);
   p->part_ml_bytes = align_up(static_cast<size_t>(2 * p->n_blocks) * rows * 2 * sizeof(float), 256);
@@ -154,7 +166,7 @@ Kv4Plan make_kv4_plan(const md_kv4_cache* c, const md_kv4_attn_args* a, int mode
   const Kv4Sizes s = kv4_sizes(c, a, mode, n_sink, window, num_cus);
   Kv4Plan p = s.p;
   if (kv4_whole(s, s.tiles, c))
-    p.n_blocks = static_cast<int32_t>(s.units);
+    p.n_blocks = whole_groups(s.units, p.share);
   else
     kv4_balance(s, s.tiles, c->head_dim, &p);
   return p;

@@ -65,7 +65,7 @@ md_kv4_attn_args args(int L, int Hq, int dtype, int64_t S) {
 int main() {
   const int64_t lens[] = {1, 16, 31, 512, 1024, 1025, 1537, 2048, 2600, 3500, 4001, 4096, 4097, 32768, 131072, 1 << 24, INT_MAX - 64};
   long plans = 0, balanced = 0;
-  for (int B : {1, 2, 7, 64, 300, 1024, 1025, 1 << 19})
+  for (int B : {1, 2, 7, 64, 300, 1024, 1025, 1 << 18})
     for (int Hkv : {1, 3, 8})
       for (int G : {1, 4, 7})
         for (int L : {1, 5, 9, 16})
@@ -89,8 +89,10 @@ int main() {
                     balanced += p.balanced;
                     const int64_t units = int64_t{B} * Hkv * p.passes;
                     check(p.R == G * L && p.NT >= 1 && p.NT <= md::kKv4MaxNT(dtype == MD_BF16), "rows", p.R, p.NT);
+                    check(Hkv * p.passes % p.share == 0 && (p.share == 1 || p.n_blocks % (8 * p.share) == 0),
+                          "whole groups", p.share, p.n_blocks);
                     check(p.NT * 16 * p.passes >= p.R && p.NT * 16 * (p.passes - 1) < p.R, "passes", p.passes, p.R);
-                    check(p.n_blocks >= 1 && (p.balanced || p.n_blocks == units), "workgroups", p.n_blocks, units);
+                    check(p.n_blocks >= 1 && (p.balanced || (p.n_blocks >= units && p.n_blocks < units + 8 * p.share)), "workgroups", p.n_blocks, units);
                     if (p.balanced) {
                       check(B <= md::kKv4BalMaxSeqs && p.n_blocks <= 256 * 4, "ranges", B, p.n_blocks);
                       check(p.part_o_bytes >= size_t(2) * p.n_blocks * p.NT * 16 * d * 4, "partials");
