@@ -257,6 +257,19 @@ def test_attention_long_and_ragged(dtype):
     check(q, cache, pt, lens, dtype)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype,Hq,Hkv,L,layout,page", [
+    ("bf16", 8, 8, 3, "token", 0), ("bf16", 12, 6, 1, "token", 16), ("f32", 8, 4, 2, "token", 4),
+    ("f32", 12, 3, 10, "head", 0), ("f32", 8, 2, 10, "head", 16), ("bf16", 4, 4, 2, "head", 16),
+    ("bf16", 5, 5, 2, "token", 0)])
+@pytest.mark.parametrize("lens", [[2500, 40, 0], [900, 1024]])
+def test_attention_neighbouring_units(dtype, d, Hq, Hkv, L, layout, page, lens):
+    """Heads that share memory lines, and two passes over a head, in ranges and whole."""
+    q = randn((len(lens), L, Hq, d), dtype, Hkv + L)
+    cache, pt = filled(len(lens), max(lens), Hkv, d, page, layout, seed=Hkv)
+    check(q, cache, pt, lens, dtype)
+
+
 def test_attention_one_long_sequence():
     cache, pt = filled(1, 30000, 1, 64, seed=9)
     check(randn((1, 1, 2, 64), "bf16", 9), cache, pt, [29999], "bf16")
