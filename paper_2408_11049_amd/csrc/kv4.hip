@@ -8,7 +8,9 @@
 // vector each, so a wave reads whole rows, and one dword of codes each -- and
 // four neighbouring threads find their block's maximum in two lane swaps.  Rows go
 // (sequence, head, token): neighbouring rows of a [block][head][token] cache are
-// then written side by side, whole lines by one workgroup.
+// then written side by side, whole lines by one workgroup.  8 x 4096 tokens of 8 heads of 128,
+// bf16: append 32 us, read 28 us, 170 MB each (a large copy would take 35).  A step of 64 x 5
+// tokens takes 3.4 and 5.7 us, a launch and one or two dependent loads.
 #include "kv4.h"
 
 namespace md {
