@@ -306,7 +306,19 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     const int64_t unit_off = static_cast<int64_t>(hk) * p.c.s_head +
                              (PG ? 0 : static_cast<int64_t>(b) * p.c.s_blk);
     const uint32_t s_tok = static_cast<uint32_t>(p.c.s_tok);
-    const uint32_t sidx = grp * (D / 4) / 32;  // this lane's scale byte in its row
+    // This lane's scale byte in its row.  d = 128: the row's four are one dword, loaded whole, and
+    // the byte is taken out of it where it is used.  (A loaded byte is widened to a register behind
+    // the softmax already, which waits for the loads in flight; d = 64 does.)
+    constexpr bool kWholeRow = D == 128;
+    const uint32_t sidx = grp * (D / 4) / 32;
+    const uint32_t sfirst = kWholeRow ? 0 : sidx;
+    auto scale_byte = [&](uint32_t loaded) {
+      return kWholeRow ? (loaded >> (8 * sidx)) & 255u : loaded;
+    };
+    auto load_scale = [](global_bytes* at) -> uint32_t {
+      if constexpr (kWholeRow) return *(const __attribute__((address_space(1))) uint32_t*)(at);
+      return *at;
+    };
     auto real_tile = [&](int v) { return v < u.head ? v : v - u.head + u.tail0; };
     // First token of block tb of piece tile v, in a block that holds a real token.
     auto block_at = [&](int v, int tb) {
@@ -330,7 +342,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
     // the sequence too where they are in the cache (masked below): the lanes' offsets are then
     // the same for every block.  Tiles past the piece are its last one, never used.
     const uint32_t code_off = static_cast<uint32_t>(l16) * s_tok + grp * LB;
-    const uint32_t scale_off = static_cast<uint32_t>(l16) * (s_tok >> 4) + sidx;
+    const uint32_t scale_off = static_cast<uint32_t>(l16) * (s_tok >> 4) + sfirst;
     auto load_tile = [&](TileRegs& r, int k) {
       const int v = wave + k * W;
 #pragma unroll
@@ -343,7 +355,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
           if (bt + 16 > p.c.capacity) {  // the cache ends inside the block
             const uint32_t dt = static_cast<uint32_t>(min(l16, S - 1 - bt));
             code = dt * s_tok + grp * LB;
-            scale = dt * (s_tok >> 4) + sidx;
+            scale = dt * (s_tok >> 4) + sfirst;
           }
         } else if constexpr (PG == 1) {
           const int id = __builtin_amdgcn_readlane(ids, (k & 31) * 2 + tb);
@@ -354,13 +366,13 @@ kv4_attn_kernel(const Kv4AttnParams p) {
           base = unit_off + static_cast<int64_t>(page_ok(ptab[t >> p.c.page_shift])) * p.c.s_blk +
                  static_cast<int64_t>(static_cast<uint64_t>(t & pmask) * s_tok);
           code = grp * LB;
-          scale = sidx;
+          scale = sfirst;
         }
         asm("" : "+v"(code), "+v"(scale));  // 32 bits up to the load: see block_ptr
         load_words(block_ptr<PG>(p.c.k, base) + code, r.k[tb]);
         load_words(block_ptr<PG>(p.c.v, base) + code, r.v[tb]);
-        r.ks[tb] = *(block_ptr<PG>(p.c.ks, base >> 4) + scale);
-        r.vs[tb] = *(block_ptr<PG>(p.c.vs, base >> 4) + scale);
+        r.ks[tb] = load_scale(block_ptr<PG>(p.c.ks, base >> 4) + scale);
+        r.vs[tb] = load_scale(block_ptr<PG>(p.c.vs, base >> 4) + scale);
       }
     };
 
@@ -434,12 +446,13 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       // V into LDS as bf16 rows.  In a masked tile a row past the sequence, or one that is NaN
       // in this lane's block, is staged as zeros: 0 * NaN must not reach a query that does
       // not see it; those that see it are noted and get their NaN at the end.
-      float vscale[2] = {scale_of(r.vs[0]), scale_of(r.vs[1])};
+      const uint32_t vbyte[2] = {scale_byte(r.vs[0]), scale_byte(r.vs[1])};
+      float vscale[2] = {scale_of(vbyte[0]), scale_of(vbyte[1])};
       if (masked) {
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
           const bool past = t0 + tb * 16 + l16 >= S;
-          const bool bad = r.vs[tb] == 255u;
+          const bool bad = vbyte[tb] == 255u;
           for (unsigned long long left = __ballot(bad && !past); left; left &= left - 1) {
             const int at = __ffsll(static_cast<long long>(left)) - 1;
 #pragma unroll
@@ -469,7 +482,7 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       for (int rt = 0; rt < NT; ++rt)
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) s[rt][tb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const float ks[2] = {scale_of(r.ks[0]), scale_of(r.ks[1])};
+      const float ks[2] = {scale_of(scale_byte(r.ks[0])), scale_of(scale_byte(r.ks[1]))};
 #pragma unroll
       for (int w = 0; w < LW; ++w) {
         bf16x8 kk[2];
