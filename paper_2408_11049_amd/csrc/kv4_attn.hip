@@ -24,9 +24,10 @@
 // unit that a cut crosses is computed in pieces, which a second launch joins.  Where a
 // workgroup for each unit is put at less than that, the plan takes that (plan_ops.cpp).
 //
-// Measured (bf16, d = 128, 32 query heads on 8): 64 sequences of 16384 .. 32768 tokens, 5 query
-// tokens, 16-token pages 320 to 371 us by the card and 7 to 8 for the joins, 1.78 GB: 4.8 to 5.5 TB/s
-// (its loads alone: 280 to 306 us); 32 of 8192, one query token 48 and 4 us: 6.0 TB/s.
+// Measured (bf16, d = 128, 32 query heads on 8): a call over 64 sequences of 16384 .. 32768
+// tokens, 5 query tokens, 16-token pages 332 to 350 us by the card, joins included: 1.78 GB at 5.1
+// to 5.3 TB/s (its loads alone: 280 to 306 us); 32 of 8192, one query token 48 us and 4.6 for the
+// joins: 6.0 TB/s.
 #include "kv4.h"
 
 namespace md {

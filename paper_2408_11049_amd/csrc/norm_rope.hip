@@ -11,7 +11,7 @@
 // their fraction of a turn) and serve all the token's heads from LDS.
 //
 // What keeps the memory busy is many small workgroups, each with two passes' rows loaded and
-// the next two under way: 4 x 4096 tokens of 32 + 8 heads of 128 in bf16 80 us, 5.0 TB/s read
+// the next two under way: 4 x 4096 tokens of 32 + 8 heads of 128 in bf16 78 us, 5.2 TB/s read
 // and written (a large copy: 4.9).  Against that, on one card: one pass at a time 97 to 93, three
 // 98, four tokens a workgroup 104, no rows ahead 100.  A step of 64 x 5 tokens takes 6.1 us, of
 // which the bytes would need 1.6.
