@@ -218,7 +218,10 @@ SpecPlan make_spec_plan(int32_t num_seqs, int32_t vocab, int num_cus) {
   pl.seg_len = static_cast<int32_t>(len);
   pl.n_segs = static_cast<int32_t>(ceil_div(vocab, len));
   const int64_t wgs = std::min(ceil_div(4 * cus, std::max(num_seqs, 1)), ceil_div(pl.n_segs, 4));
-  if (num_seqs > 0 && wgs > 1 && pl.n_segs > 32) {
+  // One workgroup's sixteen waves do up to 32 segments in a go; two goes still beat the second
+  // launch where rows start on whole vectors.
+  const int one = vocab % 8 ? 32 : 64;
+  if (num_seqs > 0 && wgs > 1 && pl.n_segs > one) {
     pl.wgs = static_cast<int32_t>(wgs);
     pl.workspace_bytes = static_cast<size_t>(num_seqs) * pl.n_segs * sizeof(double);
   }

@@ -140,7 +140,7 @@ __device__ __forceinline__ double wave_sum(double x) { return lane_value(wave_sc
 // Segment `seg` by one wave: its loads, then (every lane gets it) the sum of r.
 template <bool BF16>
 struct SegVecs {
-  static constexpr int U = 4;
+  static constexpr int U = BF16 ? 2 : 4;  // a segment of 1024 tokens
   u32x4 x[U], y[U];
 };
 template <bool BF16>
