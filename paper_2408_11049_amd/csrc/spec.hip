@@ -37,6 +37,13 @@ __device__ __forceinline__ float load_prob(const void* base, int64_t e) {
 template <bool BF16>
 struct Vec {  // 16 bytes of probabilities
   static constexpr int N = BF16 ? 8 : 4;
+  // Rows begin where the vocabulary puts them: any element's address will do for a load.
+  static __device__ __forceinline__ u32x4 load(const void* base, int64_t e) {
+    typedef u32x4 at2 __attribute__((aligned(2)));
+    typedef u32x4 at4 __attribute__((aligned(4)));
+    if constexpr (BF16) return *reinterpret_cast<const at2*>(static_cast<const uint16_t*>(base) + e);
+    return *reinterpret_cast<const at4*>(static_cast<const float*>(base) + e);
+  }
   static __device__ __forceinline__ void get(const u32x4& w, float (&x)[N]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -146,16 +153,14 @@ struct SegVecs {
 template <bool BF16>
 __device__ __forceinline__ void load_vecs(const SpecAcceptParams& p, const Residual& r, int t, int t1,
                                           SegVecs<BF16>& v) {
-  constexpr int N = Vec<BF16>::N, ES = BF16 ? 2 : 4;
-  const char* pp = static_cast<const char*>(p.p) + r.prow * ES;
-  const char* qp = static_cast<const char*>(p.q) + r.qrow * ES;
+  constexpr int N = Vec<BF16>::N;
 #pragma unroll
   for (int u = 0; u < v.U; ++u) {
     const int at = t + u * 64 * N;
     v.x[u] = v.y[u] = u32x4{0u, 0u, 0u, 0u};
-    if (at < t1) {
-      v.x[u] = *reinterpret_cast<const u32x4*>(pp + static_cast<int64_t>(at) * ES);
-      if (r.qrow >= 0) v.y[u] = *reinterpret_cast<const u32x4*>(qp + static_cast<int64_t>(at) * ES);
+    if (at + N <= t1) {
+      v.x[u] = Vec<BF16>::load(p.p, r.prow + at);
+      if (r.qrow >= 0) v.y[u] = Vec<BF16>::load(p.q, r.qrow + at);
     }
   }
 }
@@ -169,34 +174,30 @@ __device__ __forceinline__ double sum_vecs(const Residual& r, int t, const SegVe
 }
 // Segments seg and seg + next (that one: where there is one): both are loaded before either is
 // summed.
-template <bool BF16, bool VEC>
+template <bool BF16>
 __device__ __forceinline__ void segment_sums(const SpecAcceptParams& p, const Residual& r, int seg,
                                              int next, int lane, double* out) {
   constexpr int N = Vec<BF16>::N, kStep = 64 * N * SegVecs<BF16>::U;
   const bool two = seg + next < p.n_segs;
   double sum[2] = {0.0, 0.0};
   for (int c = 0; c < p.seg_len; c += kStep) {
-    if constexpr (VEC) {
-      SegVecs<BF16> v[2];
-      int t[2];
+    SegVecs<BF16> v[2];
+    int t[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int s0 = (seg + k * next) * p.seg_len;
-        t[k] = s0 + c + lane * N;
-        if (k == 0 || two) load_vecs<BF16>(p, r, t[k], min(p.vocab, s0 + p.seg_len), v[k]);
-      }
-      sum[0] += sum_vecs<BF16>(r, t[0], v[0]);
-      if (two) sum[1] += sum_vecs<BF16>(r, t[1], v[1]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (k == 1 && !two) break;
-        const int s0 = (seg + k * next) * p.seg_len;
-        const int t1 = min(min(p.vocab, s0 + p.seg_len), s0 + c + kStep);
-#pragma unroll 4
-        for (int t = s0 + c + lane; t < t1; t += 64) sum[k] += weight<BF16>(p, r, t);
-      }
+    for (int k = 0; k < 2; ++k) {
+      const int s0 = (seg + k * next) * p.seg_len;
+      t[k] = s0 + c + lane * N;
+      if (k == 0 || two) load_vecs<BF16>(p, r, t[k], min(p.vocab, s0 + p.seg_len), v[k]);
     }
+    sum[0] += sum_vecs<BF16>(r, t[0], v[0]);
+    if (two) sum[1] += sum_vecs<BF16>(r, t[1], v[1]);
+  }
+  // What is behind the row's last whole vector, in its last segment.
+  const int rest = p.vocab - p.vocab % N + lane;
+  if (rest < p.vocab) {
+    const double w = weight<BF16>(p, r, rest);
+    if (seg == p.n_segs - 1) sum[0] += w;
+    if (seg + next == p.n_segs - 1) sum[1] += w;
   }
   const double a = wave_sum(sum[0]), b = wave_sum(sum[1]);
   if (lane == 0) {
@@ -223,7 +224,7 @@ __device__ __forceinline__ int find_lane(double w, double want, bool all, double
 }
 
 // The drawn token, by one wave; sums: the segments' (LDS or global).
-template <bool BF16, bool VEC>
+template <bool BF16>
 __device__ int draw_token(const SpecAcceptParams& p, int b, Residual r, const double* sums, int lane) {
   const double u = p.u[static_cast<int64_t>(b) * (p.n_draft + 1) + p.n_draft];
   // A lane takes `per` consecutive segments.
@@ -263,17 +264,13 @@ __device__ int draw_token(const SpecAcceptParams& p, int b, Residual r, const do
   const int t0 = min(c1, c0 + lane * span), t1 = min(c1, t0 + span);
   if (total > 0.0 && span <= kSpan) {  // every segment of rows up to 2^20 tokens
     float fp[kSpan], fq[kSpan];
-    constexpr int N = VEC ? Vec<BF16>::N : 1, ES = BF16 ? 2 : 4;
+    if (t0 + kSpan <= t1) {
+      constexpr int N = Vec<BF16>::N;
 #pragma unroll
-    for (int j = 0; j < kSpan; j += N) {
-      const bool in = t0 + j < t1;
-      if constexpr (VEC) {
-        u32x4 x = {0u, 0u, 0u, 0u}, y = {0u, 0u, 0u, 0u};
-        if (in) {
-          x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.p) + (r.prow + t0 + j) * ES);
-          if (r.qrow >= 0)
-            y = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (r.qrow + t0 + j) * ES);
-        }
+      for (int j = 0; j < kSpan; j += N) {
+        const u32x4 x = Vec<BF16>::load(p.p, r.prow + t0 + j);
+        u32x4 y = {0u, 0u, 0u, 0u};
+        if (r.qrow >= 0) y = Vec<BF16>::load(p.q, r.qrow + t0 + j);
         float a[N], c[N];
         Vec<BF16>::get(x, a);
         Vec<BF16>::get(y, c);
@@ -282,7 +279,11 @@ __device__ int draw_token(const SpecAcceptParams& p, int b, Residual r, const do
           fp[j + k] = a[k];
           fq[j + k] = c[k];
         }
-      } else {
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kSpan; ++j) {
+        const bool in = t0 + j < t1;
         fp[j] = in ? load_prob<BF16>(p.p, r.prow + t0 + j) : 0.f;
         fq[j] = in && r.qrow >= 0 ? load_prob<BF16>(p.q, r.qrow + t0 + j) : 0.f;
       }
@@ -311,18 +312,17 @@ __device__ int draw_token(const SpecAcceptParams& p, int b, Residual r, const do
     return __builtin_amdgcn_readlane(t0 + (past >= 0 ? past : last), at);
   }
   double w = 0.0;
-  if constexpr (VEC) {  // t0 and t1 are multiples of the vector's width
-    constexpr int N = Vec<BF16>::N, ES = BF16 ? 2 : 4;
+  {
+    constexpr int N = Vec<BF16>::N;
+    int t = t0;
 #pragma unroll 4
-    for (int t = t0; t < t1; t += N) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.p) + (r.prow + t) * ES);
+    for (; t + N <= t1; t += N) {
+      const u32x4 x = Vec<BF16>::load(p.p, r.prow + t);
       u32x4 y = {0u, 0u, 0u, 0u};
-      if (r.qrow >= 0)
-        y = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (r.qrow + t) * ES);
+      if (r.qrow >= 0) y = Vec<BF16>::load(p.q, r.qrow + t);
       w += vec_sum<BF16>(x, y, t, r.one_at);
     }
-  } else {
-    for (int t = t0; t < t1; ++t) w += weight<BF16>(p, r, t);
+    for (; t < t1; ++t) w += weight<BF16>(p, r, t);
   }
   if (!(total > 0.0)) want = u * wave_sum(w);
   const int at = find_lane(w, want, false, before);
@@ -347,7 +347,7 @@ __device__ __forceinline__ void store_tokens(const SpecAcceptParams& p, int b, i
         i < a ? p.draft[static_cast<int64_t>(b) * n + i] : (i == a ? tok : -1);
 }
 
-template <bool BF16, bool VEC>
+template <bool BF16>
 __global__ void __launch_bounds__(256) spec_sum_kernel(const SpecAcceptParams p) {
   const int b = static_cast<int>(blockIdx.x) / p.wgs;
   const int lane = threadIdx.x & 63;
@@ -356,20 +356,20 @@ __global__ void __launch_bounds__(256) spec_sum_kernel(const SpecAcceptParams p)
   if (first == 0 && lane == 0) p.accepted[b] = a;
   const Residual r = residual(p, b, a);
   for (int seg = first; seg < p.n_segs; seg += 8 * p.wgs)
-    segment_sums<BF16, VEC>(p, r, seg, 4 * p.wgs, lane,
+    segment_sums<BF16>(p, r, seg, 4 * p.wgs, lane,
                             p.seg_sum + static_cast<int64_t>(b) * p.n_segs);
 }
 
-template <bool BF16, bool VEC>
+template <bool BF16>
 __global__ void __launch_bounds__(64) spec_pick_kernel(const SpecAcceptParams p) {
   const int b = blockIdx.x, lane = threadIdx.x;
   const int a = p.accepted[b];
-  const int tok = draw_token<BF16, VEC>(p, b, residual(p, b, a),
+  const int tok = draw_token<BF16>(p, b, residual(p, b, a),
                                         p.seg_sum + static_cast<int64_t>(b) * p.n_segs, lane);
   store_tokens(p, b, a, tok, lane);
 }
 
-template <bool BF16, bool VEC>
+template <bool BF16>
 __global__ void __launch_bounds__(1024) spec_fused_kernel(const SpecAcceptParams p) {
   __shared__ double sums[kSpecMaxSegs];
   const int b = blockIdx.x, lane = threadIdx.x & 63;
@@ -377,35 +377,27 @@ __global__ void __launch_bounds__(1024) spec_fused_kernel(const SpecAcceptParams
   const int a = accepted_count<BF16>(p, b, lane);
   const Residual r = residual(p, b, a);
   for (int seg = wave; seg < p.n_segs; seg += 32)
-    segment_sums<BF16, VEC>(p, r, seg, 16, lane, sums);
+    segment_sums<BF16>(p, r, seg, 16, lane, sums);
   __syncthreads();
   if (wave != 0) return;
   if (lane == 0) p.accepted[b] = a;
-  store_tokens(p, b, a, draw_token<BF16, VEC>(p, b, r, sums, lane), lane);
+  store_tokens(p, b, a, draw_token<BF16>(p, b, r, sums, lane), lane);
 }
 
-template <bool BF16, bool VEC>
+template <bool BF16>
 static void launch_spec(const SpecAcceptParams& p, hipStream_t s) {
   if (p.wgs == 0) {
-    hipLaunchKernelGGL((spec_fused_kernel<BF16, VEC>), dim3(p.B), dim3(1024), 0, s, p);
+    hipLaunchKernelGGL((spec_fused_kernel<BF16>), dim3(p.B), dim3(1024), 0, s, p);
     return;
   }
   const dim3 g(static_cast<uint32_t>(p.B) * static_cast<uint32_t>(p.wgs));
-  hipLaunchKernelGGL((spec_sum_kernel<BF16, VEC>), g, dim3(256), 0, s, p);
-  hipLaunchKernelGGL((spec_pick_kernel<BF16, VEC>), dim3(p.B), dim3(64), 0, s, p);
+  hipLaunchKernelGGL((spec_sum_kernel<BF16>), g, dim3(256), 0, s, p);
+  hipLaunchKernelGGL((spec_pick_kernel<BF16>), dim3(p.B), dim3(64), 0, s, p);
 }
 
 hipError_t launch_spec_accept(const SpecAcceptParams& p, bool bf16, hipStream_t s) {
-  // Whole 16-byte vectors where every row starts on one.
-  const bool vec = p.vocab % (bf16 ? 8 : 4) == 0 && (reinterpret_cast<uintptr_t>(p.p) & 15u) == 0 &&
-                   (reinterpret_cast<uintptr_t>(p.q) & 15u) == 0;
-  if (bf16) {
-    if (vec) launch_spec<true, true>(p, s);
-    else launch_spec<true, false>(p, s);
-  } else {
-    if (vec) launch_spec<false, true>(p, s);
-    else launch_spec<false, false>(p, s);
-  }
+  if (bf16) launch_spec<true>(p, s);
+  else launch_spec<false>(p, s);
   return hipGetLastError();
 }
 

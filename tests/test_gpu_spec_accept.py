@@ -53,6 +53,22 @@ def test_shapes(dtype, sampled, B, g, V):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sampled", [True, False])
+@pytest.mark.parametrize("B,V", [(3, 50257), (2, 65535), (2, 65537), (3, 70001), (1, (1 << 20) + 4099)])
+def test_rows_that_end_inside_a_vector(dtype, sampled, B, V):
+    """Rows that start and end anywhere, in one launch and in two; draws from the last tokens and
+    from all over."""
+    for last in (None, 1 - 2.0 ** -24, 1 - 2.0 ** -17, 0.0):
+        p, q, draft, u = make(B, 2, V, dtype, V % 7, sampled)
+        if last is not None:
+            u[:, -1] = last
+        check(p, q, draft, u)
+        heavy = p.clone()  # the mass on the row's last tokens
+        heavy[:, :, -3:] = 0.25
+        check(heavy, q, draft, u)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_draws_at_the_borders(dtype):
     """Probabilities that are powers of two, sums and products exact: u on every border."""
     V, g = 16, 1
