@@ -12,9 +12,10 @@
 // Bound by HBM where many rows are long: p_a and q_a are read once (the search reads one
 // segment of them again, from the caches); otherwise by the chain of loads, each of which needs
 // the one before: the drafts, their probabilities, the row, the segment.  64 sequences of
-// 128256 tokens in fp32: 13.2 us for 66 MB (5.0 TB/s; the first two loads of the chain are some
-// 3 us of it) and 3.9 us for the search.  One sequence of 32000 in one launch: 8.5 us; in two
-// 5.5 and 4, and a launch more.
+// 128256 tokens in fp32: 13.5 us for 66 MB (4.9 TB/s; the first two loads of the chain are some
+// 3 us of it) and 4.0 us for the search.  One sequence of 32000 in one launch: 8.5 us.
+// Loads are of 16 bytes wherever a row starts: element by element 64 rows of 50257 took 21.9 us
+// a call, so 14.5.
 // Lanes exchange by DPP moves; with LDS shuffles the search took 4.6 us.
 // Sums are 64-bit: r is exact there, and a sum's error, some 1e-15 of it, is far below the
 // share of a token that 32-bit sums of 10^5 terms would misplace.  Every sum has a fixed order.
