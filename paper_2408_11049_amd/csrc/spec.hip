@@ -186,7 +186,7 @@ __device__ __forceinline__ void segment_sums(const SpecAcceptParams& p, const Re
     int t[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int s0 = (seg + k * next) * p.seg_len;
+      const int s0 = (k && two ? seg + next : seg) * p.seg_len;
       t[k] = s0 + c + lane * N;
       if (k == 0 || two) load_vecs<BF16>(p, r, t[k], min(p.vocab, s0 + p.seg_len), v[k]);
     }
