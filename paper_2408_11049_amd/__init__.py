@@ -281,20 +281,25 @@ def _device_scoped(fn):
     Kv4Cache) as the current one: the library takes its plans and its launches to
     the current device."""
     scoped = _stream_scoped(fn)
+    name = fn.__code__.co_varnames[0]
 
     @functools.wraps(fn)
-    def wrapped(first, *args, stream=None, **kw):
-        t = first.k if type(first) is Kv4Cache else first
+    def wrapped(*args, stream=None, **kw):
+        if not args and name not in kw:
+            return fn(stream=stream, **kw)  # raises: the argument is missing
+        t = args[0] if args else kw[name]
+        if type(t) is Kv4Cache:
+            t = t.k
         dev = t.get_device()
         torch = _torch_module or _torch()
         if dev < 0:
             raise ValueError(f"tensors must be on a GPU, not {t.device}")
         if stream is None and torch._C._cuda_getDevice() == dev:
-            return fn(first, *args, stream=None, **kw)
+            return fn(*args, stream=None, **kw)
         if stream is not None and stream.device.index != dev:
             raise ValueError(f"stream is on {stream.device}; the call runs on {t.device}")
         with torch.cuda.device(dev):
-            return scoped(first, *args, stream=stream, **kw)
+            return scoped(*args, stream=stream, **kw)
     return wrapped
 
 
