@@ -277,8 +277,8 @@ def _stream_scoped(fn):
 
 
 def _device_scoped(fn):
-    """_stream_scoped, with the device of the call's first argument (a tensor or a
-    Kv4Cache) as the current one: the library takes its plans and its launches to
+    """_stream_scoped, with the device of the call's first argument (a tensor or a 4-bit
+    cache's tensors) as the current one: the library takes its plans and its launches to
     the current device."""
     scoped = _stream_scoped(fn)
     name = fn.__code__.co_varnames[0]
@@ -288,8 +288,8 @@ def _device_scoped(fn):
         if not args and name not in kw:
             return fn(stream=stream, **kw)  # raises: the argument is missing
         t = args[0] if args else kw[name]
-        if type(t) is Kv4Cache:
-            t = t.k
+        if isinstance(t, (tuple, list)):
+            t = t[0]
         dev = t.get_device()
         torch = _torch_module or _torch()
         if dev < 0:
@@ -938,10 +938,10 @@ def md_kv4_append(cache, k_new, v_new, pos0, *, page_table=None, lens_out=None, 
     c = make_kv4_cache(cache, num_seqs=B, page_table=page_table)
     if heads != c.num_kv_heads or d != c.head_dim:
         raise ValueError("appended rows must have the cache's heads and head_dim")
-    gpu = cache.k.get_device()
+    gpu = cache[0].get_device()
     if k_new.get_device() != gpu or v_new.get_device() != gpu or pos0.get_device() != gpu or (
             lens_out is not None and lens_out.get_device() != gpu):
-        _on_gpu(cache.k, k_new=k_new, v_new=v_new, pos0=pos0, lens_out=lens_out)
+        _on_gpu(cache[0], k_new=k_new, v_new=v_new, pos0=pos0, lens_out=lens_out)
     _ints("pos0", pos0, B)
     if lens_out is None:
         lens_out = pos0.new_empty((B,))
@@ -964,9 +964,9 @@ def md_kv4_read(cache, pos0, n, *, page_table=None, dtype=None, k_out=None, v_ou
     B = pos0.shape[0]
     c = make_kv4_cache(cache, num_seqs=B, page_table=page_table)
     shape = (B, n, c.num_kv_heads, c.head_dim)
-    gpu = cache.k.get_device()
+    gpu = cache[0].get_device()
     if pos0.get_device() != gpu or k_out is not None or v_out is not None:
-        _on_gpu(cache.k, pos0=pos0, k_out=k_out, v_out=v_out)
+        _on_gpu(cache[0], pos0=pos0, k_out=k_out, v_out=v_out)
     _ints("pos0", pos0, B)
     if dtype is None:
         dtype = _torch_module.bfloat16 if k_out is None else k_out.dtype
@@ -1031,8 +1031,8 @@ def _kv4_attention(q, cache, kv_lens, mode, n_sink, window, *, max_kv_len=None, 
     lib = load_library()
     c = make_kv4_cache(cache, num_seqs=q.shape[0], page_table=page_table)
     gpu = q.get_device()
-    if cache.k.get_device() != gpu:
-        _on_gpu(q, cache=cache.k)
+    if cache[0].get_device() != gpu:
+        _on_gpu(q, cache=cache[0])
     a = _kv4_args(q, c, kv_lens, max_kv_len, sm_scale, out, lse, workspace)
     if out is None:
         out = torch.empty_like(q)

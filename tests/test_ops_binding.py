@@ -39,3 +39,12 @@ def test_arguments_by_name(lib, name):  # noqa: F811
             f(*args, **named)
     with pytest.raises(TypeError, match=first):  # and a missing one is named
         f(**{k: kw[k] for k in kw if k != first})
+
+
+@pytest.mark.parametrize("name", [c for c in CALLS if "kv4" in c])
+def test_a_cache_of_four_tensors(lib, name):  # noqa: F811
+    """A cache may be any sequence of the four tensors."""
+    kw = host_call(name)
+    for kind in (tuple, list):
+        with pytest.raises(ValueError, match="on a GPU"):
+            getattr(md, name)(**{**kw, "cache": kind(kw["cache"])})
