@@ -848,6 +848,14 @@ def md_kv_gather(dst_k, dst_v, src_k, src_v, idx, idx_len, src_lens, *, dst_page
     return dst_lens
 
 
+def _int32(name, x):
+    """x for a 32-bit field of the library, which would take it modulo 2^32."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must fit 32 bits, not {x}")
+    return x
+
+
 class Kv4Cache(NamedTuple):
     """A KV cache in 4 bits (see include/magicdec.h).  k, v: uint8 codes, two a
     byte, [B, S_alloc, Hkv, d / 2], or paged [P, page_size, Hkv, d / 2];
@@ -910,7 +918,7 @@ def make_kv4_cache(cache, *, num_seqs=None, page_table=None) -> MdKv4Cache:
         elif num_seqs > blocks:
             raise ValueError("a contiguous cache must hold num_seqs sequences")
         return MdKv4Cache(num_seqs, heads, 2 * half, k.data_ptr(), v.data_ptr(), ks.data_ptr(),
-                          vs.data_ptr(), sb, stok, sh, 0, 0, 0, None, toks)
+                          vs.data_ptr(), sb, stok, sh, 0, 0, 0, None, min(toks, 2 ** 31 - 1))
     if (page_table.dtype != _torch_module.int32 or not page_table.is_contiguous()
             or page_table.dim() != 2):
         raise ValueError("page_table must be contiguous int32 [B, max_pages]")
@@ -920,7 +928,7 @@ def make_kv4_cache(cache, *, num_seqs=None, page_table=None) -> MdKv4Cache:
     elif rows < num_seqs:
         raise ValueError("page_table must have a row per sequence")
     return MdKv4Cache(num_seqs, heads, 2 * half, k.data_ptr(), v.data_ptr(), ks.data_ptr(),
-                      vs.data_ptr(), sb, stok, sh, toks, max_pages, blocks,
+                      vs.data_ptr(), sb, stok, sh, toks, _int32("max_pages", max_pages), blocks,
                       page_table.data_ptr(), 0)
 
 
@@ -1008,7 +1016,8 @@ def _kv4_args(q, c, kv_lens, max_kv_len, sm_scale, out, lse, workspace):
     _ints("kv_lens", kv_lens, B)
     if max_kv_len is None:  # a bound that needs no device sync
         max_kv_len = c.max_pages_per_seq * c.page_size if c.page_size else c.capacity
-    return MdKv4AttnArgs(L, Hq, _code(q), sm_scale, q.data_ptr(), kv_lens.data_ptr(), max_kv_len,
+    return MdKv4AttnArgs(L, Hq, _code(q), sm_scale, q.data_ptr(), kv_lens.data_ptr(),
+                         _int32("max_kv_len", max_kv_len),
                          None if out is None else out.data_ptr(),
                          None if lse is None else lse.data_ptr(),
                          None if workspace is None else workspace.data_ptr(),
@@ -1020,8 +1029,8 @@ def md_kv4_workspace_bytes(q, cache, kv_lens, *, mode=MD_MODE_VERIFY, n_sink=0, 
     """Workspace bytes md_kv4_verify_attn or md_kv4_draft_attn needs for these tensors."""
     c = make_kv4_cache(cache, num_seqs=q.shape[0], page_table=page_table)
     a = _kv4_args(q, c, kv_lens, max_kv_len, 0.0, None, None, None)
-    return int(load_library().md_kv4_workspace_bytes(ctypes.byref(c), ctypes.byref(a), mode, n_sink,
-                                                     window))
+    return int(load_library().md_kv4_workspace_bytes(
+        ctypes.byref(c), ctypes.byref(a), mode, _int32("n_sink", n_sink), _int32("window", window)))
 
 
 @_device_scoped
@@ -1062,7 +1071,8 @@ def md_kv4_verify_attn(q, cache, kv_lens, **kw):
 
 def md_kv4_draft_attn(q, cache, kv_lens, n_sink, window, **kw):
     """md_draft_attn (sinks and window) over a 4-bit cache (see include/magicdec.h)."""
-    return _kv4_attention(q, cache, kv_lens, MD_MODE_DRAFT, int(n_sink), int(window), **kw)
+    return _kv4_attention(q, cache, kv_lens, MD_MODE_DRAFT, _int32("n_sink", n_sink),
+                          _int32("window", window), **kw)
 
 
 @_device_scoped

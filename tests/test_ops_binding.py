@@ -48,3 +48,51 @@ def test_a_cache_of_four_tensors(lib, name):  # noqa: F811
     for kind in (tuple, list):
         with pytest.raises(ValueError, match="on a GPU"):
             getattr(md, name)(**{**kw, "cache": kind(kw["cache"])})
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it is on device 0, for host arithmetic on its sizes."""
+
+    def get_device(self):
+        return 0
+
+
+def on_gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+def test_sizes_past_32_bits_do_not_wrap(lib):  # noqa: F811
+    """A bound, window or sink count past 32 bits is refused, not taken modulo 2^32."""
+    cache = md.Kv4Cache(*map(on_gpu, md.kv4_empty(1, 16384, 1, 64, device="cpu")))
+    q, lens = on_gpu(torch.zeros((1, 1, 4, 64))), on_gpu(torch.zeros(1, dtype=torch.int32))
+
+    def need(**kw):
+        return md.md_kv4_workspace_bytes(q, cache, lens, **kw)
+    draft = dict(mode=md.MD_MODE_DRAFT)
+    assert need() == need(max_kv_len=16384) > 0
+    assert need(window=9000, **draft) > 0 == need(window=40, **draft)
+    for wrap in (2 ** 32, -2 ** 32, 2 ** 40):
+        for kw in (dict(max_kv_len=16384 + wrap), dict(max_kv_len=40 + wrap),
+                   dict(window=9000 + wrap, **draft), dict(window=9000, n_sink=4 + wrap, **draft)):
+            with pytest.raises(ValueError, match="32 bits"):
+                need(**kw)
+    for n_sink, window in ((4, 2 ** 32 + 40), (2 ** 32, 40)):
+        with pytest.raises(ValueError, match="32 bits"):
+            md.md_kv4_draft_attn(q, cache, lens, n_sink, window)
+
+
+def test_caches_past_32_bits(lib):  # noqa: F811
+    """Positions are 32-bit: a longer contiguous cache serves those it has, and a table of as
+    many columns is refused."""
+    far = 2 ** 32 + 96
+    cache = [on_gpu(torch.zeros((1, 1, 1, w), dtype=torch.uint8).expand(1, far, 1, w))
+             for w in (32, 32, 2, 2)]
+    assert md.make_kv4_cache(cache).capacity == 2 ** 31 - 1
+    pages = [on_gpu(torch.zeros((1, 16, 1, w), dtype=torch.uint8)) for w in (32, 32, 2, 2)]
+    assert md.make_kv4_cache(pages, page_table=on_gpu(torch.zeros((1, 3), dtype=torch.int32))
+                             ).max_pages_per_seq == 3
+
+    class Wide(OnGpu):
+        shape = property(lambda t: torch.Size((1, far)))
+    with pytest.raises(ValueError, match="32 bits"):
+        md.make_kv4_cache(pages, page_table=torch.zeros((1, 3), dtype=torch.int32).as_subclass(Wide))
