@@ -604,7 +604,8 @@ size_t md_kv4_workspace_bytes(const md_kv4_cache* c, const md_kv4_attn_args* a, 
  *                 contents
  * Only the rows p_a and q_a are read whole.  Errors: MD_ERR_INVALID_ARG for NULL or
  * misaligned pointers (probabilities: their element size), n_draft outside [0, 1023],
- * vocab outside [1, 2^30], a bad dtype; MD_ERR_UNSUPPORTED for num_seqs > 2^22 - 1;
+ * vocab outside [1, 2^30], a bad dtype, accepted, tokens or the workspace's bytes in use
+ * overlapping an input or each other; MD_ERR_UNSUPPORTED for num_seqs > 2^22 - 1;
  * MD_ERR_WORKSPACE; MD_ERR_HIP.
  */
 int md_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype,

@@ -174,6 +174,9 @@ int md_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dty
   if (pl.workspace_bytes && (!workspace || workspace_bytes < pl.workspace_bytes ||
                              md::misaligned(workspace, 256)))
     return MD_ERR_WORKSPACE;
+  if (md::spec_accept_overlaps(num_seqs, n_draft, vocab, dtype, target_probs, draft_probs, draft, u,
+                               accepted, tokens, workspace, pl.workspace_bytes))
+    return MD_ERR_INVALID_ARG;
   md::SpecAcceptParams p{};
   p.p = target_probs;
   p.q = draft_probs;

@@ -63,6 +63,12 @@ struct SpecPlan {
 };
 int validate_spec_accept(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype);
 SpecPlan make_spec_plan(int32_t num_seqs, int32_t vocab, int num_cus);
+// Whether an output or the workspace (its first ws_bytes) shares memory with an input or with
+// each other: they are written while other workgroups read.
+bool spec_accept_overlaps(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype,
+                          const void* p, const void* q, const void* draft, const void* u,
+                          const void* accepted, const void* tokens, const void* ws,
+                          size_t ws_bytes);
 
 // Sizes, strides, pointers and overlaps; c may be NULL (no cache).
 int validate_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* c);

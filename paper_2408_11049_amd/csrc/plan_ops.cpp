@@ -227,6 +227,25 @@ SpecPlan make_spec_plan(int32_t num_seqs, int32_t vocab, int num_cus) {
   return pl;
 }
 
+bool spec_accept_overlaps(int32_t num_seqs, int32_t n_draft, int32_t vocab, int32_t dtype,
+                          const void* p, const void* q, const void* draft, const void* u,
+                          const void* accepted, const void* tokens, const void* ws,
+                          size_t ws_bytes) {
+  const wide B = num_seqs, n = n_draft, row = static_cast<wide>(vocab) * (dtype == MD_BF16 ? 2 : 4);
+  const struct {
+    const void* p;
+    wide bytes;
+  } out[3] = {{accepted, B * 4}, {tokens, B * (n + 1) * 4}, {ws, static_cast<wide>(ws_bytes)}},
+    in[4] = {{p, B * (n + 1) * row}, {q, B * n * row}, {draft, B * n * 4}, {u, B * (n + 1) * 4}};
+  for (int i = 0; i < 3; ++i) {
+    for (const auto& x : in)
+      if (overlap(out[i].p, out[i].bytes, x.p, x.bytes)) return true;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return true;
+  }
+  return false;
+}
+
 int validate_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* c) {
   if (!a) return MD_ERR_INVALID_ARG;
   if (a->num_seqs < 0 || a->n_new < 0 || a->num_q_heads < 1 || a->num_kv_heads < 1 ||
