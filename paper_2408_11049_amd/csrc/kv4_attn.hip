@@ -25,9 +25,10 @@
 // workgroup for each unit is put at less than that, the plan takes that (plan_ops.cpp).
 //
 // Measured (bf16, d = 128, 32 query heads on 8): a call over 64 sequences of 16384 .. 32768
-// tokens, 5 query tokens, 16-token pages 332 to 350 us by the card, joins included: 1.78 GB at 5.1
-// to 5.3 TB/s (its loads alone: 280 to 306 us); 32 of 8192, one query token 48 us and 4.6 for the
-// joins: 6.0 TB/s.
+// tokens, 5 query tokens, 16-token pages 323 to 361 us by the card, 8 of them the joins: 1.78 GB at
+// 4.9 to 5.5 TB/s (its loads alone: 280 to 306 us).  That is in a loop, once the clock has settled:
+// calls 5 to 20 after an idle second take up to 426.  32 of 8192, one query token 48 us and 4.6 for
+// the joins: 6.0 TB/s.
 #include "kv4.h"
 
 namespace md {
@@ -523,6 +524,11 @@ kv4_attn_kernel(const Kv4AttnParams p) {
       for (int cb = 0; cb < kAhead; ++cb) va[cb] = read_v(cb);
       __builtin_amdgcn_sched_barrier(0);
 
+      // bf16 queries: a weight is rounded to bf16 before it multiplies V, its sum is not.  O is then
+      // 2.1e-3 to 2.3e-3 off (root mean square, of which its own rounding to bf16 is 1.66e-3) and
+      // lse 4e-8 of itself.  Weights in two bf16 parts give 1.66e-3, but take 409 us where this takes 357 to
+      // 361 (64 x 16384 .. 32768 tokens, two row tiles, one card; one row tile 57.4 and 55.7); a sum
+      // of the rounded weights gives O 2.11e-3 for 2.25e-3, but lse 2.7e-5.
       // Softmax weights 2^y, y = c s - m, c = scale * log2 e: lane's row l16, tokens tb*16 + 4
       // grp + e.  A row's m moves only when some y passes kLazy (at first: whenever a key is
       // visible), so most tiles need no exchange between the four lanes of a row; until

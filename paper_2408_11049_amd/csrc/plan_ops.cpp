@@ -89,7 +89,8 @@ int check_kv4_attn_sizes(const md_kv4_cache* c, const md_kv4_attn_args* a, int m
 // 0.62 of its rate, with two at 0.93: 32 x 8 units of 2048 tokens 26.5 us whole, 25.4 in
 // ranges; 64 x 8 of 2048 31.6 and 39.7, of 4096 56.9 and 61.0; 128 x 8 of 2048 62.7 and 66.1, of
 // 4096 114.6 and 108.1.  Lengths are not known here: from 4096 tokens on, unequal ones would
-// cost whole units more than that.
+// cost whole units more than that.  All of this was measured with bf16 queries of one row tile at
+// d = 128, three workgroups a compute unit; the other instances take the same rates.
 static bool whole_units(int64_t tiles, int64_t units, int64_t cus, int64_t resident, int d) {
   if (tiles <= kKv4WholeTiles) return true;
   if (tiles > kKv4RangeTiles) return false;

@@ -12,8 +12,10 @@
 // Bound by HBM where many rows are long: p_a and q_a are read once (the search reads one
 // segment of them again, from the caches); otherwise by the chain of loads, each of which needs
 // the one before: the drafts, their probabilities, the row, the segment.  64 sequences of
-// 128256 tokens in fp32: 13.5 us for 66 MB (4.9 TB/s; the first two loads of the chain are some
+// 128256 tokens in fp32: 13.3 us for 66 MB (4.9 TB/s; the first two loads of the chain are some
 // 3 us of it) and 4.0 us for the search.  One sequence of 32000 in one launch: 8.5 us.
+// Where nothing of p_a is above q_a, which equal rows alone give, the one wave that searches reads
+// the whole row: 132 us for those 64 sequences, 30 for 32000 tokens.
 // Loads are of 16 bytes wherever a row starts: element by element 64 rows of 50257 took 21.9 us
 // a call, so 14.5.
 // Lanes exchange by DPP moves; with LDS shuffles the search took 4.6 us.
