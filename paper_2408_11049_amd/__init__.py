@@ -860,7 +860,8 @@ class Kv4Cache(NamedTuple):
     """A KV cache in 4 bits (see include/magicdec.h).  k, v: uint8 codes, two a
     byte, [B, S_alloc, Hkv, d / 2], or paged [P, page_size, Hkv, d / 2];
     k_scale, v_scale: uint8 [.., Hkv, d / 32], the scale of each 32 channels.  Any
-    strides of whole rows; the scales' are the codes' / 16."""
+    strides of whole rows; the scales' are the codes' / 16.  The calls take any sequence of
+    the four."""
     k: Any
     v: Any
     k_scale: Any
