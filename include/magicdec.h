@@ -665,6 +665,154 @@ typedef struct {
 int md_qk_norm_rope(const md_qk_norm_rope_args* a, const md_kv_cache* cache, void* stream);
 
 /*
+ * ---- Several answers of one prompt ----
+ *
+ * A batch whose sequences share a long prefix (one prompt answered many times, a system prompt
+ * under every request) keeps the prefix's K and V once.  The B sequences form P groups of
+ * B / P neighbours: sequence b reads prefix b / (B / P), then its own cache.
+ */
+typedef struct {
+  int32_t num_prefixes;       /* P >= 1; num_seqs is a multiple of it */
+  const void* k;              /* as md_attn_args, one block (or row of page_table) a prefix */
+  const void* v;
+  int64_t kv_stride_blk, kv_stride_tok, kv_stride_head;
+  int32_t page_size;          /* 0 = contiguous, else tokens per page (power of two) */
+  int32_t max_pages_per_prefix;  /* columns of page_table (paged only) */
+  int64_t num_pages;          /* pages in the pool (paged only); the pool may be the sequences' */
+  const int32_t* page_table;  /* device [P, max_pages_per_prefix], or NULL when contiguous */
+  const int32_t* lens;        /* device [P]: tokens of each prefix, 0 allowed */
+  int32_t max_len;            /* HOST bound on every lens[p], >= 0 */
+} md_prefix;
+
+/*
+ * md_verify_attn over a prefix and a cache of the sequence's own: query row i of sequence b sees
+ * every token of its prefix and the own tokens j <= S_b - L + i.  `a` describes the queries,
+ * the own caches (kv_lens counts own tokens only, the L of the call included), the results and
+ * the workspace; head_dim, dtype and head counts hold for both caches.  A prefix is read once for
+ * all rows of its group.
+ * Softmax and sums are fp32; with bf16 inputs the softmax weights are rounded to bf16 before
+ * they multiply V (lse is not).  A query that sees nothing (an empty prefix, no own token) gets
+ * o = 0, lse = -inf; one whose sum is NaN gets o = NaN, lse = -inf.  Lengths are clamped to
+ * [0, max]; a sequence of fewer than L own tokens has its first rows see the prefix alone.
+ * Tokens on pages outside [0, num_pages) are not dereferenced, and the queries that see them
+ * get unspecified results.  err_word reports both caches.
+ * Errors: as md_verify_attn, for either cache; MD_ERR_INVALID_ARG also for a NULL prefix or lens,
+ * num_prefixes < 1 or no divisor of num_seqs, max_len < 0; MD_ERR_UNSUPPORTED also for sizes past
+ * the grid's 32 bits (2^24 - 1 workgroups); MD_ERR_WORKSPACE (a workspace is always needed).
+ */
+int md_prefix_attn(const md_attn_args* a, const md_prefix* prefix, void* stream);
+
+/* Workspace bytes of md_prefix_attn: host arithmetic on the sizes and the current device's compute
+ * units; pointers are not read; 0 for malformed arguments.  A buffer for a max_kv_len and a max_len
+ * serves every smaller ones. */
+size_t md_prefix_workspace_bytes(const md_attn_args* a, const md_prefix* prefix);
+
+/*
+ * The weight that attention gives each cached token, accumulated: what a cache of bounded size
+ * is cut by (md_kv_evict).  For own token j < S_b of sequence b and KV head hk
+ *   w(j) = sum over rows i <= accepted[b] with j <= S_b - L + i, and over the head's G query heads,
+ *          of exp(sm_scale q_i . k_j - lse_i),
+ *   mass[b][hk][j] = w(j) for the L newest tokens (j >= S_b - L), else mass[b][hk][j] + w(j),
+ *   slot_pos[b][hk][S_b - L + i] = pos0[b] + i, the newest tokens' positions in their sequence.
+ * Entries from S_b on are left as they are.
+ */
+typedef struct {
+  int32_t num_seqs;           /* B >= 0 */
+  int32_t q_len;              /* L >= 1: a step's tokens, or a whole prompt */
+  int32_t num_q_heads, num_kv_heads, head_dim, dtype;  /* as md_attn_args; any G and L */
+  float sm_scale;             /* <= 0: 1/sqrt(d) */
+  const void* q;              /* [B, L, Hq, d], contiguous, 16-byte aligned */
+  const void* k;              /* as md_attn_args (contiguous or paged) */
+  int64_t kv_stride_blk, kv_stride_tok, kv_stride_head;
+  int32_t page_size, max_pages_per_seq;
+  int64_t num_pages;
+  const int32_t* page_table;
+  const int32_t* kv_lens;     /* device [B]: S_b, the L tokens included; clamped to [0, max_kv_len] */
+  int32_t max_kv_len;         /* HOST bound, >= q_len */
+  const float* lse;           /* device [B, L, Hq]: of the attention that ran (over whatever it saw);
+                                 -inf: the row weighs nothing */
+  const int32_t* accepted;    /* device [B], clamped to [0, L - 1], or NULL: every row counts */
+  const int32_t* pos0;        /* device [B] */
+  float* mass;                /* device [B, Hkv, slot_stride] in and out */
+  int32_t* slot_pos;          /* device [B, Hkv, slot_stride] in and out */
+  int64_t slot_stride;        /* >= max_kv_len */
+  void* workspace;            /* >= md_kv_mass_workspace_bytes() (0: none), 256-byte aligned */
+  size_t workspace_bytes;
+} md_kv_mass_args;
+
+/*
+ * Products and sums are fp32, in a fixed order.  Tokens on pages outside [0, num_pages) are not
+ * dereferenced and get an unspecified mass.
+ * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers, bad sizes, strides or page
+ * geometry, q_len > max_kv_len > slot_stride, mass or slot_pos overlapping each other or an
+ * input; MD_ERR_UNSUPPORTED for head_dim not in {64,128}, kv_stride_tok > 2^28
+ * elements, max_kv_len > 2^31 - 65, L * G > 2^31 - 65, or sizes past the grid's 32 bits (2^24 - 1
+ * workgroups); MD_ERR_WORKSPACE; MD_ERR_HIP.
+ */
+int md_kv_mass(const md_kv_mass_args* a, void* stream);
+size_t md_kv_mass_workspace_bytes(const md_kv_mass_args* a);
+
+/*
+ * Cut every (sequence, KV head) of a cache down to `budget` tokens by accumulated weight.  With
+ * n = lens[b] (clamped to [0, what the cache holds and slot_stride]) and n > budget, the n - budget
+ * tokens of least mass are evicted (ties: the lower slot first; a NaN counts as the least), but those
+ * with slot_pos < n_sink or slot_pos >= seq_lens[b] - recent only after all others, the lower slot
+ * first (that takes positions that occur more than once).  No page may hold tokens of two
+ * sequences.  The tokens kept
+ * in slots >= budget move, in order, into the slots < budget that this frees, with their mass and
+ * slot_pos; everything else stays where it is.  Slots hold tokens in no particular order then,
+ * which attention over the cache does not see (positions are in the keys).
+ *   c         the cache, in place; per-head contents, one length a sequence
+ *   mass      device fp32  [B, Hkv, slot_stride], in place (see md_kv_mass)
+ *   slot_pos  device int32 [B, Hkv, slot_stride], in place
+ *   lens      device int32 [B]: tokens each sequence's cache holds
+ *   seq_lens  device int32 [B]: tokens of the sequence so far, evicted ones included
+ *   lens_out  device int32 [B] out, or NULL: min(lens[b], budget)
+ *   workspace >= md_kv_evict_workspace_bytes() (0: none), 256-byte aligned, any contents
+ * Rows on pages outside [0, num_pages) are neither read nor written; a token that would move from or
+ * to one is lost.  Values move bit for bit.
+ * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers, a malformed cache, budget < 1,
+ * n_sink < 0, recent < 0, n_sink + recent > budget, slot_stride < 1, mass, slot_pos, lens_out or
+ * the workspace overlapping an input or each other; MD_ERR_UNSUPPORTED for head_dim not in {64,128},
+ * B * Hkv > 2^22 - 1 or slot_stride > 2^31 - 65; MD_ERR_WORKSPACE; MD_ERR_HIP.
+ */
+int md_kv_evict(const md_kv_cache* c, float* mass, int32_t* slot_pos, int64_t slot_stride,
+                const int32_t* lens, const int32_t* seq_lens, int32_t budget, int32_t n_sink,
+                int32_t recent, int32_t* lens_out, void* workspace, size_t workspace_bytes,
+                void* stream);
+size_t md_kv_evict_workspace_bytes(const md_kv_cache* c, int64_t slot_stride, int32_t budget);
+
+/*
+ * Log probabilities of given tokens, the entropy and the most likely tokens of every row of
+ * logits x, with lse = ln sum_v exp(x_v):
+ *   logprobs[r]       = x[tokens[r]] - lse; 0 where tokens[r] < 0 (no token: rows after a
+ *                       step's accepted ones), NaN where tokens[r] >= vocab
+ *   entropy[r]        = -sum_v p_v ln p_v, p_v = exp(x_v - lse)
+ *   top[r][j]         the j-th largest logit's index (ties: the lower first; NaN compares as
+ *                     -inf), -1 from vocab on
+ *   top_logprobs[r][j] = x[top[r][j]] - lse, -inf from vocab on
+ * A -inf logit (a masked token) has probability 0 and log probability -inf.  A row of nothing but
+ * -inf has log probabilities -inf and entropy 0.  A NaN or +inf in a row makes its log
+ * probabilities and its entropy NaN.
+ *   logits        device, row r at r * row_stride elements, in dtype (MD_F32 or MD_BF16)
+ *   tokens        device int32 [rows], or NULL with logprobs NULL
+ *   logprobs, entropy  device fp32 [rows] out, or NULL
+ *   top, top_logprobs  device int32 and fp32 [rows, top_k] out (NULL with top_k = 0)
+ *   workspace     >= md_token_logprobs_workspace_bytes() (0: none), 256-byte aligned, any
+ *                 contents
+ * Every logit is read once; sums are fp32 in a fixed order.
+ * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers (logits: their element size), rows < 0,
+ * vocab outside [1, 2^30], row_stride < vocab (with rows > 1), top_k outside [0, 32], a bad dtype,
+ * outputs or the workspace overlapping an input or each other; MD_ERR_UNSUPPORTED for
+ * rows > 2^22 - 1; MD_ERR_WORKSPACE; MD_ERR_HIP.
+ */
+int md_token_logprobs(int64_t rows, int32_t vocab, int64_t row_stride, int32_t dtype,
+                      const void* logits, const int32_t* tokens, int32_t top_k, float* logprobs,
+                      float* entropy, int32_t* top, float* top_logprobs, void* workspace,
+                      size_t workspace_bytes, void* stream);
+size_t md_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t top_k);
+
+/*
  * ---- Speculative-decoding cost model (Sec. 3.1 Eq. 1-2; Sec. 4.1 Eq. 3-4) ----
  *
  * Host-only arithmetic (no device, no stream), for choosing the speculation

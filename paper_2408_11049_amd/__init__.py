@@ -22,6 +22,10 @@ CPU fallback: if the library is missing, every call raises.
     md_kv4_draft_attn(q, cache, kv_lens, n_sink, window, ...) -> (o, lse)
     md_spec_accept(target_probs, draft_probs, draft, u, ...) -> (accepted, tokens)
     md_qk_norm_rope(q, k_new, pos0, inv_freq, ...) -> (q_out, k_out, lens_out)
+    md_prefix_attn(q, k, v, kv_lens, prefix_k, prefix_v, prefix_lens, ...) -> (o, lse)
+    md_kv_mass(q, k, kv_lens, lse, mass, slot_pos, pos0, ...)  -> mass (in place)
+    md_kv_evict(k, v, mass, slot_pos, kv_lens, seq_lens, budget, ...) -> lens_out
+    md_token_logprobs(logits, tokens, top_k=0, ...) -> (logprobs, entropy, top, top_logprobs)
     md_sd_expected_tokens / md_sd_latency_ratio / md_sd_best_gamma /
     md_sd_alpha_from_omega                        (host-only cost model, Eq. 1-4)
 
@@ -54,6 +58,9 @@ EXPORTED = ["md_verify_attn", "md_draft_attn", "md_draft_attn_indexed", "md_merg
             "md_attn_noalloc", "md_kv4_append", "md_kv4_read", "md_kv4_verify_attn",
             "md_kv4_draft_attn", "md_kv4_workspace_bytes", "md_spec_accept",
             "md_spec_accept_workspace_bytes", "md_qk_norm_rope",
+            "md_prefix_attn", "md_prefix_workspace_bytes", "md_kv_mass",
+            "md_kv_mass_workspace_bytes", "md_kv_evict", "md_kv_evict_workspace_bytes",
+            "md_token_logprobs", "md_token_logprobs_workspace_bytes",
             "md_bench_stream_read", "md_bench_evict", "md_bench_copy", "md_bench_fill",
             "md_bench_attn_stamps"]
 MD_NOALLOC_SCRATCH_BYTES = 33 << 20
@@ -151,6 +158,36 @@ class MdQkNormRopeArgs(ctypes.Structure):
     ]
 
 
+class MdPrefix(ctypes.Structure):
+    """Mirror of ``md_prefix``."""
+    _fields_ = [
+        ("num_prefixes", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("kv_stride_blk", ctypes.c_int64), ("kv_stride_tok", ctypes.c_int64),
+        ("kv_stride_head", ctypes.c_int64),
+        ("page_size", ctypes.c_int32), ("max_pages_per_prefix", ctypes.c_int32),
+        ("num_pages", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+        ("lens", ctypes.c_void_p), ("max_len", ctypes.c_int32),
+    ]
+
+
+class MdKvMassArgs(ctypes.Structure):
+    """Mirror of ``md_kv_mass_args``."""
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("q_len", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("sm_scale", ctypes.c_float),
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+        ("kv_stride_blk", ctypes.c_int64), ("kv_stride_tok", ctypes.c_int64),
+        ("kv_stride_head", ctypes.c_int64),
+        ("page_size", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("num_pages", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+        ("kv_lens", ctypes.c_void_p), ("max_kv_len", ctypes.c_int32),
+        ("lse", ctypes.c_void_p), ("accepted", ctypes.c_void_p), ("pos0", ctypes.c_void_p),
+        ("mass", ctypes.c_void_p), ("slot_pos", ctypes.c_void_p), ("slot_stride", ctypes.c_int64),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -215,6 +252,24 @@ def load_library(path: str = LIB_PATH):
     lib.md_spec_accept_workspace_bytes.restype = sz
     lib.md_qk_norm_rope.argtypes = [ctypes.POINTER(MdQkNormRopeArgs), ctypes.POINTER(MdKvCache), vp]
     lib.md_qk_norm_rope.restype = ctypes.c_int
+    pre_p, mass_p, cache_p = (ctypes.POINTER(MdPrefix), ctypes.POINTER(MdKvMassArgs),
+                              ctypes.POINTER(MdKvCache))
+    lib.md_prefix_attn.argtypes = [args_p, pre_p, vp]
+    lib.md_prefix_attn.restype = ctypes.c_int
+    lib.md_prefix_workspace_bytes.argtypes = [args_p, pre_p]
+    lib.md_prefix_workspace_bytes.restype = sz
+    lib.md_kv_mass.argtypes = [mass_p, vp]
+    lib.md_kv_mass.restype = ctypes.c_int
+    lib.md_kv_mass_workspace_bytes.argtypes = [mass_p]
+    lib.md_kv_mass_workspace_bytes.restype = sz
+    lib.md_kv_evict.argtypes = [cache_p, vp, vp, i64, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+    lib.md_kv_evict.restype = ctypes.c_int
+    lib.md_kv_evict_workspace_bytes.argtypes = [cache_p, i64, i32]
+    lib.md_kv_evict_workspace_bytes.restype = sz
+    lib.md_token_logprobs.argtypes = [i64, i32, i64, i32, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.md_token_logprobs.restype = ctypes.c_int
+    lib.md_token_logprobs_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.md_token_logprobs_workspace_bytes.restype = sz
     f64 = ctypes.c_double
     lib.md_sd_expected_tokens.argtypes = [i32, f64]
     lib.md_sd_expected_tokens.restype = f64
@@ -1205,6 +1260,274 @@ def _row_weight(name, w, d, dtype, gpu):
     return w.data_ptr()
 
 
+def make_prefix(prefix_k, prefix_v, prefix_lens, *, max_prefix_len=None, page_table=None) -> MdPrefix:
+    """Fill md_prefix from tensors (no data is read or moved)."""
+    ks, st = prefix_k.shape, prefix_k.stride()
+    if len(ks) != 4 or prefix_v.shape != ks or prefix_v.stride() != st or st[3] != 1:
+        raise ValueError("prefix_k and prefix_v must be 4-D with equal shapes and strides, head_dim unit-stride")
+    if prefix_v.dtype != prefix_k.dtype:
+        raise ValueError("prefix_k and prefix_v must share a dtype")
+    P = prefix_lens.shape[0]
+    _ints("prefix_lens", prefix_lens, P)
+    gpu = prefix_k.get_device()
+    if gpu < 0 or prefix_v.get_device() != gpu or prefix_lens.get_device() != gpu or (
+            page_table is not None and page_table.get_device() != gpu):
+        _on_gpu(prefix_k, prefix_v=prefix_v, prefix_lens=prefix_lens, prefix_page_table=page_table)
+    if page_table is None:
+        if max_prefix_len is None:
+            max_prefix_len = ks[1]
+        if ks[0] < P or ks[1] < max_prefix_len:
+            raise ValueError("contiguous prefixes must hold max_prefix_len tokens for each of prefix_lens")
+        page, cols, pages, table = 0, 0, 0, None
+    else:
+        if (page_table.dtype != _torch_module.int32 or not page_table.is_contiguous()
+                or page_table.dim() != 2 or page_table.shape[0] < P):
+            raise ValueError("prefix_page_table must be contiguous int32 with a row per prefix")
+        page, cols, pages, table = ks[1], page_table.shape[1], ks[0], page_table.data_ptr()
+        if max_prefix_len is None:
+            max_prefix_len = cols * page
+    return MdPrefix(P, prefix_k.data_ptr(), prefix_v.data_ptr(), st[0], st[1], st[2], page,
+                    _int32("max_pages", cols), pages, table, prefix_lens.data_ptr(),
+                    _int32("max_prefix_len", max_prefix_len))
+
+
+def _prefix_args(q, k, v, kv_lens, prefix_k, prefix_v, prefix_lens, max_kv_len, page_table,
+                 max_prefix_len, prefix_page_table, sm_scale, out, lse, workspace, err_word):
+    if prefix_k.dtype != q.dtype or prefix_k.dim() != 4 or prefix_k.shape[2:] != k.shape[2:]:
+        raise ValueError("the prefix must have the caches' dtype, heads and head_dim")
+    if prefix_k.get_device() != q.get_device():
+        _on_gpu(q, prefix_k=prefix_k)
+    if max_kv_len is not None:
+        max_kv_len = _int32("max_kv_len", max_kv_len)
+    a = make_args(q, k, v, kv_lens, max_kv_len=max_kv_len, page_table=page_table, sm_scale=sm_scale,
+                  out=out, lse=lse, workspace=workspace, err_word=err_word)
+    return a, make_prefix(prefix_k, prefix_v, prefix_lens, max_prefix_len=max_prefix_len,
+                          page_table=prefix_page_table)
+
+
+def md_prefix_workspace_bytes(q, k, v, kv_lens, prefix_k, prefix_v, prefix_lens, *, max_kv_len=None,
+                              page_table=None, max_prefix_len=None, prefix_page_table=None) -> int:
+    """Workspace bytes md_prefix_attn needs for these tensors."""
+    a, p = _prefix_args(q, k, v, kv_lens, prefix_k, prefix_v, prefix_lens, max_kv_len, page_table,
+                        max_prefix_len, prefix_page_table, 0.0, None, None, None, None)
+    return int(load_library().md_prefix_workspace_bytes(ctypes.byref(a), ctypes.byref(p)))
+
+
+@_device_scoped
+def md_prefix_attn(q, k, v, kv_lens, prefix_k, prefix_v, prefix_lens, *, max_kv_len=None,
+                   page_table=None, max_prefix_len=None, prefix_page_table=None, sm_scale=0.0,
+                   out=None, lse=None, return_lse=True, workspace=None, stream=None, err_word=None):
+    """md_verify_attn for sequences that share prefixes: sequence b of B sees prefix b // (B / P)
+    of the P in prefix_k, prefix_v (contiguous [P, T_alloc, Hkv, d], or paged with
+    prefix_page_table [P, max_pages]; prefix_lens [P] int32 tokens each), then its own cache, whose
+    kv_lens count own tokens only (see include/magicdec.h)."""
+    torch = _torch_module
+    lib = load_library()
+    a, p = _prefix_args(q, k, v, kv_lens, prefix_k, prefix_v, prefix_lens, max_kv_len, page_table,
+                        max_prefix_len, prefix_page_table, sm_scale, out, lse, workspace, err_word)
+    if out is None:
+        out = torch.empty_like(q)
+        a.o = out.data_ptr()
+    if lse is None and return_lse:
+        lse = q.new_empty(q.shape[:3], dtype=torch.float32)
+        a.lse = lse.data_ptr()
+    ra, rp = ctypes.byref(a), ctypes.byref(p)
+    if workspace is None:
+        need = lib.md_prefix_workspace_bytes(ra, rp)
+        if need:
+            workspace = q.new_empty((need,), dtype=torch.uint8)
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), need
+    st = lib.md_prefix_attn(ra, rp, _raw_stream(q.get_device(), stream))
+    if st:
+        _check(st)
+    return out, lse
+
+
+def _slots(mass, slot_pos, B, heads):
+    """The slot stride of mass and slot_pos [B, Hkv, slots]."""
+    torch = _torch_module or _torch()
+    shape = mass.shape
+    if (len(shape) != 3 or shape[0] < B or shape[1] != heads or slot_pos.shape != shape
+            or mass.dtype != torch.float32 or slot_pos.dtype != torch.int32
+            or not mass.is_contiguous() or not slot_pos.is_contiguous()):
+        raise ValueError("mass and slot_pos must be contiguous float32 and int32 [B, Hkv, slots]")
+    return shape[2]
+
+
+@_device_scoped
+def md_kv_mass(q, k, kv_lens, lse, mass, slot_pos, pos0, *, accepted=None, max_kv_len=None,
+               page_table=None, sm_scale=0.0, workspace=None, stream=None):
+    """Adds to mass [B, Hkv, slots] float32 (in place) the softmax weights that the queries q
+    [B, L, Hq, d] give each token of the cache, by the attention's lse [B, L, Hq]; the L newest
+    tokens' entries are set, and so are their positions pos0[b] + i in slot_pos [B, Hkv, slots]
+    int32.  With accepted [B] int32 only rows i <= accepted[b] count.  Returns mass."""
+    torch = _torch_module
+    lib = load_library()
+    qs, ks, st = q.shape, k.shape, k.stride()
+    if len(qs) != 4 or len(ks) != 4 or not q.is_contiguous() or st[3] != 1:
+        raise ValueError("q must be contiguous [B, L, Hq, d]; k 4-D, head_dim unit-stride")
+    B, L, Hq, d = qs
+    if ks[3] != d or k.dtype != q.dtype:
+        raise ValueError("k must have q's head_dim and dtype")
+    gpu = q.get_device()
+    for t in (k, kv_lens, lse, mass, slot_pos, pos0, accepted, page_table, workspace):
+        if t is not None and t.get_device() != gpu:
+            _on_gpu(q, k=k, kv_lens=kv_lens, lse=lse, mass=mass, slot_pos=slot_pos, pos0=pos0,
+                    accepted=accepted, page_table=page_table, workspace=workspace)
+    _ints("kv_lens", kv_lens, B)
+    _ints("pos0", pos0, B)
+    if accepted is not None:
+        _ints("accepted", accepted, B)
+    if lse.shape != qs[:3] or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous float32 [B, L, Hq]")
+    slots = _slots(mass, slot_pos, B, ks[2])
+    if page_table is None:
+        page = cols = pages = 0
+        table = None
+        if max_kv_len is None:
+            max_kv_len = min(ks[1], slots)
+        if B > 0 and (ks[0] < B or ks[1] < max_kv_len):
+            raise ValueError("a contiguous k must hold max_kv_len tokens of B sequences")
+    else:
+        if (page_table.dtype != torch.int32 or not page_table.is_contiguous()
+                or page_table.dim() != 2 or page_table.shape[0] < B):
+            raise ValueError("page_table must be contiguous int32 [B, max_pages]")
+        page, cols, pages, table = ks[1], page_table.shape[1], ks[0], page_table.data_ptr()
+        if max_kv_len is None:
+            max_kv_len = min(cols * page, slots)
+    a = MdKvMassArgs(B, L, Hq, ks[2], d, _code(q), sm_scale, q.data_ptr(), k.data_ptr(), st[0], st[1],
+                     st[2], page, _int32("max_pages", cols), pages, table, kv_lens.data_ptr(),
+                     _int32("max_kv_len", max_kv_len), lse.data_ptr(),
+                     None if accepted is None else accepted.data_ptr(), pos0.data_ptr(),
+                     mass.data_ptr(), slot_pos.data_ptr(), slots, None, 0)
+    ref = ctypes.byref(a)
+    if workspace is None:
+        need = lib.md_kv_mass_workspace_bytes(ref)
+        if need:
+            workspace = q.new_empty((need,), dtype=torch.uint8)
+    if workspace is not None:
+        a.workspace = workspace.data_ptr()
+        a.workspace_bytes = workspace.numel() * workspace.element_size()
+    rc = lib.md_kv_mass(ref, _raw_stream(gpu, stream))
+    if rc:
+        _check(rc)
+    return mass
+
+
+@_device_scoped
+def md_kv_evict(k, v, mass, slot_pos, kv_lens, seq_lens, budget, *, n_sink=0, recent=0,
+                page_table=None, lens_out=None, workspace=None, stream=None):
+    """Cuts every (sequence, KV head) of the cache k, v to `budget` tokens, in place: those of
+    least mass [B, Hkv, slots] go, except slot_pos < n_sink and slot_pos >= seq_lens[b] - recent; kept
+    tokens behind the budget move into the freed slots, with their mass and slot_pos.  kv_lens [B] int32
+    counts what each cache holds, seq_lens [B] int32 the sequence's tokens, evicted ones included.
+    Returns lens_out [B] int32 = min(kv_lens, budget) (not kv_lens itself)."""
+    torch = _torch_module
+    lib = load_library()
+    B = kv_lens.shape[0]
+    c = make_kv_cache(k, v, num_seqs=B, page_table=page_table)
+    gpu = k.get_device()
+    for t in (v, mass, slot_pos, kv_lens, seq_lens, page_table, lens_out, workspace):
+        if t is not None and t.get_device() != gpu:
+            _on_gpu(k, v=v, mass=mass, slot_pos=slot_pos, kv_lens=kv_lens, seq_lens=seq_lens,
+                    page_table=page_table, lens_out=lens_out, workspace=workspace)
+    _ints("kv_lens", kv_lens, B)
+    _ints("seq_lens", seq_lens, B)
+    slots = _slots(mass, slot_pos, B, c.num_kv_heads)
+    if lens_out is None:
+        lens_out = kv_lens.new_empty((B,))
+    else:
+        _ints("lens_out", lens_out, B)
+    budget, ref = _int32("budget", budget), ctypes.byref(c)
+    if workspace is None:
+        need = lib.md_kv_evict_workspace_bytes(ref, slots, budget)
+        workspace = k.new_empty((need,), dtype=torch.uint8) if need else None
+    rc = lib.md_kv_evict(ref, mass.data_ptr(), slot_pos.data_ptr(), slots, kv_lens.data_ptr(),
+                         seq_lens.data_ptr(), budget, _int32("n_sink", n_sink),
+                         _int32("recent", recent), lens_out.data_ptr(),
+                         None if workspace is None else workspace.data_ptr(),
+                         0 if workspace is None else workspace.numel() * workspace.element_size(),
+                         _raw_stream(gpu, stream))
+    if rc:
+        _check(rc)
+    return lens_out
+
+
+def _flat_rows(t):
+    """(rows, element stride of a row) of t [..., vocab], the rows in order at one stride."""
+    shape, st = t.shape, t.stride()
+    if len(shape) < 1 or (shape[-1] > 1 and st[-1] != 1):
+        raise ValueError("logits must be [..., vocab] with unit-stride tokens")
+    rows, stride = 1, None
+    for n, x in zip(reversed(shape[:-1]), reversed(st[:-1])):
+        if n == 0:
+            return 0, shape[-1]
+        if n > 1:
+            if stride is None:
+                stride = x
+            elif x != stride * rows:
+                raise ValueError("the rows of logits must lie at one stride")
+            rows *= n
+    return rows, shape[-1] if stride is None else stride
+
+
+@_device_scoped
+def md_token_logprobs(logits, tokens=None, *, top_k=0, with_entropy=True, logprobs=None, entropy=None,
+                      top=None, top_logprobs=None, workspace=None, stream=None):
+    """Of every row of logits [..., vocab] (float32/bfloat16): the log probability of tokens [...]
+    int32 (0 where negative), the entropy, and the top_k most likely tokens with theirs.  Returns
+    (logprobs [...], entropy [...], top [..., top_k] int32, top_logprobs [..., top_k]); None
+    without tokens or with_entropy (see include/magicdec.h)."""
+    torch = _torch_module
+    lib = load_library()
+    rows, stride = _flat_rows(logits)
+    lead, vocab = logits.shape[:-1], logits.shape[-1]
+    gpu = logits.get_device()
+    if tokens is not None:
+        if tokens.shape != lead or tokens.dtype != torch.int32 or not tokens.is_contiguous():
+            raise ValueError("tokens must be contiguous int32, one a row of logits")
+        if tokens.get_device() != gpu:
+            _on_gpu(logits, tokens=tokens)
+    elif logprobs is not None:
+        raise ValueError("logprobs without tokens")
+    top_k = _int32("top_k", top_k)
+    wide = lead + (max(top_k, 0),)
+    if not (logprobs is None and entropy is None and top is None and top_logprobs is None
+            and workspace is None):
+        _on_gpu(logits, logprobs=logprobs, entropy=entropy, top=top, top_logprobs=top_logprobs,
+                workspace=workspace)
+        for name, t, shape, dt in (("logprobs", logprobs, lead, torch.float32),
+                                   ("entropy", entropy, lead, torch.float32),
+                                   ("top", top, wide, torch.int32),
+                                   ("top_logprobs", top_logprobs, wide, torch.float32)):
+            if t is not None and (t.shape != shape or t.dtype != dt or not t.is_contiguous()):
+                raise ValueError(f"{name} must be contiguous {dt} {tuple(shape)}")
+    if logprobs is None and tokens is not None:
+        logprobs = logits.new_empty(lead, dtype=torch.float32)
+    if entropy is None and with_entropy:
+        entropy = logits.new_empty(lead, dtype=torch.float32)
+    if top is None:
+        top = logits.new_empty(wide, dtype=torch.int32)
+    if top_logprobs is None:
+        top_logprobs = logits.new_empty(wide, dtype=torch.float32)
+    vocab32 = _int32("vocab", vocab)
+    if workspace is None:
+        need = lib.md_token_logprobs_workspace_bytes(rows, vocab32, top_k)
+        workspace = logits.new_empty((need,), dtype=torch.uint8) if need else None
+    rc = lib.md_token_logprobs(
+        rows, vocab32, stride, _code(logits), logits.data_ptr(),
+        None if tokens is None else tokens.data_ptr(), top_k,
+        None if logprobs is None else logprobs.data_ptr(),
+        None if entropy is None else entropy.data_ptr(),
+        top.data_ptr() if top_k > 0 else None, top_logprobs.data_ptr() if top_k > 0 else None,
+        None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _raw_stream(gpu, stream))
+    if rc:
+        _check(rc)
+    return logprobs, entropy, top, top_logprobs
+
+
 def md_sd_expected_tokens(gamma: int, alpha: float) -> float:
     """Eq. 1: expected tokens per verification (NaN for invalid arguments)."""
     return load_library().md_sd_expected_tokens(int(gamma), float(alpha))
@@ -1251,3 +1574,7 @@ kv4_verify_attn = md_kv4_verify_attn
 kv4_draft_attn = md_kv4_draft_attn
 spec_accept = md_spec_accept
 qk_norm_rope = md_qk_norm_rope
+prefix_attn = md_prefix_attn
+kv_mass = md_kv_mass
+kv_evict = md_kv_evict
+token_logprobs = md_token_logprobs

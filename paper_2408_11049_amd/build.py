@@ -18,7 +18,8 @@ ARCH = "gfx950"
 
 SOURCES = ["api.cpp", "plan.cpp", "costmodel.cpp", "attn.hip", "attn_agpr.hip", "merge.hip",
            "snapkv.hip", "step.hip", "bench.hip", "noalloc.hip", "plan_ops.cpp", "api_ops.cpp",
-           "kv4.hip", "kv4_attn.hip", "spec.hip", "norm_rope.hip"]
+           "kv4.hip", "kv4_attn.hip", "spec.hip", "norm_rope.hip", "plan_answers.cpp",
+           "api_answers.cpp", "prefix_attn.hip", "kv_mass.hip", "kv_evict.hip", "logprobs.hip"]
 
 
 def hipcc() -> str:

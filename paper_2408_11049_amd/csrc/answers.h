@@ -1,0 +1,74 @@
+// answers.h -- host-side checks and plans of the operators for several answers of one
+// prompt: attention over a shared prefix, eviction by accumulated weight, token log
+// probabilities.  No HIP types, so they compile and run without a GPU.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "internal.h"
+#include "magicdec.h"
+#include "ops.h"
+
+namespace md {
+
+// Shared-prefix attention: query rows and keys of a workgroup's tile.
+constexpr int kPrefixRows = 128;
+constexpr int kPrefixTile(bool bf16) { return bf16 ? 64 : 32; }
+struct PrefixPlan {
+  int32_t group_rows = 0;   // rows of a (prefix, KV head): B / P * L * G
+  int32_t row_blocks = 0;   // of kPrefixRows
+  int32_t c_pre = 0, c_own = 0;  // parts of the prefix's and of the own keys
+  int32_t n_pre = 0;        // workgroups of the prefix, padded to whole rounds of the XCDs
+  int64_t n_wgs = 0;
+  int64_t n_rows = 0;       // B * L * Hq
+  size_t part_o_bytes = 0, part_lse_bytes = 0, workspace_bytes = 0;
+};
+// Sizes alone: MD_OK, MD_ERR_INVALID_ARG or MD_ERR_UNSUPPORTED.
+int check_prefix_sizes(const md_attn_args* a, const md_prefix* p);
+PrefixPlan make_prefix_plan(const md_attn_args* a, const md_prefix* p, int num_cus);
+size_t prefix_workspace_need(const md_attn_args* a, const md_prefix* p, int num_cus);
+int validate_prefix(const md_attn_args* a, const md_prefix* p, PrefixPlan* plan);
+
+// Accumulated weights: keys of a workgroup, rows of a tile.
+struct MassPlan {
+  int32_t keys = 0;         // keys of a workgroup
+  int32_t key_blocks = 0;   // of the longest sequence
+  int32_t row_parts = 1;    // parts of the rows; the workspace holds each part's weights
+  int64_t n_wgs = 0;
+  size_t workspace_bytes = 0;
+};
+int check_mass_sizes(const md_kv_mass_args* a);
+MassPlan make_mass_plan(const md_kv_mass_args* a, int num_cus);
+int validate_mass(const md_kv_mass_args* a, MassPlan* plan);
+
+// Eviction: the most rows that any (sequence, KV head) moves; up to kEvictFused of them the
+// workgroup that selects moves them, more are a launch of their own, listed in the workspace.
+constexpr int kEvictFused = 512;
+struct EvictPlan {
+  int64_t slots = 0;        // tokens a sequence can hold
+  int32_t max_moves = 0;
+  size_t workspace_bytes = 0;  // [units] counts, then [units][max_moves] (to, from)
+};
+EvictPlan make_evict_plan(const md_kv_cache* c, int64_t slot_stride, int32_t budget);
+int check_evict_sizes(const md_kv_cache* c, int64_t slot_stride, int32_t budget);
+int validate_evict(const md_kv_cache* c, const void* mass, const void* slot_pos,
+                   int64_t slot_stride, const void* lens, const void* seq_lens, int32_t budget,
+                   int32_t n_sink, int32_t recent, const void* lens_out, const void* workspace,
+                   size_t workspace_bytes, EvictPlan* plan);
+
+// Log probabilities: rows in segments, a workgroup each.
+constexpr int kLogpMaxTop = 32;
+struct LogpPlan {
+  int32_t per_lane = 0;     // logits a lane holds at once
+  int32_t seg_len = 0, n_segs = 0;
+  size_t stats_bytes = 0, cand_bytes = 0, workspace_bytes = 0;
+};
+int check_logp_sizes(int64_t rows, int32_t vocab, int64_t row_stride, int32_t dtype, int32_t top_k);
+LogpPlan make_logp_plan(int64_t rows, int32_t vocab, int32_t top_k, int num_cus);
+int validate_logp(int64_t rows, int32_t vocab, int64_t row_stride, int32_t dtype,
+                  const void* logits, const void* tokens, int32_t top_k, const void* logprobs,
+                  const void* entropy, const void* top, const void* top_logprobs,
+                  const void* workspace, size_t workspace_bytes, LogpPlan* plan);
+
+}  // namespace md

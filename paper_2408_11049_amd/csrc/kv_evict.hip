@@ -1,0 +1,208 @@
+// kv_evict.hip -- a cache cut down to its budget by accumulated weight: per (sequence, KV
+// head) the n - budget tokens of least weight go, and the tokens kept behind the budget move
+// into the slots that this frees.
+//
+// One workgroup a (sequence, KV head) finds the key of rank n - budget by a radix select (four
+// rounds of 8 bits over weights that stay in the caches), counts in slot order and lists
+// (freed slot, kept slot) pairs; pairs are moved by the same workgroup or, where a call may have
+// more than kEvictFused of them a head, by a second launch over the whole device.
+#include "answers_kernels.h"
+
+namespace md {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+namespace {
+
+constexpr uint32_t kHeld = 0xffffffffu;  // sinks and recent tokens: above every weight
+
+struct EvictUnit {
+  const float* mass;
+  const int32_t* pos;
+  int32_t n_sink;
+  int64_t recent_from;
+};
+
+// The order of a slot's token: its weight's, NaN least, held tokens last.
+__device__ __forceinline__ uint32_t order_key(const EvictUnit& u, int j) {
+  const int pos = u.pos[j];
+  const float w = u.mass[j] + 0.f;  // -0 and 0 are equal
+  if (pos < u.n_sink || pos >= u.recent_from) return kHeld;
+  const uint32_t x = __float_as_uint(w);
+  if (w != w) return 0u;
+  return (x >> 31) ? ~x : x | 0x80000000u;
+}
+
+// Byte offset of a token's row of head hk, or -1: on no page of the pool.
+__device__ __forceinline__ int64_t row_offset(const EvictParams& p, int b, int hk, int j) {
+  int64_t off;
+  if (p.paged) {
+    const int pid = p.c.page_table[static_cast<int64_t>(b) * p.c.max_pages + (j >> p.c.page_shift)];
+    if (pid < 0 || pid >= p.c.num_pages) return -1;
+    off = static_cast<int64_t>(pid) * p.c.s_blk +
+          static_cast<int64_t>(j & ((1 << p.c.page_shift) - 1)) * p.c.s_tok;
+  } else {
+    off = static_cast<int64_t>(b) * p.c.s_blk + static_cast<int64_t>(j) * p.c.s_tok;
+  }
+  return (off + static_cast<int64_t>(hk) * p.c.s_head) * p.esize;
+}
+
+// One 16-byte vector of a pair's K or V row (item: pair, then K or V, then the vector); the first of
+// a pair moves its mass and position.
+__device__ __forceinline__ void move_vector(const EvictParams& p, int unit, int2 pair, int vec) {
+  const int b = unit / p.Hkv, hk = unit % p.Hkv;
+  const int64_t to = row_offset(p, b, hk, pair.x), from = row_offset(p, b, hk, pair.y);
+  if (to >= 0 && from >= 0) {
+    unsigned char* const base = vec < p.row_vecs ? p.c.k : p.c.v;
+    const int at = (vec < p.row_vecs ? vec : vec - p.row_vecs) * 16;
+    *reinterpret_cast<u32x4*>(base + to + at) = *reinterpret_cast<const u32x4*>(base + from + at);
+  }
+  if (vec == 0) {
+    const int64_t s = static_cast<int64_t>(unit) * p.slot_stride;
+    p.mass[s + pair.x] = p.mass[s + pair.y];
+    p.slot_pos[s + pair.x] = p.slot_pos[s + pair.y];
+  }
+}
+
+template <int NT>
+__global__ void __launch_bounds__(NT)
+evict_select(const EvictParams p) {
+  constexpr int NW = NT / 64;
+  __shared__ uint32_t hist[256];
+  __shared__ int counts[3][NW];
+  __shared__ uint32_t pick[2];
+  __shared__ int2 listed[kEvictFused];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int unit = blockIdx.x, b = unit / p.Hkv;
+  const int n = min(max(p.lens[b], 0), p.slots);
+  if (p.lens_out && unit % p.Hkv == 0 && tid == 0) p.lens_out[b] = min(n, p.budget);
+  if (n <= p.budget) {
+    if (p.counts && tid == 0) p.counts[unit] = 0;
+    return;
+  }
+  const int64_t s0 = static_cast<int64_t>(unit) * p.slot_stride;
+  const EvictUnit u = {p.mass + s0, p.slot_pos + s0, p.n_sink,
+                       static_cast<int64_t>(p.seq_lens[b]) - p.recent};
+
+  // The key of rank n - budget (from 1), eight bits a round: of the keys that agree with `prefix`
+  // in the bits above, `want` is the rank looked for.
+  uint32_t prefix = 0;
+  int want = n - p.budget;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += NT) hist[i] = 0;
+    __syncthreads();
+    for (int j = tid; j < n; j += NT) {
+      const uint32_t key = order_key(u, j);
+      if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8)))
+        atomicAdd(&hist[(key >> shift) & 255u], 1u);
+    }
+    __syncthreads();
+    if (wave == 0) {  // each lane four bins; the bin in which the running count reaches `want`
+      uint32_t h[4], mine = 0;
+      for (int i = 0; i < 4; ++i) mine += h[i] = hist[lane * 4 + i];
+      uint32_t incl = mine;
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t x = __shfl_up(incl, o);
+        if (lane >= o) incl += x;
+      }
+      uint32_t run = incl - mine;
+      for (int i = 0; i < 4; ++i) {
+        if (run < static_cast<uint32_t>(want) && static_cast<uint32_t>(want) <= run + h[i]) {
+          pick[0] = lane * 4 + i;
+          pick[1] = want - run;
+        }
+        run += h[i];
+      }
+    }
+    __syncthreads();
+    prefix |= pick[0] << shift;
+    want = static_cast<int>(pick[1]);
+    __syncthreads();
+  }
+  // Evicted: keys below `prefix`, and the first `want` slots whose key is `prefix`.
+
+  // Each wave takes a run of slots; what comes before it is counted first.
+  const int per = (n + NW - 1) / NW, lo = min(n, wave * per), hi = min(n, lo + per);
+  int ties = 0;
+  for (int j0 = lo; j0 < hi; j0 += 64) {
+    const int j = j0 + lane;
+    ties += __popcll(__ballot(j < hi && order_key(u, j) == prefix));
+  }
+  if (lane == 0) counts[0][wave] = ties;
+  __syncthreads();
+  int tie0 = 0;
+  for (int x = 0; x < wave; ++x) tie0 += counts[0][x];
+  const unsigned long long below = (1ull << lane) - 1;
+  // Calls f(j, freed, moved, rank of its kind within this wave) over the wave's slots.
+  auto scan = [&](auto f) {
+    int tie = tie0, holes = 0, extras = 0;
+    for (int j0 = lo; j0 < hi; j0 += 64) {
+      const int j = j0 + lane;
+      const uint32_t key = j < hi ? order_key(u, j) : kHeld;
+      const unsigned long long eq = __ballot(j < hi && key == prefix);
+      const bool out = j < hi && (key < prefix || (key == prefix && tie + __popcll(eq & below) < want));
+      tie += __popcll(eq);
+      const bool hole = out && j < p.budget, extra = j < hi && !out && j >= p.budget;
+      const unsigned long long hm = __ballot(hole), em = __ballot(extra);
+      f(j, hole, extra, hole ? holes + __popcll(hm & below) : extras + __popcll(em & below));
+      holes += __popcll(hm);
+      extras += __popcll(em);
+    }
+    return make_int2(holes, extras);
+  };
+  const int2 mine = scan([](int, bool, bool, int) {});
+  if (lane == 0) {
+    counts[1][wave] = mine.x;
+    counts[2][wave] = mine.y;
+  }
+  __syncthreads();
+  int hole0 = 0, extra0 = 0, total = 0;
+  for (int x = 0; x < NW; ++x) {
+    if (x < wave) {
+      hole0 += counts[1][x];
+      extra0 += counts[2][x];
+    }
+    total += counts[1][x];
+  }
+  // As many slots are freed below the budget as tokens are kept behind it.
+  int2* const pairs = p.counts ? p.moves + static_cast<int64_t>(unit) * p.max_moves : listed;
+  scan([&](int j, bool hole, bool extra, int rank) {
+    if (hole) pairs[hole0 + rank].x = j;
+    if (extra) pairs[extra0 + rank].y = j;
+  });
+  if (p.counts) {
+    if (tid == 0) p.counts[unit] = total;
+    return;
+  }
+  __syncthreads();
+  const int vecs = 2 * p.row_vecs;
+  for (int x = tid; x < total * vecs; x += NT) move_vector(p, unit, listed[x / vecs], x % vecs);
+}
+
+// Workgroups (unit, y): each takes every gridDim.y-th run of 256 vectors of the unit's pairs.
+__global__ void __launch_bounds__(256)
+evict_move(const EvictParams p) {
+  const int unit = blockIdx.x, vecs = 2 * p.row_vecs;
+  const int64_t total = static_cast<int64_t>(p.counts[unit]) * vecs;
+  const int2* const pairs = p.moves + static_cast<int64_t>(unit) * p.max_moves;
+  const int64_t step = static_cast<int64_t>(gridDim.y) * 256;
+  for (int64_t x = static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x; x < total; x += step)
+    move_vector(p, unit, pairs[x / vecs], static_cast<int>(x % vecs));
+}
+
+}  // namespace
+
+hipError_t launch_kv_evict(const EvictParams& p, hipStream_t s) {
+  const uint32_t units = static_cast<uint32_t>(p.B) * static_cast<uint32_t>(p.Hkv);
+  if (p.slots <= 4096)
+    hipLaunchKernelGGL((evict_select<256>), dim3(units), dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL((evict_select<1024>), dim3(units), dim3(1024), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.counts) return e;
+  const uint32_t y = units >= 2048 ? 1 : (2048 + units - 1) / units;
+  hipLaunchKernelGGL(evict_move, dim3(units, y), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace md

@@ -1,0 +1,407 @@
+// logprobs.hip -- per row of logits: the log probability of a given token, the entropy and
+// the top_k most likely tokens, from one pass over the row.
+//
+// A workgroup takes a segment of a row, 256 lanes holding 16 or 64 logits each in
+// registers at a time.  Sums: each lane keeps a maximum m, z = sum exp(x - m) and
+// t = sum exp(x - m) (x - m); lse = m + ln z, entropy = ln z - t / z.  Differences to the maximum
+// are taken before the scaling to log2, so that large logits lose nothing.
+// Top tokens: the top_k-th largest of a wave's 64 lane maxima is below no more than top_k of its
+// logits, so only logits from there on are candidates, hardly more than top_k of them; they go to
+// a list in LDS, which is cut to its best top_k where it would overflow (rows of equal
+// or clustered values).  Candidates are ranked by counting the better ones.
+// Rows of several segments are joined by a second launch.
+#include <float.h>
+
+#include "answers_kernels.h"
+
+namespace md {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr int kList = 256;  // candidates a wave lists
+
+// Larger value first, then the lower index.  Values are no NaN.
+__device__ __forceinline__ bool better(float v, int i, float w, int j) {
+  return v > w || (v == w && i < j);
+}
+
+struct Stats {
+  float m, z, t;
+};
+// Of two disjoint sets of logits.  An empty set is (-inf, 0, 0).
+__device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
+  const float m = fmaxf(a.m, b.m);
+  if (m == -INFINITY) return Stats{m, a.z + b.z, a.t + b.t};  // nothing, or NaN
+  // A set far below the other has weight 0; its distance must stay finite times z.
+  const float da = a.m == -INFINITY ? 0.f : fmaxf(a.m - m, -1e20f);
+  const float db = b.m == -INFINITY ? 0.f : fmaxf(b.m - m, -1e20f);
+  const float fa = a.m == -INFINITY && a.z == 0.f ? 0.f : __builtin_amdgcn_exp2f(da * kLog2e);
+  const float fb = b.m == -INFINITY && b.z == 0.f ? 0.f : __builtin_amdgcn_exp2f(db * kLog2e);
+  // exp(x - m) (x - m) = f exp(x - a.m) ((x - a.m) + da)
+  return Stats{m, a.z * fa + b.z * fb, fa * (a.t + a.z * da) + fb * (b.t + b.z * db)};
+}
+__device__ __forceinline__ Stats wave_join(Stats s) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1)
+    s = join(s, Stats{__shfl_xor(s.m, o), __shfl_xor(s.z, o), __shfl_xor(s.t, o)});
+  return s;
+}
+
+struct Finals {
+  float lse, entropy;
+};
+// A row of nothing but -inf has lse -inf and entropy 0; a NaN or +inf makes both NaN.
+__device__ __forceinline__ Finals finals(const Stats& s) {
+  if (s.z != s.z) return Finals{s.z, s.z};
+  if (s.m == -INFINITY) return Finals{-INFINITY, 0.f};
+  const float lz = __builtin_amdgcn_logf(s.z) * kLn2;
+  return Finals{s.m + lz, lz - s.t / s.z};
+}
+// x - lse of a logit: -inf for a masked one, whatever the row.
+__device__ __forceinline__ float log_prob(float x, float lse) {
+  if (lse != lse) return lse;
+  return x == -INFINITY ? -INFINITY : x - lse;
+}
+
+template <bool BF16>
+__device__ __forceinline__ float logit(const void* base, int64_t e) {
+  if constexpr (BF16)
+    return __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(base)[e]) << 16);
+  return static_cast<const float*>(base)[e];
+}
+
+// The list of one wave, cut to its best top_k in order (best first); returns how many remain.
+// `n` entries; rank by counting.  All lanes of the wave take part.
+__device__ __forceinline__ int cut_list(float* val, int* idx, int n, int top_k, int lane) {
+  float v[kList / 64];
+  int i[kList / 64], rank[kList / 64];
+#pragma unroll
+  for (int x = 0; x < kList / 64; ++x) {
+    const int e = x * 64 + lane;
+    v[x] = e < n ? val[e] : 0.f;
+    i[x] = e < n ? idx[e] : 0;
+    rank[x] = e < n ? 0 : kList;
+  }
+  for (int e = 0; e < n; ++e) {
+    const float w = val[e];
+    const int j = idx[e];
+#pragma unroll
+    for (int x = 0; x < kList / 64; ++x) rank[x] += better(w, j, v[x], i[x]);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int x = 0; x < kList / 64; ++x)
+    if (rank[x] < top_k) {
+      val[rank[x]] = v[x];
+      idx[rank[x]] = i[x];
+    }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  return min(n, top_k);
+}
+
+// A wave's list of candidates and what a logit has to beat to enter it.
+struct List {
+  float* val;
+  int* idx;
+  int n;           // the same in all lanes
+  float floor_v;   // enters: better than (floor_v, floor_i)
+  int floor_i;
+};
+// Adds the (v, i) of the lanes in m.
+__device__ __forceinline__ void append(List& l, unsigned long long m, float v, int i, int lane) {
+  if ((m >> lane) & 1ull) {
+    const int at = l.n + __popcll(m & ((1ull << lane) - 1));
+    l.val[at] = v;
+    l.idx[at] = i;
+  }
+  l.n += __popcll(m);
+}
+// The same where `in`, cutting a list that is full.
+__device__ __forceinline__ void push(List& l, bool in, float v, int i, int top_k, int lane) {
+  unsigned long long m = __ballot(in);
+  if (l.n + __popcll(m) > kList) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    l.n = cut_list(l.val, l.idx, l.n, top_k, lane);
+    l.floor_v = l.val[top_k - 1];  // kList > 2 * kLogpMaxTop: the list held more than top_k
+    l.floor_i = l.idx[top_k - 1];
+    in = in && better(v, i, l.floor_v, l.floor_i);
+    m = __ballot(in);
+  }
+  append(l, m, v, i, lane);
+}
+
+// The best top_k of four waves' lists, by the whole workgroup: each thread takes one entry in
+// turn and counts the better ones.  f(rank, value, index) for each of the best.
+template <typename F>
+__device__ __forceinline__ void best_of(const float (&val)[4][kList], const int (&idx)[4][kList],
+                                        const int (&n)[4], int top_k, F f) {
+  const int total = n[0] + n[1] + n[2] + n[3];
+  for (int e0 = threadIdx.x; e0 < total; e0 += 256) {
+    int w = 0, e = e0;
+    while (e >= n[w]) e -= n[w++];
+    const float v = val[w][e];
+    const int i = idx[w][e];
+    int rank = 0;
+    for (int x = 0; x < 4; ++x)
+      for (int y = 0; y < n[x]; ++y) rank += better(val[x][y], idx[x][y], v, i);
+    if (rank < top_k) f(rank, v, i);
+  }
+}
+
+// PL logits a lane at a time.
+template <bool BF16, int PL>
+__global__ void __launch_bounds__(256)
+logprobs_kernel(const LogpParams p) {
+  constexpr int VN = BF16 ? 8 : 4, NV = PL / VN;  // logits of a 16-byte vector, vectors a lane
+  __shared__ float l_val[4][kList];
+  __shared__ int l_idx[4][kList];
+  __shared__ int l_n[4];
+  __shared__ Stats l_stats[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row = static_cast<int>(blockIdx.x) / p.n_segs, seg = static_cast<int>(blockIdx.x) % p.n_segs;
+  const int64_t row0 = row * p.row_stride;
+  const int seg0 = seg * p.seg_len, seg1 = static_cast<int>(min(static_cast<int64_t>(p.vocab),
+                                                                 static_cast<int64_t>(seg0) + p.seg_len));
+  const int K = p.top_k;
+  float x_tok = 0.f;
+  int tok = -1;
+  if (p.n_segs == 1 && p.tokens && tid == 0) {
+    tok = p.tokens[row];
+    if (tok >= 0 && tok < p.vocab) x_tok = logit<BF16>(p.logits, row0 + tok);
+  }
+
+  Stats st = {-INFINITY, 0.f, 0.f};
+  List list = {l_val[wave], l_idx[wave], 0, -INFINITY, INT32_MAX};
+  // Element j of vector v of this lane.
+  auto at = [&](int wave0, int v, int j) { return wave0 + v * 64 * VN + lane * VN + j; };
+  for (int c0 = seg0; c0 < seg1; c0 += 256 * PL) {
+    float x[PL];
+    const int wave0 = c0 + wave * PL * 64;
+    if (wave0 + PL * 64 <= seg1) {
+      u32x4 raw[NV];
+      // Rows begin where the vocabulary puts them: any element's address will do for a load.
+      typedef u32x4 at2 __attribute__((aligned(2)));
+      typedef u32x4 at4 __attribute__((aligned(4)));
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int64_t e = row0 + at(wave0, v, 0);
+        if constexpr (BF16)
+          raw[v] = __builtin_nontemporal_load(
+              reinterpret_cast<const at2*>(static_cast<const uint16_t*>(p.logits) + e));
+        else
+          raw[v] = __builtin_nontemporal_load(
+              reinterpret_cast<const at4*>(static_cast<const float*>(p.logits) + e));
+      }
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (BF16) {
+            x[v * 8 + 2 * j] = __uint_as_float(raw[v][j] << 16);
+            x[v * 8 + 2 * j + 1] = __uint_as_float(raw[v][j] & 0xffff0000u);
+          } else {
+            x[v * 4 + j] = __uint_as_float(raw[v][j]);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < VN; ++j) {
+          const int i = at(wave0, v, j);
+          x[v * VN + j] = i < seg1 ? logit<BF16>(p.logits, row0 + i) : -INFINITY;
+        }
+    }
+
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < PL; ++e) mx = fmaxf(mx, x[e]);
+    {
+      const float m = fmaxf(st.m, mx), m_use = m == -INFINITY ? 0.f : m;
+      float z[4] = {}, t[4] = {};
+#pragma unroll
+      for (int e = 0; e < PL; ++e) {
+        const float d = x[e] - m_use;
+        const float w = __builtin_amdgcn_exp2f(d * kLog2e);
+        z[e & 3] += w;
+        t[e & 3] = __builtin_fmaf(w, fmaxf(d, -1e30f), t[e & 3]);  // 0 * -inf is no term
+      }
+      st = join(st, Stats{mx, (z[0] + z[1]) + (z[2] + z[3]), (t[0] + t[1]) + (t[2] + t[3])});
+    }
+
+    if (K > 0) {
+      // The K-th largest lane maximum, in the upper 16 bits of its order (rounded down, which a lower
+      // bound may be): bit by bit, whether K lanes still reach it.
+      const uint32_t mb = __float_as_uint(mx);
+      const uint32_t key = (mb >> 31) ? ~mb : mb | 0x80000000u;
+      uint32_t kth = 0;
+#pragma unroll
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t trial = kth | (1u << bit);
+        if (__popcll(__ballot(key >= trial)) >= K) kth = trial;
+      }
+      if (kth > 0x007fffffu) {  // above the order of -inf
+        const float bound = __uint_as_float((kth >> 31) ? kth & 0x7fffffffu : ~kth);
+        if (bound > list.floor_v) {
+          list.floor_v = bound;
+          list.floor_i = INT32_MAX;
+        }
+      }
+      // Without a bound, everything above -inf.
+      const float least = fmaxf(list.floor_v, -FLT_MAX);
+      const int n0 = list.n;
+      bool room = true;
+#pragma unroll
+      for (int e = 0; e < PL; ++e) {
+        const unsigned long long hit = __ballot(x[e] >= least);
+        if (hit && room) {
+          const int i = at(wave0, e / VN, e % VN);
+          const unsigned long long m = __ballot(x[e] >= least && better(x[e], i, list.floor_v, list.floor_i));
+          room = list.n + __popcll(m) <= kList;
+          if (room) append(list, m, x[e], i, lane);
+        }
+      }
+      if (!room) {  // clustered values: once more from memory, with the list cut where it is full
+        list.n = n0;
+        for (int e = 0; e < PL; ++e) {
+          const int i = at(wave0, e / VN, e % VN);
+          const float v = i < seg1 ? logit<BF16>(p.logits, row0 + i) : -INFINITY;
+          push(list, v >= least && better(v, i, list.floor_v, list.floor_i), v, i, K, lane);
+        }
+      }
+      // Fewer than K above -inf so far: tokens of -inf and NaN count too, by index.
+      for (int v = 0; v < NV && list.n < K && at(wave0, v, 0) - lane * VN < seg1; ++v)
+        for (int j = 0; j < VN; ++j) {
+          const int i = at(wave0, v, j);
+          const bool none = i < seg1 && !(logit<BF16>(p.logits, row0 + i) > -INFINITY);
+          push(list, none && better(-INFINITY, i, list.floor_v, list.floor_i), -INFINITY, i, K, lane);
+        }
+    }
+  }
+
+  st = wave_join(st);
+  if (lane == 0) {
+    l_stats[wave] = st;
+    l_n[wave] = list.n;
+  }
+  __syncthreads();
+  st = join(join(l_stats[0], l_stats[1]), join(l_stats[2], l_stats[3]));
+  const int total = l_n[0] + l_n[1] + l_n[2] + l_n[3];
+  if (p.n_segs > 1) {
+    const int64_t s = static_cast<int64_t>(row) * p.n_segs + seg;
+    if (tid == 0) {
+      p.stats[3 * s] = st.m;
+      p.stats[3 * s + 1] = st.z;
+      p.stats[3 * s + 2] = st.t;
+    }
+    uint2* const out = p.cand + s * K;
+    if (K > 0) {
+      best_of(l_val, l_idx, l_n, K, [&](int r, float v, int i) {
+        out[r] = make_uint2(__float_as_uint(v), static_cast<uint32_t>(i));
+      });
+      if (tid < K && tid >= total) out[tid] = make_uint2(__float_as_uint(-INFINITY), 0xffffffffu);
+    }
+    return;
+  }
+  const Finals f = finals(st);
+  if (tid == 0) {
+    if (p.tokens)
+      p.logprobs[row] = tok < 0 ? 0.f : (tok < p.vocab ? log_prob(x_tok, f.lse) : NAN);
+    if (p.entropy) p.entropy[row] = f.entropy;
+  }
+  if (K > 0) {
+    const int64_t o = static_cast<int64_t>(row) * K;
+    best_of(l_val, l_idx, l_n, K, [&](int r, float v, int i) {
+      p.top[o + r] = i;
+      p.top_logprobs[o + r] = log_prob(v, f.lse);
+    });
+    if (tid < K && tid >= total) {
+      p.top[o + tid] = -1;
+      p.top_logprobs[o + tid] = -INFINITY;
+    }
+  }
+}
+
+// Joins a row's segments.
+template <bool BF16>
+__global__ void __launch_bounds__(256)
+logprobs_join_kernel(const LogpParams p) {
+  __shared__ float l_val[4][kList];
+  __shared__ int l_idx[4][kList];
+  __shared__ int l_n[4];
+  __shared__ Stats l_stats[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row = blockIdx.x, K = p.top_k;
+  float x_tok = 0.f;
+  int tok = -1;
+  if (p.tokens && tid == 0) {
+    tok = p.tokens[row];
+    if (tok >= 0 && tok < p.vocab) x_tok = logit<BF16>(p.logits, row * p.row_stride + tok);
+  }
+  Stats st = {-INFINITY, 0.f, 0.f};
+  for (int s = tid; s < p.n_segs; s += 256) {
+    const float* const x = p.stats + 3 * (static_cast<int64_t>(row) * p.n_segs + s);
+    st = join(st, Stats{x[0], x[1], x[2]});
+  }
+  st = wave_join(st);
+  List list = {l_val[wave], l_idx[wave], 0, -INFINITY, INT32_MAX};
+  const uint2* const cand = p.cand + static_cast<int64_t>(row) * p.n_segs * K;
+  for (int c0 = wave * 64; c0 < p.n_segs * K; c0 += 256) {
+    const int c = c0 + lane;
+    const uint2 e = c < p.n_segs * K ? cand[c] : make_uint2(0u, 0xffffffffu);
+    const float v = __uint_as_float(e.x);
+    const int i = static_cast<int>(e.y);
+    push(list, i >= 0 && better(v, i, list.floor_v, list.floor_i), v, i, K, lane);
+  }
+  if (lane == 0) {
+    l_stats[wave] = st;
+    l_n[wave] = list.n;
+  }
+  __syncthreads();
+  const Finals f = finals(join(join(l_stats[0], l_stats[1]), join(l_stats[2], l_stats[3])));
+  if (tid == 0) {
+    if (p.tokens)
+      p.logprobs[row] = tok < 0 ? 0.f : (tok < p.vocab ? log_prob(x_tok, f.lse) : NAN);
+    if (p.entropy) p.entropy[row] = f.entropy;
+  }
+  if (K > 0) {
+    const int64_t o = static_cast<int64_t>(row) * K;
+    best_of(l_val, l_idx, l_n, K, [&](int r, float v, int i) {
+      p.top[o + r] = i;
+      p.top_logprobs[o + r] = log_prob(v, f.lse);
+    });
+    const int total = l_n[0] + l_n[1] + l_n[2] + l_n[3];
+    if (tid < K && tid >= total) {
+      p.top[o + tid] = -1;
+      p.top_logprobs[o + tid] = -INFINITY;
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_token_logprobs(const LogpParams& p, const LogpPlan& pl, bool bf16, hipStream_t s) {
+  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(p.rows) * p.n_segs)), block(256);
+#define MD_LOGP(BF, PL) hipLaunchKernelGGL((logprobs_kernel<BF, PL>), grid, block, 0, s, p)
+  if (pl.per_lane == 64) {
+    if (bf16) MD_LOGP(true, 64); else MD_LOGP(false, 64);
+  } else {
+    if (bf16) MD_LOGP(true, 16); else MD_LOGP(false, 16);
+  }
+#undef MD_LOGP
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.n_segs == 1) return e;
+  if (bf16)
+    hipLaunchKernelGGL((logprobs_join_kernel<true>), dim3(static_cast<uint32_t>(p.rows)), block, 0, s, p);
+  else
+    hipLaunchKernelGGL((logprobs_join_kernel<false>), dim3(static_cast<uint32_t>(p.rows)), block, 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace md
