@@ -746,7 +746,7 @@ typedef struct {
  * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers, bad sizes, strides or page
  * geometry, q_len > max_kv_len > slot_stride, mass or slot_pos overlapping each other or an
  * input; MD_ERR_UNSUPPORTED for head_dim not in {64,128}, kv_stride_tok > 2^28
- * elements, max_kv_len > 2^31 - 65, L * G > 2^31 - 65, or sizes past the grid's 32 bits (2^24 - 1
+ * elements, max_kv_len > 2^31 - 65, L * G > 2^30, or sizes past the grid's 32 bits (2^24 - 1
  * workgroups); MD_ERR_WORKSPACE; MD_ERR_HIP.
  */
 int md_kv_mass(const md_kv_mass_args* a, void* stream);

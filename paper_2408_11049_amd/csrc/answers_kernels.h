@@ -45,7 +45,7 @@ struct MassParams {
   int32_t* slot_pos;
   int64_t slot_stride;
   int32_t B, L, Hq, Hkv, G;
-  int32_t keys, key_blocks, row_parts;
+  int32_t row_parts, part_rows;
   float* parts;               // [row_parts][B, Hkv][max_len] (row_parts > 1)
   float scale_log2;
 };
@@ -80,7 +80,8 @@ struct LogpParams {
 
 hipError_t launch_prefix_attn(const PrefixParams& p, int64_t n_wgs, int head_dim, bool bf16,
                               hipStream_t s);
-hipError_t launch_kv_mass(const MassParams& p, int64_t n_wgs, int head_dim, bool bf16, hipStream_t s);
+hipError_t launch_kv_mass(const MassParams& p, const MassPlan& pl, int head_dim, bool bf16,
+                          hipStream_t s);
 hipError_t launch_kv_evict(const EvictParams& p, hipStream_t s);
 hipError_t launch_token_logprobs(const LogpParams& p, const LogpPlan& pl, bool bf16, hipStream_t s);
 

@@ -2,10 +2,17 @@
 // over rows and the query heads of a KV head, added to what the token had:
 //   w(j) = sum_r exp(scale q_r . k_j - lse_r)
 //
-// A workgroup takes 128 keys of one KV head, 32 a wave, which stay in registers as the second
-// operand while the rows of Q go past in LDS tiles of 32: S = Q K^T leaves a lane one key and 16
-// rows, so the sum over rows is in the lane but for one exchange at the end.  Every sum has a
-// fixed order: a tile's 32 rows first, then the tiles.
+// A wave holds 32 or 64 keys of one KV head in registers as the second operand while the rows of
+// Q go past in LDS: S = Q K^T leaves a lane one key and 16 rows, so the sum over rows is in the
+// lane but for one exchange at the end.  Every sum has a fixed order: a tile's 32 rows first,
+// then the tiles, then the parts.
+//
+//   mass_step    few rows (a step's): bound by reading K, which goes through LDS in whole rows
+//                (the operand's own pattern, 32 bytes of each row an instruction, streams at two
+//                thirds of that);
+//   mass_prompt  many rows (a prompt's): bound by the matrix and vector units alike.  The rows are
+//                cut into parts, whose sums mass_reduce adds, so that early keys, which
+//                most rows see, are no longer work than late ones.
 #include "answers_kernels.h"
 
 namespace md {
@@ -17,137 +24,86 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 namespace {
 
-constexpr int kRows = 32;  // of a tile
+constexpr float kLog2e = 1.44269504088896340736f;
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256)
-kv_mass_kernel(const MassParams p) {
-  constexpr int ES = BF16 ? 2 : 4, ROW = D * ES, CH = ROW / 16, ST = CH / 2;
-  constexpr int NP = kRows * CH / 256;  // chunks of a Q tile a thread moves
-  constexpr float kLog2e = 1.44269504088896340736f;
-  // Q rows unpadded, chunk c of row r in place c ^ turn(r): see the shared-prefix attention.
-  __shared__ __attribute__((aligned(16))) unsigned char qt[2][kRows * ROW];
-  __shared__ __attribute__((aligned(16))) float nl[2][kRows];  // -lse in log2, -inf: weighs nothing
-  auto at = [](int r, int c) {
-    const int turn = ROW == 128 ? (r >> 1) & 7 : r & 15;
-    return r * ROW + ((c ^ turn) << 4);
-  };
+struct Row {
+  static constexpr int ES = BF16 ? 2 : 4, BYTES = D * ES, CH = BYTES / 16, ST = CH / 2;
+  // LDS rows unpadded, chunk c of row r in place c ^ turn(r): see the shared-prefix attention.
+  static __device__ __forceinline__ int at(int r, int c) {
+    const int turn = BYTES == 128 ? (r >> 1) & 7 : r & 15;
+    return r * BYTES + ((c ^ turn) << 4);
+  }
+};
 
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5, wave = tid >> 6;
-  const int units = p.B * p.Hkv;
-  const int unit = static_cast<int>(blockIdx.x) % units;
-  const int kb = static_cast<int>(blockIdx.x) / units;
-  const int hk = unit % p.Hkv, b = unit / p.Hkv;
-  const int S = min(max(p.c.lens[b], 0), p.c.max_len);
-  const int key_first = kb * p.keys;
-  if (key_first >= S) return;
-  const int key = key_first + wave * 32 + l32;
-  const bool live = key < S;
-  const int base = S - p.L;  // the key that row 0 sits at (below 0: a length shorter than L)
+// Byte offset of a key's row, or -1: no token of the pool.
+__device__ __forceinline__ int64_t key_offset(const MassParams& p, int b, int hk, int key, int es) {
+  int64_t off;
+  if (p.c.page_table != nullptr) {
+    const int pid = p.c.page_table[static_cast<int64_t>(b) * p.c.max_pages + (key >> p.c.page_shift)];
+    if (pid < 0 || pid >= p.c.num_pages) return -1;
+    off = static_cast<int64_t>(pid) * p.c.s_blk +
+          static_cast<int64_t>(key & ((1 << p.c.page_shift) - 1)) * p.c.s_tok;
+  } else {
+    off = static_cast<int64_t>(b) * p.c.s_blk + static_cast<int64_t>(key) * p.c.s_tok;
+  }
+  return (off + static_cast<int64_t>(hk) * p.c.s_head) * es;
+}
 
-  // This lane's key as an operand: chunks 2 st + half of its row.
-  u32x4 k[ST];
-  {
-    int64_t off = 0;
-    bool ok = live;
-    if (p.c.page_table != nullptr) {
-      const int pid = ok ? p.c.page_table[static_cast<int64_t>(b) * p.c.max_pages + (key >> p.c.page_shift)] : -1;
-      ok = pid >= 0 && pid < p.c.num_pages;
-      off = static_cast<int64_t>(pid) * p.c.s_blk +
-            static_cast<int64_t>(key & ((1 << p.c.page_shift) - 1)) * p.c.s_tok;
+// Row r = i * G + g of KV head hk: its place among the [B, L, Hq] rows.
+__device__ __forceinline__ int64_t query_row(const MassParams& p, int b, int hk, int r) {
+  const int i = r / p.G;
+  return (static_cast<int64_t>(b) * p.L + i) * p.Hq + hk * p.G + (r - i * p.G);
+}
+
+// What a row's score gets under the exponential: -lse in log2; -inf: the row weighs nothing.
+__device__ __forceinline__ float neg_lse(const MassParams& p, int b, int hk, int r, int r_end) {
+  if (r >= r_end) return -INFINITY;
+  const float l = p.lse[query_row(p, b, hk, r)];
+  return l == -INFINITY ? -INFINITY : -l * kLog2e;
+}
+
+template <int D, bool BF16>
+__device__ __forceinline__ f32x16 scores(const u32x4 (&q)[D * (BF16 ? 2 : 4) / 32],
+                                         const u32x4 (&k)[D * (BF16 ? 2 : 4) / 32]) {
+  f32x16 s = {};
+#pragma unroll
+  for (int st = 0; st < Row<D, BF16>::ST; ++st) {
+    if constexpr (BF16) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q[st]),
+                                                  __builtin_bit_cast(bf16x8, k[st]), s, 0, 0, 0);
     } else {
-      off = static_cast<int64_t>(b) * p.c.s_blk + static_cast<int64_t>(key) * p.c.s_tok;
-    }
-    off = ok ? (off + static_cast<int64_t>(hk) * p.c.s_head) * ES : 0;
 #pragma unroll
-    for (int st = 0; st < ST; ++st)
-      k[st] = *reinterpret_cast<const u32x4*>(p.c.k + off + (2 * st + half) * 16);
+      for (int j = 0; j < 4; ++j)
+        s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(q[st][j]), __uint_as_float(k[st][j]), s,
+                                                 0, 0, 0);
+    }
   }
+  return s;
+}
 
-  // Rows i * G + g that count and see a key of this workgroup.
-  int n_count = p.L;
-  if (p.accepted) n_count = min(max(p.accepted[b], 0), p.L - 1) + 1;
-  const int r_begin = max(0, key_first - base) * p.G;  // base may be < 0: then rows start later
-  const int r_end = n_count * p.G;
-  // The first row that sees this lane's key.
-  const int r_sees = max(0, key - base) * p.G;
-
-  u32x4 stage_q[NP];
-  float stage_l = -INFINITY;
-  auto load_tile = [&](int r0) {
-    if (r0 >= r_end) return;
+// The weights of a tile's 16 rows in this lane (8 (e / 4) + 4 half + e % 4), summed.  nl: the tile's
+// neg_lse.  masked: rows before `first` do not see the lane's key, and rows of -inf count nothing
+// whatever their score (else -inf alone does that, where the score is finite).
+__device__ __forceinline__ float weigh(const f32x16& s, const float* nl, float scale_log2, int half,
+                                       bool masked, int first) {
+  float part[4];
 #pragma unroll
-    for (int n = 0; n < NP; ++n) {
-      const int x = n * 256 + tid, r = r0 + x / CH;
-      const bool ok = r < r_end;
-      const int i = r / p.G;
-      const int64_t row = (static_cast<int64_t>(b) * p.L + i) * p.Hq + hk * p.G + (r - i * p.G);
-      stage_q[n] = ok ? *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(p.q) +
-                                                        row * ROW + (x % CH) * 16)
-                      : u32x4{0, 0, 0, 0};
+  for (int j = 0; j < 4; ++j) {
+    const f32x4 l4 = *reinterpret_cast<const f32x4*>(nl + 8 * j + 4 * half);
+    part[j] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * j + e], scale_log2, l4[e]));
+      if (masked && (l4[e] == -INFINITY || 8 * j + 4 * half + e < first)) x = 0.f;
+      part[j] += x;
     }
-    if (tid < kRows) {
-      const int r = r0 + tid;
-      stage_l = -INFINITY;
-      if (r < r_end) {
-        const int i = r / p.G;
-        const float l = p.lse[(static_cast<int64_t>(b) * p.L + i) * p.Hq + hk * p.G + (r - i * p.G)];
-        if (l != -INFINITY) stage_l = -l * kLog2e;
-      }
-    }
-  };
-  auto store_tile = [&](int buf, int r0) {
-    if (r0 >= r_end) return;
-#pragma unroll
-    for (int n = 0; n < NP; ++n) {
-      const int x = n * 256 + tid;
-      *reinterpret_cast<u32x4*>(qt[buf] + at(x / CH, x % CH)) = stage_q[n];
-    }
-    if (tid < kRows) nl[buf][tid] = stage_l;
-  };
-
-  float w = 0.f;
-  load_tile(r_begin);
-  store_tile(0, r_begin);
-  load_tile(r_begin + kRows);
-  __syncthreads();
-  int buf = 0;
-  for (int r0 = r_begin; r0 < r_end; r0 += kRows, buf ^= 1) {
-    store_tile(buf ^ 1, r0 + kRows);
-    load_tile(r0 + 2 * kRows);
-    f32x16 s = {};
-#pragma unroll
-    for (int st = 0; st < ST; ++st) {
-      const u32x4 q = *reinterpret_cast<const u32x4*>(qt[buf] + at(l32, 2 * st + half));
-      if constexpr (BF16) {
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q),
-                                                    __builtin_bit_cast(bf16x8, k[st]), s, 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(q[j]), __uint_as_float(k[st][j]), s,
-                                                   0, 0, 0);
-      }
-    }
-    // Rows r0 + 8 (e / 4) + 4 half + e % 4.
-    const bool masked = __any(r0 < r_sees);
-    float part[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4 l4 = *reinterpret_cast<const f32x4*>(&nl[buf][8 * j + 4 * half]);
-      part[j] = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * j + e], p.scale_log2, l4[e]));
-        if (l4[e] == -INFINITY || (masked && r0 + 8 * j + 4 * half + e < r_sees)) x = 0.f;
-        part[j] += x;
-      }
-    }
-    w += (part[0] + part[1]) + (part[2] + part[3]);
-    __syncthreads();
   }
-  w += __shfl_xor(w, 32);
-  if (half || !live) return;
+  return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+__device__ __forceinline__ void store(const MassParams& p, int unit, int b, int key, int base, float w) {
   const int64_t slot = static_cast<int64_t>(unit) * p.slot_stride + key;
   if (key >= base) {  // a newest token
     p.mass[slot] = w;
@@ -157,17 +113,227 @@ kv_mass_kernel(const MassParams p) {
   }
 }
 
+// Up to kMassStepRows rows, all in LDS at once; 128 keys a workgroup, 32 a wave.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256)
+mass_step(const MassParams p) {
+  using T = Row<D, BF16>;
+  constexpr int KP = 128 * T::CH / 256;  // chunks of the keys a thread moves
+  __shared__ __attribute__((aligned(16))) unsigned char kt[128 * T::BYTES];
+  __shared__ __attribute__((aligned(16))) unsigned char qt[32 * T::BYTES];
+  __shared__ __attribute__((aligned(16))) float nl[32];
+
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = uniform(tid >> 6);
+  const int units = p.B * p.Hkv;
+  const int unit = static_cast<int>(blockIdx.x) % units, kb = static_cast<int>(blockIdx.x) / units;
+  const int hk = unit % p.Hkv, b = unit / p.Hkv;
+  const int S = min(max(p.c.lens[b], 0), p.c.max_len);
+  const int key_first = kb * 128;
+  if (key_first >= S) return;
+  const int base = S - p.L;  // the key that row 0 sits at (below 0: a length shorter than L)
+  u32x4 kr[KP];
+#pragma unroll
+  for (int n = 0; n < KP; ++n) {
+    const int x = n * 256 + tid, key = key_first + x / T::CH;
+    const int64_t off = key < S ? key_offset(p, b, hk, key, T::ES) : -1;
+    // No token: the first row stands in, its weight is not stored (or, on no page of the pool,
+    // unspecified).
+    kr[n] = __builtin_nontemporal_load(
+        reinterpret_cast<const u32x4*>(p.c.k + (off < 0 ? 0 : off) + (x % T::CH) * 16));
+  }
+  int n_count = p.L;
+  if (p.accepted) n_count = min(max(p.accepted[b], 0), p.L - 1) + 1;
+  const int r_begin = max(0, key_first - base) * p.G;
+  const int r_end = n_count * p.G;
+  const int key = key_first + wave * 32 + l32;
+  const int r_sees = max(0, key - base) * p.G;  // the first row that sees this lane's key
+  float w = 0.f;
+  u32x4 k[T::ST];
+  for (int r0 = r_begin; r0 < r_end; r0 += 32) {
+#pragma unroll
+    for (int n = 0; n < 32 * T::CH / 256; ++n) {
+      const int x = n * 256 + tid, r = r0 + x / T::CH;
+      u32x4 q = {0, 0, 0, 0};
+      if (r < r_end)
+        q = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(p.q) +
+                                            query_row(p, b, hk, r) * T::BYTES + (x % T::CH) * 16);
+      *reinterpret_cast<u32x4*>(qt + T::at(x / T::CH, x % T::CH)) = q;
+    }
+    if (tid < 32) nl[tid] = neg_lse(p, b, hk, r0 + tid, r_end);
+    if (r0 == r_begin) {
+#pragma unroll
+      for (int n = 0; n < KP; ++n) {
+        const int x = n * 256 + tid;
+        *reinterpret_cast<u32x4*>(kt + T::at(x / T::CH, x % T::CH)) = kr[n];
+      }
+    }
+    __syncthreads();
+    if (r0 == r_begin) {
+#pragma unroll
+      for (int st = 0; st < T::ST; ++st)
+        k[st] = *reinterpret_cast<const u32x4*>(kt + T::at(wave * 32 + l32, 2 * st + half));
+    }
+    u32x4 q[T::ST];
+#pragma unroll
+    for (int st = 0; st < T::ST; ++st)
+      q[st] = *reinterpret_cast<const u32x4*>(qt + T::at(l32, 2 * st + half));
+    w += weigh(scores<D, BF16>(q, k), nl, p.scale_log2, half, true, r_sees - r0);
+    __syncthreads();
+  }
+  w += __shfl_xor(w, 32);
+  if (!half && key < S) store(p, unit, b, key, base, w);
+}
+
+// A part of the rows, 64 of them in LDS at a time (two such tiles in turn); 256 keys a
+// workgroup, 64 a wave.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(D == 128 && !BF16 ? 1 : 2)))
+mass_prompt(const MassParams p) {
+  using T = Row<D, BF16>;
+  constexpr int NR = 64, QP = NR * T::CH / 256;
+  __shared__ __attribute__((aligned(16))) unsigned char qt[2][NR * T::BYTES];
+  __shared__ __attribute__((aligned(16))) float nl[2][NR];
+  __shared__ int odd[2];  // the tile has rows that count nothing
+
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = uniform(tid >> 6);
+  const int units = p.B * p.Hkv;
+  const int unit = static_cast<int>(blockIdx.x) % units;
+  const int part = (static_cast<int>(blockIdx.x) / units) % p.row_parts;
+  const int kb = static_cast<int>(blockIdx.x) / units / p.row_parts;
+  const int hk = unit % p.Hkv, b = unit / p.Hkv;
+  const int S = uniform(min(max(p.c.lens[b], 0), p.c.max_len));
+  const int key_first = kb * kMassPromptKeys;
+  if (key_first >= S) return;
+  const int base = S - p.L;
+  int n_count = p.L;
+  if (p.accepted) n_count = min(max(uniform(p.accepted[b]), 0), p.L - 1) + 1;
+  // Rows of this part that count and see a key of this workgroup.
+  const int r_begin = max(part * p.part_rows, max(0, key_first - base) * p.G);
+  const int r_end = min(n_count * p.G, (part + 1) * p.part_rows);
+  if (r_begin >= r_end && p.row_parts > 1) return;  // mass_reduce does not ask for it
+
+  int key[2], sees[2];
+  u32x4 k[2][T::ST];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    key[x] = key_first + wave * 64 + x * 32 + l32;
+    sees[x] = max(0, min(key[x], S - 1) - base) * p.G;
+    const int64_t off = key[x] < S ? key_offset(p, b, hk, key[x], T::ES) : -1;
+#pragma unroll
+    for (int st = 0; st < T::ST; ++st)
+      k[x][st] = *reinterpret_cast<const u32x4*>(p.c.k + (off < 0 ? 0 : off) + (2 * st + half) * 16);
+  }
+
+  u32x4 sq[QP];
+  float sl = -INFINITY;
+  auto load_tile = [&](int r0) {
+    if (r0 >= r_end) return;
+#pragma unroll
+    for (int n = 0; n < QP; ++n) {
+      const int x = n * 256 + tid, r = r0 + x / T::CH;
+      sq[n] = r < r_end ? *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(p.q) +
+                                                          query_row(p, b, hk, r) * T::BYTES + (x % T::CH) * 16)
+                        : u32x4{0, 0, 0, 0};
+    }
+    if (tid < NR) sl = neg_lse(p, b, hk, r0 + tid, r_end);
+  };
+  auto store_tile = [&](int buf, int r0) {
+    if (r0 >= r_end) return;
+#pragma unroll
+    for (int n = 0; n < QP; ++n) {
+      const int x = n * 256 + tid;
+      *reinterpret_cast<u32x4*>(qt[buf] + T::at(x / T::CH, x % T::CH)) = sq[n];
+    }
+    if (tid < NR) {
+      nl[buf][tid] = sl;
+      const bool none = __any(sl == -INFINITY);
+      if (tid == 0) odd[buf] = none;
+    }
+  };
+
+  float w[2] = {};
+  load_tile(r_begin);
+  store_tile(0, r_begin);
+  load_tile(r_begin + NR);
+  __syncthreads();
+  int buf = 0;
+  for (int r0 = r_begin; r0 < r_end; r0 += NR, buf ^= 1) {
+    store_tile(buf ^ 1, r0 + NR);
+    load_tile(r0 + 2 * NR);
+    const bool masked = odd[buf] || __any(r0 < max(sees[0], sees[1]));
+#pragma unroll
+    for (int y = 0; y < NR / 32; ++y) {
+      u32x4 q[T::ST];
+#pragma unroll
+      for (int st = 0; st < T::ST; ++st)
+        q[st] = *reinterpret_cast<const u32x4*>(qt[buf] + T::at(y * 32 + l32, 2 * st + half));
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const f32x16 s = scores<D, BF16>(q, k[x]);
+        // Two instances: the mask costs as much as the rest of the vector work.
+        if (masked)
+          w[x] += weigh(s, nl[buf] + y * 32, p.scale_log2, half, true, sees[x] - (r0 + y * 32));
+        else
+          w[x] += weigh(s, nl[buf] + y * 32, p.scale_log2, half, false, 0);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const float sum = w[x] + __shfl_xor(w[x], 32);
+    if (half || key[x] >= S) continue;
+    if (p.row_parts == 1)
+      store(p, unit, b, key[x], base, sum);
+    else
+      p.parts[(static_cast<int64_t>(part) * units + unit) * p.c.max_len + key[x]] = sum;
+  }
+}
+
+// The parts' sums, in order; a thread a key.
+__global__ void __launch_bounds__(256)
+mass_reduce(const MassParams p) {
+  const int units = p.B * p.Hkv;
+  const int unit = static_cast<int>(blockIdx.x) % units;
+  const int key = static_cast<int>(blockIdx.x) / units * 256 + static_cast<int>(threadIdx.x);
+  const int b = unit / p.Hkv;
+  const int S = min(max(p.c.lens[b], 0), p.c.max_len);
+  if (key >= S) return;
+  const int base = S - p.L;
+  int n_count = p.L;
+  if (p.accepted) n_count = min(max(p.accepted[b], 0), p.L - 1) + 1;
+  const int key_first = key / kMassPromptKeys * kMassPromptKeys;
+  const int r_begin = max(0, key_first - base) * p.G, r_end = n_count * p.G;
+  float w = 0.f;
+  for (int c = r_begin / p.part_rows; c < p.row_parts && c * p.part_rows < r_end && r_begin < r_end; ++c)
+    w += p.parts[(static_cast<int64_t>(c) * units + unit) * p.c.max_len + key];
+  store(p, unit, b, key, base, w);
+}
+
 }  // namespace
 
-hipError_t launch_kv_mass(const MassParams& p, int64_t n_wgs, int head_dim, bool bf16, hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(n_wgs)), block(256);
-#define MD_MASS(D, BF) hipLaunchKernelGGL((kv_mass_kernel<D, BF>), grid, block, 0, s, p)
+hipError_t launch_kv_mass(const MassParams& p, const MassPlan& pl, int head_dim, bool bf16,
+                          hipStream_t s) {
+  const dim3 grid(static_cast<uint32_t>(pl.n_wgs)), block(256);
+#define MD_MASS(D, BF)                                                          \
+  do {                                                                          \
+    if (pl.prompt)                                                              \
+      hipLaunchKernelGGL((mass_prompt<D, BF>), grid, block, 0, s, p);           \
+    else                                                                        \
+      hipLaunchKernelGGL((mass_step<D, BF>), grid, block, 0, s, p);             \
+  } while (0)
   if (head_dim == 128) {
     if (bf16) MD_MASS(128, true); else MD_MASS(128, false);
   } else {
     if (bf16) MD_MASS(64, true); else MD_MASS(64, false);
   }
 #undef MD_MASS
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.row_parts == 1) return e;
+  hipLaunchKernelGGL(mass_reduce, dim3(static_cast<uint32_t>(pl.reduce_wgs)), block, 0, s, p);
   return hipGetLastError();
 }
 

@@ -23,10 +23,20 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kList = 256;  // candidates a wave lists
 
-// Larger value first, then the lower index.  Values are no NaN.
-__device__ __forceinline__ bool better(float v, int i, float w, int j) {
-  return v > w || (v == w && i < j);
+// A candidate as one number: the larger value first, then the lower index.
+typedef unsigned long long Key;
+__device__ __forceinline__ uint32_t order(float v) {  // v is no NaN
+  const uint32_t x = __float_as_uint(v + 0.f);  // -0 and 0 are equal
+  return (x >> 31) ? ~x : x | 0x80000000u;
 }
+__device__ __forceinline__ Key make_key(float v, int i) {
+  return (static_cast<Key>(order(v)) << 32) | ~static_cast<uint32_t>(i);
+}
+__device__ __forceinline__ float key_value(Key k) {
+  const uint32_t x = static_cast<uint32_t>(k >> 32);
+  return __uint_as_float((x >> 31) ? x & 0x7fffffffu : ~x);
+}
+__device__ __forceinline__ int key_index(Key k) { return static_cast<int>(~static_cast<uint32_t>(k)); }
 
 struct Stats {
   float m, z, t;
@@ -73,84 +83,83 @@ __device__ __forceinline__ float logit(const void* base, int64_t e) {
   return static_cast<const float*>(base)[e];
 }
 
-// The list of one wave, cut to its best top_k in order (best first); returns how many remain.
-// `n` entries; rank by counting.  All lanes of the wave take part.
-__device__ __forceinline__ int cut_list(float* val, int* idx, int n, int top_k, int lane) {
-  float v[kList / 64];
-  int i[kList / 64], rank[kList / 64];
+// How many of list[0 .. n) are above k; the entries from n to the next multiple of 8 are 0.
+__device__ __forceinline__ int count_above(const Key* list, int n, Key k) {
+  int above = 0;
+  for (int e = 0; e < n; e += 8) {
+    Key x[8];
 #pragma unroll
-  for (int x = 0; x < kList / 64; ++x) {
-    const int e = x * 64 + lane;
-    v[x] = e < n ? val[e] : 0.f;
-    i[x] = e < n ? idx[e] : 0;
-    rank[x] = e < n ? 0 : kList;
-  }
-  for (int e = 0; e < n; ++e) {
-    const float w = val[e];
-    const int j = idx[e];
+    for (int j = 0; j < 8; ++j) x[j] = list[e + j];
 #pragma unroll
-    for (int x = 0; x < kList / 64; ++x) rank[x] += better(w, j, v[x], i[x]);
+    for (int j = 0; j < 8; ++j) above += x[j] > k;
   }
+  return above;
+}
+__device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-#pragma unroll
-  for (int x = 0; x < kList / 64; ++x)
-    if (rank[x] < top_k) {
-      val[rank[x]] = v[x];
-      idx[rank[x]] = i[x];
-    }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  return min(n, top_k);
 }
 
 // A wave's list of candidates and what a logit has to beat to enter it.
 struct List {
-  float* val;
-  int* idx;
+  Key* key;        // kList, and 8 behind them
   int n;           // the same in all lanes
-  float floor_v;   // enters: better than (floor_v, floor_i)
-  int floor_i;
+  float floor;     // no logit below it enters
+  Key floor_key;   // nor any candidate that is not above this
 };
-// Adds the (v, i) of the lanes in m.
-__device__ __forceinline__ void append(List& l, unsigned long long m, float v, int i, int lane) {
-  if ((m >> lane) & 1ull) {
-    const int at = l.n + __popcll(m & ((1ull << lane) - 1));
-    l.val[at] = v;
-    l.idx[at] = i;
+__device__ __forceinline__ void pad(const List& l, int lane) {
+  wave_sync();
+  if (lane < 8) l.key[l.n + lane] = 0;
+  wave_sync();
+}
+// The list cut to its best top_k, best first.  All lanes of the wave take part.
+__device__ __forceinline__ void cut(List& l, int top_k, int lane) {
+  pad(l, lane);
+  Key k[kList / 64];
+  int rank[kList / 64];
+#pragma unroll
+  for (int x = 0; x < kList / 64; ++x) {
+    const int e = x * 64 + lane;
+    k[x] = e < l.n ? l.key[e] : 0;
+    rank[x] = e < l.n ? count_above(l.key, l.n, k[x]) : kList;
   }
+  wave_sync();
+#pragma unroll
+  for (int x = 0; x < kList / 64; ++x)
+    if (rank[x] < top_k) l.key[rank[x]] = k[x];
+  wave_sync();
+  l.n = min(l.n, top_k);
+}
+// Adds the keys of the lanes in m.
+__device__ __forceinline__ void append(List& l, unsigned long long m, Key k, int lane) {
+  if ((m >> lane) & 1ull) l.key[l.n + __popcll(m & ((1ull << lane) - 1))] = k;
   l.n += __popcll(m);
 }
 // The same where `in`, cutting a list that is full.
-__device__ __forceinline__ void push(List& l, bool in, float v, int i, int top_k, int lane) {
+__device__ __forceinline__ void push(List& l, bool in, Key k, int top_k, int lane) {
   unsigned long long m = __ballot(in);
   if (l.n + __popcll(m) > kList) {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    l.n = cut_list(l.val, l.idx, l.n, top_k, lane);
-    l.floor_v = l.val[top_k - 1];  // kList > 2 * kLogpMaxTop: the list held more than top_k
-    l.floor_i = l.idx[top_k - 1];
-    in = in && better(v, i, l.floor_v, l.floor_i);
-    m = __ballot(in);
+    cut(l, top_k, lane);
+    l.floor_key = l.key[top_k - 1];  // kList > 2 * kLogpMaxTop: the list held more than top_k
+    l.floor = key_value(l.floor_key);
+    m = __ballot(in && k > l.floor_key);
   }
-  append(l, m, v, i, lane);
+  append(l, m, k, lane);
 }
 
-// The best top_k of four waves' lists, by the whole workgroup: each thread takes one entry in
-// turn and counts the better ones.  f(rank, value, index) for each of the best.
+// The best top_k of four waves' lists, by the whole workgroup: a thread takes a candidate in
+// turn and counts those above it.  f(rank, value, index) for each of the best.
 template <typename F>
-__device__ __forceinline__ void best_of(const float (&val)[4][kList], const int (&idx)[4][kList],
-                                        const int (&n)[4], int top_k, F f) {
+__device__ __forceinline__ void best_of(const Key (&key)[4][kList + 8], const int (&n)[4], int top_k, F f) {
   const int total = n[0] + n[1] + n[2] + n[3];
   for (int e0 = threadIdx.x; e0 < total; e0 += 256) {
     int w = 0, e = e0;
     while (e >= n[w]) e -= n[w++];
-    const float v = val[w][e];
-    const int i = idx[w][e];
+    const Key k = key[w][e];
     int rank = 0;
-    for (int x = 0; x < 4; ++x)
-      for (int y = 0; y < n[x]; ++y) rank += better(val[x][y], idx[x][y], v, i);
-    if (rank < top_k) f(rank, v, i);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) rank += count_above(key[x], n[x], k);
+    if (rank < top_k) f(rank, key_value(k), key_index(k));
   }
 }
 
@@ -159,8 +168,7 @@ template <bool BF16, int PL>
 __global__ void __launch_bounds__(256)
 logprobs_kernel(const LogpParams p) {
   constexpr int VN = BF16 ? 8 : 4, NV = PL / VN;  // logits of a 16-byte vector, vectors a lane
-  __shared__ float l_val[4][kList];
-  __shared__ int l_idx[4][kList];
+  __shared__ __attribute__((aligned(16))) Key l_key[4][kList + 8];
   __shared__ int l_n[4];
   __shared__ Stats l_stats[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -177,7 +185,7 @@ logprobs_kernel(const LogpParams p) {
   }
 
   Stats st = {-INFINITY, 0.f, 0.f};
-  List list = {l_val[wave], l_idx[wave], 0, -INFINITY, INT32_MAX};
+  List list = {l_key[wave], 0, -INFINITY, 0};
   // Element j of vector v of this lane.
   auto at = [&](int wave0, int v, int j) { return wave0 + v * 64 * VN + lane * VN + j; };
   for (int c0 = seg0; c0 < seg1; c0 += 256 * PL) {
@@ -248,23 +256,23 @@ logprobs_kernel(const LogpParams p) {
       }
       if (kth > 0x007fffffu) {  // above the order of -inf
         const float bound = __uint_as_float((kth >> 31) ? kth & 0x7fffffffu : ~kth);
-        if (bound > list.floor_v) {
-          list.floor_v = bound;
-          list.floor_i = INT32_MAX;
+        if (bound > list.floor) {
+          list.floor = bound;
+          list.floor_key = 0;
         }
       }
       // Without a bound, everything above -inf.
-      const float least = fmaxf(list.floor_v, -FLT_MAX);
+      const float least = fmaxf(list.floor, -FLT_MAX);
       const int n0 = list.n;
       bool room = true;
 #pragma unroll
       for (int e = 0; e < PL; ++e) {
         const unsigned long long hit = __ballot(x[e] >= least);
         if (hit && room) {
-          const int i = at(wave0, e / VN, e % VN);
-          const unsigned long long m = __ballot(x[e] >= least && better(x[e], i, list.floor_v, list.floor_i));
+          const Key k = make_key(x[e], at(wave0, e / VN, e % VN));
+          const unsigned long long m = __ballot(x[e] >= least && k > list.floor_key);
           room = list.n + __popcll(m) <= kList;
-          if (room) append(list, m, x[e], i, lane);
+          if (room) append(list, m, k, lane);
         }
       }
       if (!room) {  // clustered values: once more from memory, with the list cut where it is full
@@ -272,7 +280,8 @@ logprobs_kernel(const LogpParams p) {
         for (int e = 0; e < PL; ++e) {
           const int i = at(wave0, e / VN, e % VN);
           const float v = i < seg1 ? logit<BF16>(p.logits, row0 + i) : -INFINITY;
-          push(list, v >= least && better(v, i, list.floor_v, list.floor_i), v, i, K, lane);
+          const Key k = make_key(v, i);
+          push(list, v >= least && k > list.floor_key, k, K, lane);
         }
       }
       // Fewer than K above -inf so far: tokens of -inf and NaN count too, by index.
@@ -280,12 +289,14 @@ logprobs_kernel(const LogpParams p) {
         for (int j = 0; j < VN; ++j) {
           const int i = at(wave0, v, j);
           const bool none = i < seg1 && !(logit<BF16>(p.logits, row0 + i) > -INFINITY);
-          push(list, none && better(-INFINITY, i, list.floor_v, list.floor_i), -INFINITY, i, K, lane);
+          const Key k = make_key(-INFINITY, i);
+          push(list, none && k > list.floor_key, k, K, lane);
         }
     }
   }
 
   st = wave_join(st);
+  pad(list, lane);
   if (lane == 0) {
     l_stats[wave] = st;
     l_n[wave] = list.n;
@@ -302,7 +313,7 @@ logprobs_kernel(const LogpParams p) {
     }
     uint2* const out = p.cand + s * K;
     if (K > 0) {
-      best_of(l_val, l_idx, l_n, K, [&](int r, float v, int i) {
+      best_of(l_key, l_n, K, [&](int r, float v, int i) {
         out[r] = make_uint2(__float_as_uint(v), static_cast<uint32_t>(i));
       });
       if (tid < K && tid >= total) out[tid] = make_uint2(__float_as_uint(-INFINITY), 0xffffffffu);
@@ -317,7 +328,7 @@ logprobs_kernel(const LogpParams p) {
   }
   if (K > 0) {
     const int64_t o = static_cast<int64_t>(row) * K;
-    best_of(l_val, l_idx, l_n, K, [&](int r, float v, int i) {
+    best_of(l_key, l_n, K, [&](int r, float v, int i) {
       p.top[o + r] = i;
       p.top_logprobs[o + r] = log_prob(v, f.lse);
     });
@@ -332,8 +343,7 @@ logprobs_kernel(const LogpParams p) {
 template <bool BF16>
 __global__ void __launch_bounds__(256)
 logprobs_join_kernel(const LogpParams p) {
-  __shared__ float l_val[4][kList];
-  __shared__ int l_idx[4][kList];
+  __shared__ __attribute__((aligned(16))) Key l_key[4][kList + 8];
   __shared__ int l_n[4];
   __shared__ Stats l_stats[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -350,15 +360,17 @@ logprobs_join_kernel(const LogpParams p) {
     st = join(st, Stats{x[0], x[1], x[2]});
   }
   st = wave_join(st);
-  List list = {l_val[wave], l_idx[wave], 0, -INFINITY, INT32_MAX};
+  List list = {l_key[wave], 0, -INFINITY, 0};
   const uint2* const cand = p.cand + static_cast<int64_t>(row) * p.n_segs * K;
   for (int c0 = wave * 64; c0 < p.n_segs * K; c0 += 256) {
     const int c = c0 + lane;
     const uint2 e = c < p.n_segs * K ? cand[c] : make_uint2(0u, 0xffffffffu);
     const float v = __uint_as_float(e.x);
     const int i = static_cast<int>(e.y);
-    push(list, i >= 0 && better(v, i, list.floor_v, list.floor_i), v, i, K, lane);
+    const Key k = make_key(v, i);
+    push(list, i >= 0 && k > list.floor_key, k, K, lane);
   }
+  pad(list, lane);
   if (lane == 0) {
     l_stats[wave] = st;
     l_n[wave] = list.n;
@@ -372,7 +384,7 @@ logprobs_join_kernel(const LogpParams p) {
   }
   if (K > 0) {
     const int64_t o = static_cast<int64_t>(row) * K;
-    best_of(l_val, l_idx, l_n, K, [&](int r, float v, int i) {
+    best_of(l_key, l_n, K, [&](int r, float v, int i) {
       p.top[o + r] = i;
       p.top_logprobs[o + r] = log_prob(v, f.lse);
     });

@@ -165,7 +165,7 @@ int check_mass_sizes(const md_kv_mass_args* a) {
   if (a->head_dim != 64 && a->head_dim != 128) return MD_ERR_UNSUPPORTED;
   if (a->kv_stride_tok > kMaxTokStride || a->max_kv_len > kMaxPosition) return MD_ERR_UNSUPPORTED;
   const int64_t G = a->num_q_heads / a->num_kv_heads;
-  if (G * a->q_len > kMaxPosition) return MD_ERR_UNSUPPORTED;
+  if (G * a->q_len > (1 << 30)) return MD_ERR_UNSUPPORTED;
   const int64_t units = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads;
   if (units > kMaxWgs256 || units * ceil_div(a->max_kv_len, 128) > kMaxWgs256)
     return MD_ERR_UNSUPPORTED;
@@ -174,10 +174,25 @@ int check_mass_sizes(const md_kv_mass_args* a) {
 
 MassPlan make_mass_plan(const md_kv_mass_args* a, int num_cus) {
   MassPlan pl;
-  (void)num_cus;
-  pl.keys = 128;
-  pl.key_blocks = static_cast<int32_t>(ceil_div(a->max_kv_len, pl.keys));
-  pl.n_wgs = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads * pl.key_blocks;
+  const int64_t cus = num_cus > 0 ? num_cus : 256;
+  const int64_t units = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads;
+  const int64_t rows = static_cast<int64_t>(a->num_q_heads / a->num_kv_heads) * a->q_len;
+  pl.part_rows = static_cast<int32_t>(rows);
+  pl.prompt = rows > kMassStepRows;
+  if (!pl.prompt) {
+    pl.n_wgs = units * ceil_div(a->max_kv_len, kMassStepKeys);
+    return pl;
+  }
+  const int64_t blocks = units * ceil_div(a->max_kv_len, kMassPromptKeys);
+  // Half of a prompt's (row, key) pairs are masked.  Four workgroups of what is left to each place of
+  // the device (two a compute unit), of 256 rows at least.
+  const int64_t parts = std::min(ceil_div(16 * cus, std::max<int64_t>(blocks, 1)), ceil_div(rows, 256));
+  pl.part_rows = static_cast<int32_t>(ceil_div(ceil_div(rows, std::max<int64_t>(parts, 1)), 64) * 64);
+  pl.row_parts = static_cast<int32_t>(ceil_div(rows, pl.part_rows));
+  pl.n_wgs = blocks * pl.row_parts;
+  pl.reduce_wgs = units * ceil_div(a->max_kv_len, 256);
+  if (pl.row_parts > 1)
+    pl.workspace_bytes = align_up(static_cast<size_t>(pl.row_parts) * units * a->max_kv_len * 4, 256);
   return pl;
 }
 
