@@ -12,15 +12,19 @@
 
 namespace md {
 
-// Shared-prefix attention: query rows and keys of a workgroup's tile.
-constexpr int kPrefixRows = 128;
-constexpr int kPrefixTile(bool bf16) { return bf16 ? 64 : 32; }
+// Shared-prefix attention: query rows of a workgroup and keys of a tile where the call is bound by
+// reading K and V, and where bf16 groups of more than kPrefixFewRows rows a KV head are by the products.
+constexpr int kPrefixStreamRows = 32, kPrefixStreamTile = 32;
+constexpr int kPrefixWideRows = 256, kPrefixWideTile = 64, kPrefixFewRows = 64;
+// Tokens that a page has to hold for the latter: a load instruction's rows.
+constexpr int kPrefixWidePage(int d) { return d == 128 ? 4 : 8; }
 struct PrefixPlan {
+  bool wide = false;
   int32_t group_rows = 0;   // rows of a (prefix, KV head): B / P * L * G
-  int32_t row_blocks = 0;   // of kPrefixRows
+  int32_t row_blocks = 0, own_blocks = 0;  // of the workgroups' rows: a group's, a sequence's
   int32_t c_pre = 0, c_own = 0;  // parts of the prefix's and of the own keys
   int32_t n_pre = 0;        // workgroups of the prefix, padded to whole rounds of the XCDs
-  int64_t n_wgs = 0;
+  int64_t n_own = 0;        // and of the own caches
   int64_t n_rows = 0;       // B * L * Hq
   size_t part_o_bytes = 0, part_lse_bytes = 0, workspace_bytes = 0;
 };

@@ -27,7 +27,7 @@ struct PrefixParams {
   const void* q;
   int32_t P, n;               // prefixes, sequences of each
   int32_t L, Hq, Hkv, G;
-  int32_t group_rows, row_blocks, c_pre, c_own, n_pre;
+  int32_t group_rows, row_blocks, own_blocks, c_pre, c_own, n_pre;
   float scale_log2;           // softmax scale * log2(e)
   float* part_o;              // [c_pre + c_own][n_rows][d]
   float* part_lse;            // [c_pre + c_own][n_rows]
@@ -78,7 +78,7 @@ struct LogpParams {
   uint2* cand;                // [rows][n_segs][top_k]: value, index
 };
 
-hipError_t launch_prefix_attn(const PrefixParams& p, int64_t n_wgs, int head_dim, bool bf16,
+hipError_t launch_prefix_attn(const PrefixParams& p, const PrefixPlan& pl, int head_dim, bool bf16,
                               hipStream_t s);
 hipError_t launch_kv_mass(const MassParams& p, const MassPlan& pl, int head_dim, bool bf16,
                           hipStream_t s);

@@ -60,6 +60,7 @@ int md_prefix_attn(const md_attn_args* a, const md_prefix* prefix, void* stream)
   p.G = a->num_q_heads / a->num_kv_heads;
   p.group_rows = pl.group_rows;
   p.row_blocks = pl.row_blocks;
+  p.own_blocks = pl.own_blocks;
   p.c_pre = pl.c_pre;
   p.c_own = pl.c_own;
   p.n_pre = pl.n_pre;
@@ -70,7 +71,7 @@ int md_prefix_attn(const md_attn_args* a, const md_prefix* prefix, void* stream)
   p.err = a->err_word;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool bf16 = a->dtype == MD_BF16;
-  const int rc = md::status(md::launch_prefix_attn(p, pl.n_wgs, a->head_dim, bf16, s));
+  const int rc = md::status(md::launch_prefix_attn(p, pl, a->head_dim, bf16, s));
   if (rc != MD_OK) return rc;
   return md::status(md::launch_merge_lse(pl.c_pre + pl.c_own, pl.n_rows, a->head_dim, bf16, p.part_o,
                                          p.part_lse, a->o, a->lse, s, true));

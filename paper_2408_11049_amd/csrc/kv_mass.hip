@@ -125,11 +125,12 @@ mass_step(const MassParams p) {
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = uniform(tid >> 6);
-  const int units = p.B * p.Hkv;
-  const int unit = static_cast<int>(blockIdx.x) % units, kb = static_cast<int>(blockIdx.x) / units;
-  const int hk = unit % p.Hkv, b = unit / p.Hkv;
+  // The heads of a block of keys on one XCD, one after another: they share its token rows.
+  const int x8 = static_cast<int>(blockIdx.x) >> 3;
+  const int v = x8 / p.Hkv * 8 + (static_cast<int>(blockIdx.x) & 7);
+  const int hk = x8 % p.Hkv, b = v % p.B, kb = v / p.B, unit = b * p.Hkv + hk;
   const int S = min(max(p.c.lens[b], 0), p.c.max_len);
-  const int key_first = kb * 128;
+  const int key_first = kb * kMassStepKeys;
   if (key_first >= S) return;
   const int base = S - p.L;  // the key that row 0 sits at (below 0: a length shorter than L)
   u32x4 kr[KP];

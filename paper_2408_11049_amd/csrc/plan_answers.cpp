@@ -102,24 +102,28 @@ int check_prefix_sizes(const md_attn_args* a, const md_prefix* p) {
 
 PrefixPlan make_prefix_plan(const md_attn_args* a, const md_prefix* p, int num_cus) {
   PrefixPlan pl;
-  const int64_t cus = num_cus > 0 ? num_cus : 256, slots = 2 * cus;
+  const int64_t cus = num_cus > 0 ? num_cus : 256;
   const int64_t G = a->num_q_heads / a->num_kv_heads;
-  const int64_t tile = kPrefixTile(a->dtype == MD_BF16);
   pl.n_rows = static_cast<int64_t>(a->num_seqs) * a->q_len * a->num_q_heads;
   pl.group_rows = static_cast<int32_t>(a->num_seqs / p->num_prefixes * a->q_len * G);
-  pl.row_blocks = static_cast<int32_t>(ceil_div(pl.group_rows, kPrefixRows));
+  pl.wide = a->dtype == MD_BF16 && pl.group_rows > kPrefixFewRows && p->max_len > 0 &&
+            (p->page_size == 0 || p->page_size >= kPrefixWidePage(a->head_dim));
+  pl.row_blocks = static_cast<int32_t>(ceil_div(pl.group_rows, pl.wide ? kPrefixWideRows : kPrefixStreamRows));
+  pl.own_blocks = static_cast<int32_t>(ceil_div(G * a->q_len, kPrefixStreamRows));
   const int64_t heads = static_cast<int64_t>(p->num_prefixes) * a->num_kv_heads;
-  const int64_t units = heads * pl.row_blocks, own = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads;
-  // Parts of a range: enough workgroups to fill the device, at least two tiles a part.
-  auto parts = [&](int64_t len, int64_t n) {
-    const int64_t most = ceil_div(ceil_div(len, tile), 2);
-    return static_cast<int32_t>(std::max<int64_t>(1, std::min(slots / std::max<int64_t>(n, 1), most)));
+  const int64_t units = heads * pl.row_blocks;
+  const int64_t own = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads * pl.own_blocks;
+  // Parts of a range: enough workgroups to fill the device's places, at least two tiles a part.
+  auto parts = [&](int64_t len, int64_t n, int64_t places, int64_t least) {
+    const int64_t most = ceil_div(len, least);
+    return static_cast<int32_t>(std::max<int64_t>(1, std::min(places / std::max<int64_t>(n, 1), most)));
   };
-  pl.c_pre = parts(p->max_len, units);
-  pl.c_own = parts(a->max_kv_len, own);
+  const int64_t k1 = env_knob("MD_C_PRE", 1, 512), k2 = env_knob("MD_C_OWN", 1, 512);
+  pl.c_pre = k1 ? k1 : parts(p->max_len, units, pl.wide ? cus : 2 * cus, 128);
+  pl.c_own = k2 ? k2 : parts(a->max_kv_len, own, 4 * cus, 128);
   pl.n_pre = static_cast<int32_t>(ceil_div(heads * pl.c_pre, 8) * 8 * pl.row_blocks);
   if (p->max_len == 0) pl.c_pre = pl.n_pre = 0;
-  pl.n_wgs = pl.n_pre + own * pl.c_own;
+  pl.n_own = ceil_div(static_cast<int64_t>(a->num_seqs) * pl.c_own, 8) * 8 * a->num_kv_heads * pl.own_blocks;
   const size_t n = static_cast<size_t>(pl.c_pre + pl.c_own) * static_cast<size_t>(pl.n_rows);
   pl.part_o_bytes = align_up(n * a->head_dim * 4, 256);
   pl.part_lse_bytes = align_up(n * 4, 256);
@@ -148,7 +152,7 @@ int validate_prefix(const md_attn_args* a, const md_prefix* p, PrefixPlan* plan)
       !rows_ok(geom(p), a->num_kv_heads, a->head_dim, a->dtype))
     return MD_ERR_INVALID_ARG;
   *plan = make_prefix_plan(a, p, device_cu_count());
-  if (plan->n_wgs > kMaxWgs256) return MD_ERR_UNSUPPORTED;
+  if (plan->n_pre + plan->n_own > kMaxWgs256) return MD_ERR_UNSUPPORTED;
   if (!a->workspace || a->workspace_bytes < plan->workspace_bytes || !aligned(a->workspace, 256))
     return MD_ERR_WORKSPACE;
   return MD_OK;
@@ -180,7 +184,8 @@ MassPlan make_mass_plan(const md_kv_mass_args* a, int num_cus) {
   pl.part_rows = static_cast<int32_t>(rows);
   pl.prompt = rows > kMassStepRows;
   if (!pl.prompt) {
-    pl.n_wgs = units * ceil_div(a->max_kv_len, kMassStepKeys);
+    // Whole rounds of the XCDs, which take all heads of a block of keys (see kv_mass.hip).
+    pl.n_wgs = ceil_div(a->num_seqs * ceil_div(a->max_kv_len, kMassStepKeys), 8) * 8 * a->num_kv_heads;
     return pl;
   }
   const int64_t blocks = units * ceil_div(a->max_kv_len, kMassPromptKeys);
