@@ -2,9 +2,8 @@
 // head) the n - budget tokens of least weight go, and the tokens kept behind the budget move
 // into the slots that this frees.
 //
-// One workgroup a (sequence, KV head) finds the key of rank n - budget by a radix select (four
-// rounds of 8 bits over weights that stay in the caches), counts in slot order and lists
-// (freed slot, kept slot) pairs; pairs are moved by the same workgroup or, where a call may have
+// One workgroup a (sequence, KV head) finds the key of rank n - budget by a radix select (three
+// rounds over keys in LDS), counts in slot order and lists (freed slot, kept slot) pairs; pairs are moved by the same workgroup or, where a call may have
 // more than kEvictFused of them a head, by a second launch over the whole device.
 #include "answers_kernels.h"
 
@@ -24,13 +23,10 @@ struct EvictUnit {
 };
 
 // The order of a slot's token: its weight's, NaN least, held tokens last.
-__device__ __forceinline__ uint32_t order_key(const EvictUnit& u, int j) {
-  const int pos = u.pos[j];
-  const float w = u.mass[j] + 0.f;  // -0 and 0 are equal
-  if (pos < u.n_sink || pos >= u.recent_from) return kHeld;
-  const uint32_t x = __float_as_uint(w);
-  if (w != w) return 0u;
-  return (x >> 31) ? ~x : x | 0x80000000u;
+__device__ __forceinline__ uint32_t order_key(const EvictUnit& u, int pos, float mass) {
+  const uint32_t x = __float_as_uint(mass + 0.f);  // -0 and 0 are equal
+  const uint32_t key = mass != mass ? 0u : ((x >> 31) ? ~x : x | 0x80000000u);
+  return pos < u.n_sink || pos >= u.recent_from ? kHeld : key;
 }
 
 // Byte offset of a token's row of head hk, or -1: on no page of the pool.
@@ -64,14 +60,18 @@ __device__ __forceinline__ void move_vector(const EvictParams& p, int unit, int2
   }
 }
 
-template <int NT>
+// NT threads; the order of the first KEYS slots is kept in LDS (of more, it is made from memory every
+// time).
+template <int NT, int KEYS>
 __global__ void __launch_bounds__(NT)
 evict_select(const EvictParams p) {
-  constexpr int NW = NT / 64;
-  __shared__ uint32_t hist[256];
+  constexpr int NW = NT / 64, BINS = 2048;
+  __shared__ uint32_t hist[BINS];
   __shared__ int counts[3][NW];
   __shared__ uint32_t pick[2];
-  __shared__ int2 listed[kEvictFused];
+  __shared__ uint32_t keys[KEYS];
+  int2* const listed = reinterpret_cast<int2*>(hist);  // after the select
+  static_assert(sizeof(hist) >= sizeof(int2) * kEvictFused, "the pairs take the histogram's place");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int unit = blockIdx.x, b = unit / p.Hkv;
   const int n = min(max(p.lens[b], 0), p.slots);
@@ -83,32 +83,59 @@ evict_select(const EvictParams p) {
   const int64_t s0 = static_cast<int64_t>(unit) * p.slot_stride;
   const EvictUnit u = {p.mass + s0, p.slot_pos + s0, p.n_sink,
                        static_cast<int64_t>(p.seq_lens[b]) - p.recent};
+  for (int j0 = 0; j0 < min(n, KEYS); j0 += 8 * NT) {
+    int pos[8];
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = min(j0 + i * NT + tid, n - 1);
+      pos[i] = u.pos[j];
+      w[i] = u.mass[j];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int j = j0 + i * NT + tid;
+      if (j < min(n, KEYS)) keys[j] = order_key(u, pos[i], w[i]);
+    }
+  }
+  auto key_of = [&](int j) { return j < KEYS ? keys[j] : order_key(u, u.pos[j], u.mass[j]); };
 
-  // The key of rank n - budget (from 1), eight bits a round: of the keys that agree with `prefix`
-  // in the bits above, `want` is the rank looked for.
+  // The key of rank n - budget (from 1), 11, 11 and 10 bits a round (weights spread over few exponents, and
+  // atomics on one bin take turns: with the upper 8 bits alone they took longer than the rest): of the
+  // keys that agree with `prefix` in the bits above, `want` is the rank looked for.
   uint32_t prefix = 0;
   int want = n - p.budget;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += NT) hist[i] = 0;
+#pragma unroll
+  for (int round = 0; round < 3; ++round) {
+    const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
+    for (int i = tid; i < BINS; i += NT) hist[i] = 0;
     __syncthreads();
     for (int j = tid; j < n; j += NT) {
-      const uint32_t key = order_key(u, j);
-      if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8)))
-        atomicAdd(&hist[(key >> shift) & 255u], 1u);
+      const uint32_t key = key_of(j);
+      if (round == 0 || (key >> (shift + bits)) == (prefix >> (shift + bits)))
+        atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1u)], 1u);
     }
     __syncthreads();
-    if (wave == 0) {  // each lane four bins; the bin in which the running count reaches `want`
-      uint32_t h[4], mine = 0;
-      for (int i = 0; i < 4; ++i) mine += h[i] = hist[lane * 4 + i];
-      uint32_t incl = mine;
+    // The bin in which the running count reaches `want`: 256 threads of eight bins each.
+    uint32_t h[8], mine = 0, incl = 0;
+    if (tid < 256) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mine += h[i] = hist[tid * 8 + i];
+      incl = mine;
       for (int o = 1; o < 64; o <<= 1) {
         const uint32_t x = __shfl_up(incl, o);
         if (lane >= o) incl += x;
       }
+      if (lane == 63) counts[0][wave] = static_cast<int>(incl);
+    }
+    __syncthreads();
+    if (tid < 256) {
       uint32_t run = incl - mine;
-      for (int i = 0; i < 4; ++i) {
+      for (int x = 0; x < wave; ++x) run += static_cast<uint32_t>(counts[0][x]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
         if (run < static_cast<uint32_t>(want) && static_cast<uint32_t>(want) <= run + h[i]) {
-          pick[0] = lane * 4 + i;
+          pick[0] = tid * 8 + i;
           pick[1] = want - run;
         }
         run += h[i];
@@ -117,7 +144,6 @@ evict_select(const EvictParams p) {
     __syncthreads();
     prefix |= pick[0] << shift;
     want = static_cast<int>(pick[1]);
-    __syncthreads();
   }
   // Evicted: keys below `prefix`, and the first `want` slots whose key is `prefix`.
 
@@ -126,8 +152,9 @@ evict_select(const EvictParams p) {
   int ties = 0;
   for (int j0 = lo; j0 < hi; j0 += 64) {
     const int j = j0 + lane;
-    ties += __popcll(__ballot(j < hi && order_key(u, j) == prefix));
+    ties += __popcll(__ballot(j < hi && key_of(min(j, n - 1)) == prefix));
   }
+  __syncthreads();
   if (lane == 0) counts[0][wave] = ties;
   __syncthreads();
   int tie0 = 0;
@@ -138,7 +165,7 @@ evict_select(const EvictParams p) {
     int tie = tie0, holes = 0, extras = 0;
     for (int j0 = lo; j0 < hi; j0 += 64) {
       const int j = j0 + lane;
-      const uint32_t key = j < hi ? order_key(u, j) : kHeld;
+      const uint32_t key = j < hi ? key_of(j) : kHeld;
       const unsigned long long eq = __ballot(j < hi && key == prefix);
       const bool out = j < hi && (key < prefix || (key == prefix && tie + __popcll(eq & below) < want));
       tie += __popcll(eq);
@@ -195,9 +222,9 @@ evict_move(const EvictParams p) {
 hipError_t launch_kv_evict(const EvictParams& p, hipStream_t s) {
   const uint32_t units = static_cast<uint32_t>(p.B) * static_cast<uint32_t>(p.Hkv);
   if (p.slots <= 4096)
-    hipLaunchKernelGGL((evict_select<256>), dim3(units), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((evict_select<256, 4096>), dim3(units), dim3(256), 0, s, p);
   else
-    hipLaunchKernelGGL((evict_select<1024>), dim3(units), dim3(1024), 0, s, p);
+    hipLaunchKernelGGL((evict_select<1024, 32768>), dim3(units), dim3(1024), 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.counts) return e;
   const uint32_t y = units >= 2048 ? 1 : (2048 + units - 1) / units;

@@ -1,13 +1,13 @@
 // logprobs.hip -- per row of logits: the log probability of a given token, the entropy and
 // the top_k most likely tokens, from one pass over the row.
 //
-// A workgroup takes a segment of a row, 256 lanes holding 16 or 64 logits each in
+// A workgroup takes a segment of a row, 256 lanes holding 16 or 32 logits each in
 // registers at a time.  Sums: each lane keeps a maximum m, z = sum exp(x - m) and
 // t = sum exp(x - m) (x - m); lse = m + ln z, entropy = ln z - t / z.  Differences to the maximum
 // are taken before the scaling to log2, so that large logits lose nothing.
-// Top tokens: the top_k-th largest of a wave's 64 lane maxima is below no more than top_k of its
-// logits, so only logits from there on are candidates, hardly more than top_k of them; they go to
-// a list in LDS, which is cut to its best top_k where it would overflow (rows of equal
+// Top tokens: with each wave's (top_k / 4)-th largest lane maximum, the least of the four is below
+// top_k logits at least, so only logits from there on are candidates, some twice top_k of them; they go
+// to a list in LDS, which is cut to its best top_k where it would overflow (rows of equal
 // or clustered values).  Candidates are ranked by counting the better ones.
 // Rows of several segments are joined by a second launch.
 #include <float.h>
@@ -53,11 +53,26 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
   // exp(x - m) (x - m) = f exp(x - a.m) ((x - a.m) + da)
   return Stats{m, a.z * fa + b.z * fb, fa * (a.t + a.z * da) + fb * (b.t + b.z * db)};
 }
-__device__ __forceinline__ Stats wave_join(Stats s) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1)
-    s = join(s, Stats{__shfl_xor(s.m, o), __shfl_xor(s.z, o), __shfl_xor(s.t, o)});
-  return s;
+// A reduction over the wave by DPP moves: within rows of 16, then over the rows; all lanes get it.
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float x, float none, F f) {
+  const int id = __float_as_int(none);
+#define MD_STEP(ctrl, rows) \
+  x = f(x, __int_as_float(__builtin_amdgcn_update_dpp(id, __float_as_int(x), ctrl, rows, 0xf, false)))
+  MD_STEP(0x111, 0xf);  // row_shr 1, 2, 4, 8
+  MD_STEP(0x112, 0xf);
+  MD_STEP(0x114, 0xf);
+  MD_STEP(0x118, 0xf);
+  MD_STEP(0x142, 0xa);  // the last lane of rows 0 and 2 to rows 1 and 3,
+  MD_STEP(0x143, 0xc);  // of row 1 to rows 2 and 3
+#undef MD_STEP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+__device__ __forceinline__ Stats wave_join(const Stats& s) {
+  const float m = wave_reduce(s.m, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+  const Stats at = join(s, Stats{m, 0.f, 0.f});  // each lane's sums under the common maximum
+  auto add = [](float a, float b) { return a + b; };
+  return Stats{m, wave_reduce(at.z, 0.f, add), wave_reduce(at.t, 0.f, add)};
 }
 
 struct Finals {
@@ -231,7 +246,7 @@ logprobs_kernel(const LogpParams p) {
 #pragma unroll
     for (int e = 0; e < PL; ++e) mx = fmaxf(mx, x[e]);
     {
-      const float m = fmaxf(st.m, mx), m_use = m == -INFINITY ? 0.f : m;
+      const float m_use = mx == -INFINITY ? 0.f : mx;
       float z[4] = {}, t[4] = {};
 #pragma unroll
       for (int e = 0; e < PL; ++e) {
@@ -244,22 +259,28 @@ logprobs_kernel(const LogpParams p) {
     }
 
     if (K > 0) {
-      // The K-th largest lane maximum, in the upper 16 bits of its order (rounded down, which a lower
-      // bound may be): bit by bit, whether K lanes still reach it.
-      const uint32_t mb = __float_as_uint(mx);
-      const uint32_t key = (mb >> 31) ? ~mb : mb | 0x80000000u;
-      uint32_t kth = 0;
+      if (c0 == seg0) {
+        // A bound below no more than K of the logits: of a whole segment the least, over the waves, of each
+        // wave's (K / 4)-th largest lane maximum, else the largest of each one's K-th.  In the upper 16
+        // bits of its order (rounded down, as a lower bound may be), bit by bit: whether enough lanes still
+        // reach it.
+        const bool whole = c0 + 256 * PL <= seg1;
+        const int count = whole ? (K + 3) / 4 : K;
+        const uint32_t key = order(mx);
+        uint32_t kth = 0;
 #pragma unroll
-      for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t trial = kth | (1u << bit);
-        if (__popcll(__ballot(key >= trial)) >= K) kth = trial;
-      }
-      if (kth > 0x007fffffu) {  // above the order of -inf
-        const float bound = __uint_as_float((kth >> 31) ? kth & 0x7fffffffu : ~kth);
-        if (bound > list.floor) {
-          list.floor = bound;
-          list.floor_key = 0;
+        for (int bit = 31; bit >= 16; --bit) {
+          const uint32_t trial = kth | (1u << bit);
+          if (__popcll(__ballot(key >= trial)) >= count) kth = trial;
         }
+        if (lane == 0) l_n[wave] = static_cast<int>(kth >> 1);  // in 31 bits, for signed comparisons
+        __syncthreads();
+        const int lo = min(min(l_n[0], l_n[1]), min(l_n[2], l_n[3]));
+        const int hi = max(max(l_n[0], l_n[1]), max(l_n[2], l_n[3]));
+        kth = static_cast<uint32_t>(whole ? lo : hi) << 1;
+        if (kth > 0x007fffffu)  // above the order of -inf
+          list.floor = __uint_as_float((kth >> 31) ? kth & 0x7fffffffu : ~kth);
+        if (list.floor != list.floor) list.floor = -INFINITY;
       }
       // Without a bound, everything above -inf.
       const float least = fmaxf(list.floor, -FLT_MAX);
@@ -284,8 +305,8 @@ logprobs_kernel(const LogpParams p) {
           push(list, v >= least && k > list.floor_key, k, K, lane);
         }
       }
-      // Fewer than K above -inf so far: tokens of -inf and NaN count too, by index.
-      for (int v = 0; v < NV && list.n < K && at(wave0, v, 0) - lane * VN < seg1; ++v)
+      // No bound, and fewer than K above -inf so far: tokens of -inf and NaN count too, by index.
+      for (int v = 0; list.floor == -INFINITY && v < NV && list.n < K && at(wave0, v, 0) - lane * VN < seg1; ++v)
         for (int j = 0; j < VN; ++j) {
           const int i = at(wave0, v, j);
           const bool none = i < seg1 && !(logit<BF16>(p.logits, row0 + i) > -INFINITY);
@@ -401,8 +422,8 @@ logprobs_join_kernel(const LogpParams p) {
 hipError_t launch_token_logprobs(const LogpParams& p, const LogpPlan& pl, bool bf16, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>(p.rows) * p.n_segs)), block(256);
 #define MD_LOGP(BF, PL) hipLaunchKernelGGL((logprobs_kernel<BF, PL>), grid, block, 0, s, p)
-  if (pl.per_lane == 64) {
-    if (bf16) MD_LOGP(true, 64); else MD_LOGP(false, 64);
+  if (pl.per_lane == 32) {
+    if (bf16) MD_LOGP(true, 32); else MD_LOGP(false, 32);
   } else {
     if (bf16) MD_LOGP(true, 16); else MD_LOGP(false, 16);
   }

@@ -310,9 +310,10 @@ int check_logp_sizes(int64_t rows, int32_t vocab, int64_t row_stride, int32_t dt
 LogpPlan make_logp_plan(int64_t rows, int32_t vocab, int32_t top_k, int num_cus) {
   LogpPlan pl;
   const int64_t cus = num_cus > 0 ? num_cus : 256;
-  // A lane holds 64 logits, 16 where that leaves compute units without work.
-  pl.per_lane = rows * ceil_div(vocab, 64 * 256) >= cus ? 64 : 16;
-  const int64_t at_once = pl.per_lane * 256;
+  // Segments of 16384 logits, 32 a lane twice; of 4096 where that leaves compute units without work.
+  const bool many = rows * ceil_div(vocab, 64 * 256) >= cus;
+  pl.per_lane = many ? 32 : 16;
+  const int64_t at_once = many ? 64 * 256 : 16 * 256;
   // Up to 256 segments a row, fewer where the grid's 32 bits would end.
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256, kMaxWgs256 / std::max<int64_t>(rows, 1)));
   pl.seg_len = static_cast<int32_t>(at_once * ceil_div(ceil_div(vocab, at_once), most));
