@@ -14,6 +14,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 namespace {
 
 constexpr uint32_t kHeld = 0xffffffffu;  // sinks and recent tokens: above every weight
+constexpr int kFew = 8;                  // tokens that go one after another rather than by a select
 
 struct EvictUnit {
   const float* mass;
@@ -41,6 +42,27 @@ __device__ __forceinline__ int64_t row_offset(const EvictParams& p, int b, int h
     off = static_cast<int64_t>(b) * p.c.s_blk + static_cast<int64_t>(j) * p.c.s_tok;
   }
   return (off + static_cast<int64_t>(hk) * p.c.s_head) * p.esize;
+}
+
+// The least pair over the wave, by DPP moves; all lanes get it.
+__device__ __forceinline__ unsigned long long wave_least(unsigned long long x) {
+#define MD_STEP(ctrl, rows)                                                                          \
+  do {                                                                                               \
+    const uint32_t lo = __builtin_amdgcn_update_dpp(-1, static_cast<int>(x), ctrl, rows, 0xf, false);  \
+    const uint32_t hi = __builtin_amdgcn_update_dpp(-1, static_cast<int>(x >> 32), ctrl, rows, 0xf, false); \
+    const unsigned long long y = (static_cast<unsigned long long>(hi) << 32) | lo;                   \
+    x = y < x ? y : x;                                                                               \
+  } while (0)
+  MD_STEP(0x111, 0xf);  // within rows of 16: row_shr 1, 2, 4, 8
+  MD_STEP(0x112, 0xf);
+  MD_STEP(0x114, 0xf);
+  MD_STEP(0x118, 0xf);
+  MD_STEP(0x142, 0xa);  // the last lane of rows 0 and 2 to rows 1 and 3,
+  MD_STEP(0x143, 0xc);  // of row 1 to rows 2 and 3
+#undef MD_STEP
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(x), 63);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), 63);
+  return (static_cast<unsigned long long>(hi) << 32) | lo;
 }
 
 // One 16-byte vector of a pair's K or V row (item: pair, then K or V, then the vector); the first of
@@ -100,6 +122,55 @@ evict_select(const EvictParams p) {
   }
   auto key_of = [&](int j) { return j < KEYS ? keys[j] : order_key(u, u.pos[j], u.mass[j]); };
 
+  const int vecs = 2 * p.row_vecs;
+  if (n - p.budget <= kFew && n <= KEYS) {
+    // A step's few tokens: the least (key, slot) pair above the last one found, one after another
+    // (up to six of 2055 tokens in 512 heads: 10.0 us a call so, 17.8 by the select and its scans).
+    __shared__ unsigned long long least[2][NW];
+    const int m = n - p.budget;
+    unsigned long long last = 0;  // below every pair, as slots are counted from 1 in them
+    int gone[kFew];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) {
+      gone[i] = INT32_MAX;
+      if (i >= m) continue;
+      unsigned long long mine = ~0ull;
+      for (int j = tid; j < n; j += NT) {
+        const unsigned long long x = (static_cast<unsigned long long>(keys[j]) << 32) | static_cast<uint32_t>(j + 1);
+        if (x > last && x < mine) mine = x;
+      }
+      mine = wave_least(mine);
+      if (lane == 0) least[i & 1][wave] = mine;
+      __syncthreads();
+      last = least[i & 1][0];
+      for (int x = 1; x < NW; ++x) last = least[i & 1][x] < last ? least[i & 1][x] : last;
+      gone[i] = static_cast<int>(static_cast<uint32_t>(last)) - 1;
+    }
+    // The kept slots behind the budget, in order, take the freed ones below it, in order.
+    if (tid == 0) {
+      int total = 0, at = -1;
+      for (int j = p.budget; j < n; ++j) {
+        bool out = false;
+        int next = INT32_MAX;  // the least freed slot above the last one taken
+#pragma unroll
+        for (int i = 0; i < kFew; ++i) {
+          out |= gone[i] == j;
+          if (gone[i] > at && gone[i] < next) next = gone[i];
+        }
+        if (out) continue;
+        listed[total++] = make_int2(next, j);
+        at = next;
+      }
+      counts[0][0] = total;
+    }
+    __syncthreads();
+    const int total = counts[0][0];
+    if (p.counts && tid == 0) p.counts[unit] = 0;  // moved here
+    for (int x = tid; x < total * vecs; x += NT) move_vector(p, unit, listed[x / vecs], x % vecs);
+    return;
+  }
+
   // The key of rank n - budget (from 1), 11, 11 and 10 bits a round (weights spread over few exponents, and
   // atomics on one bin take turns: with the upper 8 bits alone they took longer than the rest): of the
   // keys that agree with `prefix` in the bits above, `want` is the rank looked for.
@@ -147,62 +218,66 @@ evict_select(const EvictParams p) {
   }
   // Evicted: keys below `prefix`, and the first `want` slots whose key is `prefix`.
 
-  // Each wave takes a run of slots; what comes before it is counted first.
-  const int per = (n + NW - 1) / NW, lo = min(n, wave * per), hi = min(n, lo + per);
-  int ties = 0;
+  // Each wave takes a run of slots and counts, below and from the budget on, those that go by their key,
+  // those that stay, and those with the key `prefix`.
+  const int per = (n + NW * 64 - 1) / (NW * 64) * 64, lo = min(n, wave * per), hi = min(n, lo + per);
+  int holes = 0, extras = 0, ties_low = 0, ties_high = 0;
   for (int j0 = lo; j0 < hi; j0 += 64) {
     const int j = j0 + lane;
-    ties += __popcll(__ballot(j < hi && key_of(min(j, n - 1)) == prefix));
+    const bool in = j < hi, low = j < p.budget;
+    const uint32_t key = key_of(min(j, n - 1));
+    holes += __popcll(__ballot(in && low && key < prefix));
+    extras += __popcll(__ballot(in && !low && key > prefix));
+    ties_low += __popcll(__ballot(in && low && key == prefix));
+    ties_high += __popcll(__ballot(in && !low && key == prefix));
   }
   __syncthreads();
-  if (lane == 0) counts[0][wave] = ties;
+  if (lane == 0) counts[0][wave] = ties_low + ties_high;
   __syncthreads();
   int tie0 = 0;
   for (int x = 0; x < wave; ++x) tie0 += counts[0][x];
-  const unsigned long long below = (1ull << lane) - 1;
-  // Calls f(j, freed, moved, rank of its kind within this wave) over the wave's slots.
-  auto scan = [&](auto f) {
-    int tie = tie0, holes = 0, extras = 0;
-    for (int j0 = lo; j0 < hi; j0 += 64) {
-      const int j = j0 + lane;
-      const uint32_t key = j < hi ? key_of(j) : kHeld;
-      const unsigned long long eq = __ballot(j < hi && key == prefix);
-      const bool out = j < hi && (key < prefix || (key == prefix && tie + __popcll(eq & below) < want));
-      tie += __popcll(eq);
-      const bool hole = out && j < p.budget, extra = j < hi && !out && j >= p.budget;
-      const unsigned long long hm = __ballot(hole), em = __ballot(extra);
-      f(j, hole, extra, hole ? holes + __popcll(hm & below) : extras + __popcll(em & below));
-      holes += __popcll(hm);
-      extras += __popcll(em);
-    }
-    return make_int2(holes, extras);
-  };
-  const int2 mine = scan([](int, bool, bool, int) {});
+  // Of this wave's ties the first `go` go.
+  const int go = min(max(want - tie0, 0), ties_low + ties_high);
+  holes += min(go, ties_low);
+  extras += ties_high - max(go - ties_low, 0);
   if (lane == 0) {
-    counts[1][wave] = mine.x;
-    counts[2][wave] = mine.y;
+    counts[1][wave] = holes;
+    counts[2][wave] = extras;
   }
   __syncthreads();
-  int hole0 = 0, extra0 = 0, total = 0;
+  int hole = 0, extra = 0, total = 0, tie = tie0;
   for (int x = 0; x < NW; ++x) {
     if (x < wave) {
-      hole0 += counts[1][x];
-      extra0 += counts[2][x];
+      hole += counts[1][x];
+      extra += counts[2][x];
     }
     total += counts[1][x];
   }
-  // As many slots are freed below the budget as tokens are kept behind it.
+  // As many slots are freed below the budget as tokens are kept behind it: the x-th takes the x-th.
   int2* const pairs = p.counts ? p.moves + static_cast<int64_t>(unit) * p.max_moves : listed;
-  scan([&](int j, bool hole, bool extra, int rank) {
-    if (hole) pairs[hole0 + rank].x = j;
-    if (extra) pairs[extra0 + rank].y = j;
-  });
+  auto before = [](unsigned long long m) {  // lanes of m before this one
+    return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32),
+                                                      __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0u)));
+  };
+  for (int j0 = lo; j0 < hi; j0 += 64) {
+    const int j = j0 + lane;
+    const bool in = j < hi;
+    const uint32_t key = key_of(min(j, n - 1));
+    const unsigned long long eq = __ballot(in && key == prefix);
+    const bool out = key < prefix || (key == prefix && tie + before(eq) < want);
+    tie += __popcll(eq);
+    const bool is_hole = in && out && j < p.budget, is_extra = in && !out && j >= p.budget;
+    const unsigned long long hm = __ballot(is_hole), em = __ballot(is_extra);
+    if (is_hole) pairs[hole + before(hm)].x = j;
+    if (is_extra) pairs[extra + before(em)].y = j;
+    hole += __popcll(hm);
+    extra += __popcll(em);
+  }
   if (p.counts) {
     if (tid == 0) p.counts[unit] = total;
     return;
   }
   __syncthreads();
-  const int vecs = 2 * p.row_vecs;
   for (int x = tid; x < total * vecs; x += NT) move_vector(p, unit, listed[x / vecs], x % vecs);
 }
 
