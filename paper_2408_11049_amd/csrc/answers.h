@@ -34,10 +34,12 @@ PrefixPlan make_prefix_plan(const md_attn_args* a, const md_prefix* p, int num_c
 size_t prefix_workspace_need(const md_attn_args* a, const md_prefix* p, int num_cus);
 int validate_prefix(const md_attn_args* a, const md_prefix* p, PrefixPlan* plan);
 
-// Accumulated weights: keys of a workgroup; more rows than kMassStepRows a KV head are a prompt's.
-constexpr int kMassStepKeys = 128, kMassPromptKeys = 256, kMassStepRows = 128;
+// Accumulated weights: more rows than kMassStepRows a KV head are a prompt's, whose workgroups take
+// kMassPromptKeys keys each.
+constexpr int kMassPromptKeys = 256, kMassStepRows = 128;
 struct MassPlan {
   bool prompt = false;
+  int32_t key_parts = 1;    // of a sequence, a step's
   int32_t row_parts = 1;    // parts of part_rows rows; the workspace holds each part's weights
   int32_t part_rows = 0;
   int64_t n_wgs = 0, reduce_wgs = 0;

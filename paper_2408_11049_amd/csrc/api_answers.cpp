@@ -101,6 +101,7 @@ int md_kv_mass(const md_kv_mass_args* a, void* stream) {
   p.Hq = a->num_q_heads;
   p.Hkv = a->num_kv_heads;
   p.G = a->num_q_heads / a->num_kv_heads;
+  p.key_parts = pl.key_parts;
   p.row_parts = pl.row_parts;
   p.part_rows = pl.part_rows;
   p.parts = static_cast<float*>(a->workspace);

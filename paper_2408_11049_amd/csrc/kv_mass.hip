@@ -13,29 +13,17 @@
 //   mass_prompt  many rows (a prompt's): bound by the matrix and vector units alike.  The rows are
 //                cut into parts, whose sums mass_reduce adds, so that early keys, which
 //                most rows see, are no longer work than late ones.
-#include "answers_kernels.h"
+#include "kv_stream.h"
 
 namespace md {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-template <int D, bool BF16>
-struct Row {
-  static constexpr int ES = BF16 ? 2 : 4, BYTES = D * ES, CH = BYTES / 16, ST = CH / 2;
-  // LDS rows unpadded, chunk c of row r in place c ^ turn(r): see the shared-prefix attention.
-  static __device__ __forceinline__ int at(int r, int c) {
-    const int turn = BYTES == 128 ? (r >> 1) & 7 : r & 15;
-    return r * BYTES + ((c ^ turn) << 4);
-  }
-};
 
 // Byte offset of a key's row, or -1: no token of the pool.
 __device__ __forceinline__ int64_t key_offset(const MassParams& p, int b, int hk, int key, int es) {
@@ -69,7 +57,7 @@ __device__ __forceinline__ f32x16 scores(const u32x4 (&q)[D * (BF16 ? 2 : 4) / 3
                                          const u32x4 (&k)[D * (BF16 ? 2 : 4) / 32]) {
   f32x16 s = {};
 #pragma unroll
-  for (int st = 0; st < Row<D, BF16>::ST; ++st) {
+  for (int st = 0; st < Tile<D, BF16>::CH / 2; ++st) {
     if constexpr (BF16) {
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q[st]),
                                                   __builtin_bit_cast(bf16x8, k[st]), s, 0, 0, 0);
@@ -103,87 +91,90 @@ __device__ __forceinline__ float weigh(const f32x16& s, const float* nl, float s
   return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__device__ __forceinline__ void store(const MassParams& p, int unit, int b, int key, int base, float w) {
+// w onto the token's weight so far; a newest token has none.
+__device__ __forceinline__ void store(const MassParams& p, int unit, int b, int key, int base, float w,
+                                      float old) {
   const int64_t slot = static_cast<int64_t>(unit) * p.slot_stride + key;
-  if (key >= base) {  // a newest token
-    p.mass[slot] = w;
-    p.slot_pos[slot] = p.pos0[b] + (key - base);
-  } else {
-    p.mass[slot] += w;
-  }
+  p.mass[slot] = key >= base ? w : old + w;
+  if (key >= base) p.slot_pos[slot] = p.pos0[b] + (key - base);
 }
 
-// Up to kMassStepRows rows, all in LDS at once; 128 keys a workgroup, 32 a wave.
-template <int D, bool BF16>
+// Up to RT tiles of 32 rows, in LDS for the whole call; each wave streams its own tiles of 32 keys of a
+// part of the sequence, the next one on its way while one is weighed.
+template <int D, bool BF16, int RT>
 __global__ void __launch_bounds__(256)
+__attribute__((amdgpu_waves_per_eu(D == 128 && !BF16 ? 1 : 2)))
 mass_step(const MassParams p) {
-  using T = Row<D, BF16>;
-  constexpr int KP = 128 * T::CH / 256;  // chunks of the keys a thread moves
-  __shared__ __attribute__((aligned(16))) unsigned char kt[128 * T::BYTES];
-  __shared__ __attribute__((aligned(16))) unsigned char qt[32 * T::BYTES];
-  __shared__ __attribute__((aligned(16))) float nl[32];
+  using T = Tile<D, BF16>;
+  constexpr int ST = T::CH / 2;
+  __shared__ __attribute__((aligned(16))) unsigned char kt[4][32 * T::ROW];
+  __shared__ __attribute__((aligned(16))) unsigned char qt[RT * 32 * T::ROW];
+  __shared__ __attribute__((aligned(16))) float nl[RT * 32];
 
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = uniform(tid >> 6);
-  // The heads of a block of keys on one XCD, one after another: they share its token rows.
+  // The heads of a sequence's part on one XCD, one after another: they share its token rows.
   const int x8 = static_cast<int>(blockIdx.x) >> 3;
-  const int v = x8 / p.Hkv * 8 + (static_cast<int>(blockIdx.x) & 7);
-  const int hk = x8 % p.Hkv, b = v % p.B, kb = v / p.B, unit = b * p.Hkv + hk;
-  const int S = min(max(p.c.lens[b], 0), p.c.max_len);
-  const int key_first = kb * kMassStepKeys;
-  if (key_first >= S) return;
+  const int x = x8 / p.Hkv * 8 + (static_cast<int>(blockIdx.x) & 7);
+  if (x >= p.B * p.key_parts) return;
+  const int hk = x8 % p.Hkv, part = x % p.key_parts, b = x / p.key_parts, unit = b * p.Hkv + hk;
+  const int S = uniform(min(max(p.c.lens[b], 0), p.c.max_len));
+  const int n_tiles = (S + 31) / 32;
+  const int t0 = static_cast<int>(static_cast<int64_t>(n_tiles) * part / p.key_parts);
+  const int t1 = static_cast<int>(static_cast<int64_t>(n_tiles) * (part + 1) / p.key_parts);
+  if (t0 >= t1) return;
   const int base = S - p.L;  // the key that row 0 sits at (below 0: a length shorter than L)
-  u32x4 kr[KP];
-#pragma unroll
-  for (int n = 0; n < KP; ++n) {
-    const int x = n * 256 + tid, key = key_first + x / T::CH;
-    const int64_t off = key < S ? key_offset(p, b, hk, key, T::ES) : -1;
-    // No token: the first row stands in, its weight is not stored (or, on no page of the pool,
-    // unspecified).
-    kr[n] = __builtin_nontemporal_load(
-        reinterpret_cast<const u32x4*>(p.c.k + (off < 0 ? 0 : off) + (x % T::CH) * 16));
-  }
   int n_count = p.L;
-  if (p.accepted) n_count = min(max(p.accepted[b], 0), p.L - 1) + 1;
-  const int r_begin = max(0, key_first - base) * p.G;
+  if (p.accepted) n_count = min(max(uniform(p.accepted[b]), 0), p.L - 1) + 1;
   const int r_end = n_count * p.G;
-  const int key = key_first + wave * 32 + l32;
-  const int r_sees = max(0, key - base) * p.G;  // the first row that sees this lane's key
-  float w = 0.f;
-  u32x4 k[T::ST];
-  for (int r0 = r_begin; r0 < r_end; r0 += 32) {
+
+  Stream<D, BF16, false> rows(p.c, b, hk, S, lane);
+  const int first = t0 + wave;
+  const int block = rows.load_block(first);
+  int block_next = rows.load_block(first + 4);
+  // A token's weight so far comes ahead of its tile: loads return in order, and behind the next tile's
+  // it would hold up this one.
+  const float* const weights = p.mass + static_cast<int64_t>(unit) * p.slot_stride;
+  float old = weights[min(first * 32 + l32, S - 1)];
+  rows.load(first, block);
 #pragma unroll
-    for (int n = 0; n < 32 * T::CH / 256; ++n) {
-      const int x = n * 256 + tid, r = r0 + x / T::CH;
-      u32x4 q = {0, 0, 0, 0};
-      if (r < r_end)
-        q = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(p.q) +
-                                            query_row(p, b, hk, r) * T::BYTES + (x % T::CH) * 16);
-      *reinterpret_cast<u32x4*>(qt + T::at(x / T::CH, x % T::CH)) = q;
-    }
-    if (tid < 32) nl[tid] = neg_lse(p, b, hk, r0 + tid, r_end);
-    if (r0 == r_begin) {
-#pragma unroll
-      for (int n = 0; n < KP; ++n) {
-        const int x = n * 256 + tid;
-        *reinterpret_cast<u32x4*>(kt + T::at(x / T::CH, x % T::CH)) = kr[n];
-      }
-    }
-    __syncthreads();
-    if (r0 == r_begin) {
-#pragma unroll
-      for (int st = 0; st < T::ST; ++st)
-        k[st] = *reinterpret_cast<const u32x4*>(kt + T::at(wave * 32 + l32, 2 * st + half));
-    }
-    u32x4 q[T::ST];
-#pragma unroll
-    for (int st = 0; st < T::ST; ++st)
-      q[st] = *reinterpret_cast<const u32x4*>(qt + T::at(l32, 2 * st + half));
-    w += weigh(scores<D, BF16>(q, k), nl, p.scale_log2, half, true, r_sees - r0);
-    __syncthreads();
+  for (int n = 0; n < RT * 32 * T::CH / 256; ++n) {
+    const int c = n * 256 + tid, r = c / T::CH;
+    u32x4 q = {0, 0, 0, 0};
+    if (r < r_end)
+      q = *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(p.q) +
+                                          query_row(p, b, hk, r) * T::ROW + (c % T::CH) * 16);
+    *reinterpret_cast<u32x4*>(qt + T::at(r, c % T::CH)) = q;
   }
-  w += __shfl_xor(w, 32);
-  if (!half && key < S) store(p, unit, b, key, base, w);
+  if (tid < RT * 32) nl[tid] = neg_lse(p, b, hk, tid, r_end);
+  __syncthreads();
+
+  for (int t = first; t < t1; t += 4) {
+    rows.store(kt[wave], nullptr);
+    const int ahead = rows.load_block(t + 8);
+    const float old_next = weights[min(t * 32 + 128 + l32, S - 1)];
+    rows.load(t + 4, block_next);
+    block_next = ahead;
+    wave_sync();
+    u32x4 k[ST];
+#pragma unroll
+    for (int st = 0; st < ST; ++st)
+      k[st] = *reinterpret_cast<const u32x4*>(kt[wave] + T::at(l32, 2 * st + half));
+    wave_sync();  // the next tile overwrites this one
+    const int key = t * 32 + l32;
+    const int sees = max(0, key - base) * p.G;  // the first row that sees this lane's key
+    float w = 0.f;
+    for (int r0 = 0; r0 < r_end; r0 += 32) {
+      u32x4 q[ST];
+#pragma unroll
+      for (int st = 0; st < ST; ++st)
+        q[st] = *reinterpret_cast<const u32x4*>(qt + T::at(r0 + l32, 2 * st + half));
+      w += weigh(scores<D, BF16>(q, k), nl + r0, p.scale_log2, half, true, sees - r0);
+    }
+    w += __shfl_xor(w, 32);
+    if (!half && key < S) store(p, unit, b, key, base, w, old);
+    old = old_next;
+  }
 }
 
 // A part of the rows, 64 of them in LDS at a time (two such tiles in turn); 256 keys a
@@ -192,9 +183,10 @@ template <int D, bool BF16>
 __global__ void __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(D == 128 && !BF16 ? 1 : 2)))
 mass_prompt(const MassParams p) {
-  using T = Row<D, BF16>;
+  using T = Tile<D, BF16>;
+  constexpr int ST = T::CH / 2;
   constexpr int NR = 64, QP = NR * T::CH / 256;
-  __shared__ __attribute__((aligned(16))) unsigned char qt[2][NR * T::BYTES];
+  __shared__ __attribute__((aligned(16))) unsigned char qt[2][NR * T::ROW];
   __shared__ __attribute__((aligned(16))) float nl[2][NR];
   __shared__ int odd[2];  // the tile has rows that count nothing
 
@@ -217,14 +209,14 @@ mass_prompt(const MassParams p) {
   if (r_begin >= r_end && p.row_parts > 1) return;  // mass_reduce does not ask for it
 
   int key[2], sees[2];
-  u32x4 k[2][T::ST];
+  u32x4 k[2][ST];
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     key[x] = key_first + wave * 64 + x * 32 + l32;
     sees[x] = max(0, min(key[x], S - 1) - base) * p.G;
     const int64_t off = key[x] < S ? key_offset(p, b, hk, key[x], T::ES) : -1;
 #pragma unroll
-    for (int st = 0; st < T::ST; ++st)
+    for (int st = 0; st < ST; ++st)
       k[x][st] = *reinterpret_cast<const u32x4*>(p.c.k + (off < 0 ? 0 : off) + (2 * st + half) * 16);
   }
 
@@ -236,7 +228,7 @@ mass_prompt(const MassParams p) {
     for (int n = 0; n < QP; ++n) {
       const int x = n * 256 + tid, r = r0 + x / T::CH;
       sq[n] = r < r_end ? *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(p.q) +
-                                                          query_row(p, b, hk, r) * T::BYTES + (x % T::CH) * 16)
+                                                          query_row(p, b, hk, r) * T::ROW + (x % T::CH) * 16)
                         : u32x4{0, 0, 0, 0};
     }
     if (tid < NR) sl = neg_lse(p, b, hk, r0 + tid, r_end);
@@ -267,9 +259,9 @@ mass_prompt(const MassParams p) {
     const bool masked = odd[buf] || __any(r0 < max(sees[0], sees[1]));
 #pragma unroll
     for (int y = 0; y < NR / 32; ++y) {
-      u32x4 q[T::ST];
+      u32x4 q[ST];
 #pragma unroll
-      for (int st = 0; st < T::ST; ++st)
+      for (int st = 0; st < ST; ++st)
         q[st] = *reinterpret_cast<const u32x4*>(qt[buf] + T::at(y * 32 + l32, 2 * st + half));
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -288,7 +280,7 @@ mass_prompt(const MassParams p) {
     const float sum = w[x] + __shfl_xor(w[x], 32);
     if (half || key[x] >= S) continue;
     if (p.row_parts == 1)
-      store(p, unit, b, key[x], base, sum);
+      store(p, unit, b, key[x], base, sum, p.mass[static_cast<int64_t>(unit) * p.slot_stride + key[x]]);
     else
       p.parts[(static_cast<int64_t>(part) * units + unit) * p.c.max_len + key[x]] = sum;
   }
@@ -309,9 +301,10 @@ mass_reduce(const MassParams p) {
   const int key_first = key / kMassPromptKeys * kMassPromptKeys;
   const int r_begin = max(0, key_first - base) * p.G, r_end = n_count * p.G;
   float w = 0.f;
+#pragma unroll 8
   for (int c = r_begin / p.part_rows; c < p.row_parts && c * p.part_rows < r_end && r_begin < r_end; ++c)
     w += p.parts[(static_cast<int64_t>(c) * units + unit) * p.c.max_len + key];
-  store(p, unit, b, key, base, w);
+  store(p, unit, b, key, base, w, p.mass[static_cast<int64_t>(unit) * p.slot_stride + key]);
 }
 
 }  // namespace
@@ -323,8 +316,10 @@ hipError_t launch_kv_mass(const MassParams& p, const MassPlan& pl, int head_dim,
   do {                                                                          \
     if (pl.prompt)                                                              \
       hipLaunchKernelGGL((mass_prompt<D, BF>), grid, block, 0, s, p);           \
+    else if (p.L * p.G <= 32)                                                   \
+      hipLaunchKernelGGL((mass_step<D, BF, 1>), grid, block, 0, s, p);          \
     else                                                                        \
-      hipLaunchKernelGGL((mass_step<D, BF>), grid, block, 0, s, p);             \
+      hipLaunchKernelGGL((mass_step<D, BF, 4>), grid, block, 0, s, p);          \
   } while (0)
   if (head_dim == 128) {
     if (bf16) MD_MASS(128, true); else MD_MASS(128, false);

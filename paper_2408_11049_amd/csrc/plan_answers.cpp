@@ -184,15 +184,20 @@ MassPlan make_mass_plan(const md_kv_mass_args* a, int num_cus) {
   pl.part_rows = static_cast<int32_t>(rows);
   pl.prompt = rows > kMassStepRows;
   if (!pl.prompt) {
-    // Whole rounds of the XCDs, which take all heads of a block of keys (see kv_mass.hip).
-    pl.n_wgs = ceil_div(a->num_seqs * ceil_div(a->max_kv_len, kMassStepKeys), 8) * 8 * a->num_kv_heads;
+    // Enough workgroups for the device's places, two a compute unit; a tile of 32 keys a wave at least.
+    // (64 x 8 heads of 2054 tokens: 52 us whole, 59 in two parts, 61 in four.)
+    pl.key_parts = static_cast<int32_t>(std::max<int64_t>(
+        1, std::min(2 * cus / std::max<int64_t>(units, 1), ceil_div(a->max_kv_len, 128))));
+    // Whole rounds of the XCDs, which take all heads of a part (see kv_mass.hip).
+    pl.n_wgs = ceil_div(static_cast<int64_t>(a->num_seqs) * pl.key_parts, 8) * 8 * a->num_kv_heads;
     return pl;
   }
   const int64_t blocks = units * ceil_div(a->max_kv_len, kMassPromptKeys);
   // Half of a prompt's (row, key) pairs are masked.  Four workgroups of what is left to each place of
   // the device (two a compute unit), of 256 rows at least.
   const int64_t parts = std::min(ceil_div(16 * cus, std::max<int64_t>(blocks, 1)), ceil_div(rows, 256));
-  pl.part_rows = static_cast<int32_t>(ceil_div(ceil_div(rows, std::max<int64_t>(parts, 1)), 64) * 64);
+  const int64_t mp = env_knob("MD_MP", 1, 64);
+  pl.part_rows = static_cast<int32_t>(ceil_div(ceil_div(rows, std::max<int64_t>(mp ? mp : parts, 1)), 64) * 64);
   pl.row_parts = static_cast<int32_t>(ceil_div(rows, pl.part_rows));
   pl.n_wgs = blocks * pl.row_parts;
   pl.reduce_wgs = units * ceil_div(a->max_kv_len, 256);

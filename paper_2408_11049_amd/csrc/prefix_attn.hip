@@ -11,7 +11,7 @@
 // Both compute S^T = K Q^T, which leaves a lane one query row: the softmax needs no shuffles but one
 // exchange between the halves of the wave when the running maximum moves, and P^T is in place as the
 // second product's operand, O^T += V^T P^T, V read transposed from LDS.
-#include "answers_kernels.h"
+#include "kv_stream.h"
 
 namespace md {
 
@@ -21,7 +21,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
@@ -30,22 +29,8 @@ namespace {
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 constexpr float kLazy = 8.f;  // log2 headroom before a running maximum must move
-
-template <int D, bool BF16>
-struct Tile {
-  static constexpr int ES = BF16 ? 2 : 4;
-  static constexpr int ROW = D * ES;          // bytes of a row
-  static constexpr int CH = ROW / 16;         // 16-byte chunks of a row
-  // Rows sit unpadded, chunk c of row r in place c ^ turn(r): 16 rows at one c, as the waves
-  // read K, then cover all banks.
-  static __device__ __forceinline__ int at(int r, int c) {
-    const int turn = ROW == 128 ? (r >> 1) & 7 : r & 15;
-    return r * ROW + ((c ^ turn) << 4);
-  }
-};
 
 // Reports page ids outside the pool among the pages of tokens [from, to) of a block: a look of its
 // own ahead of the stream, for callers that ask.
@@ -67,10 +52,6 @@ __device__ __forceinline__ void check_length(int raw, int least, int most, int32
 __device__ __forceinline__ float part_lse(float m, float sum) {
   return sum > 0.f ? (m + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f
                    : (sum == sum ? -INFINITY : sum);
-}
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
 }
 
 // A row's part: its normalised O (32 channels a block, 8 j + 4 half + .. of each in this lane) and
@@ -125,7 +106,8 @@ __global__ void __launch_bounds__(256)
 __attribute__((amdgpu_waves_per_eu(D == 128 && !BF16 ? 1 : 2)))
 prefix_stream_kernel(const PrefixParams p) {
   using T = Tile<D, BF16>;
-  constexpr int KEYS = kPrefixStreamTile, NV = KEYS * T::CH / 64, RPW = 64 / T::CH;
+  constexpr int KEYS = kPrefixStreamTile;
+  static_assert(KEYS == Stream<D, BF16, true>::KEYS, "tiles of the plan");
   constexpr int ST = T::CH / 2;       // 16-byte operand chunks a lane holds of its row
   constexpr int CB = D / 32;          // blocks of 32 channels
   constexpr int BYTES = KEYS * T::ROW;
@@ -141,7 +123,7 @@ prefix_stream_kernel(const PrefixParams p) {
   // find its K and V in that L2; so are the heads of a sequence's part, which share token rows.
   const bool pre = static_cast<int>(blockIdx.x) < p.n_pre;
   const int x8 = (static_cast<int>(blockIdx.x) - (pre ? 0 : p.n_pre)) >> 3, xcd = static_cast<int>(blockIdx.x) & 7;
-  int blk, hk, chunk, C, row_base, tok0, rows;
+  int blk, hk, chunk, C, row_base, tok0, n_rows;
   if (pre) {
     const int u = x8 / p.row_blocks * 8 + xcd;
     C = p.c_pre;
@@ -151,7 +133,7 @@ prefix_stream_kernel(const PrefixParams p) {
     blk = u / (C * p.Hkv);
     row_base = x8 % p.row_blocks * 32;
     tok0 = blk * p.n * p.L;
-    rows = p.group_rows;
+    n_rows = p.group_rows;
   } else {
     const int per = p.Hkv * p.own_blocks, v = x8 / per * 8 + xcd;
     C = p.c_own;
@@ -161,7 +143,7 @@ prefix_stream_kernel(const PrefixParams p) {
     chunk = v % C;
     blk = v / C;
     tok0 = blk * p.L;
-    rows = p.L * p.G;
+    n_rows = p.L * p.G;
   }
   const KvView c = pre ? p.pre : p.own;
   const int raw_len = uniform(c.lens[blk]);
@@ -178,7 +160,7 @@ prefix_stream_kernel(const PrefixParams p) {
 
   // This lane's query row, and the keys it sees: those below lim.
   const int r = row_base + l32, tq = r / p.G;
-  const bool valid = r < rows;
+  const bool valid = r < n_rows;
   const int64_t row_g = static_cast<int64_t>(tok0 + tq) * p.Hq + hk * p.G + (r - tq * p.G);
   const int lim = min(end, valid && !pre ? len - p.L + tq + 1 : end);
 
@@ -191,57 +173,10 @@ prefix_stream_kernel(const PrefixParams p) {
     const Places<D, BF16> at(lane);
     unsigned char* const kt = lds[wave];
     unsigned char* const vt = lds[wave] + BYTES;
-    const int64_t head = static_cast<int64_t>(hk) * c.s_head;
-    const int pmask = paged ? (1 << c.page_shift) - 1 : INT32_MAX;
-    const bool groups = !paged || (1 << c.page_shift) >= RPW;
-    const uint32_t lane_off = static_cast<uint32_t>((lane / T::CH) * c.s_tok * T::ES + (lane % T::CH) * 16);
-    u32x4 k[NV], v[NV];
-    uint32_t ok;  // bit n: row n of this lane is a token
-    // The block (sequence or page) of this lane's token of tile t, lane & 31; past the end the last one's.
-    // A contiguous cache loads something of no use, so that the loads on their way are as many either way.
-    const int32_t* const table = paged ? c.page_table + static_cast<int64_t>(blk) * c.max_pages : c.lens;
-    auto load_block = [&](int t) -> int {
-      const int tok = min(t * KEYS + l32, end - 1);
-      const int id = table[paged ? tok >> c.page_shift : 0];
-      return paged ? id : blk;
-    };
-    // K and V of tile t, whole rows: RPW of them an instruction, at one scalar address and a fixed offset a
-    // lane where they are all tokens of one page, else each lane at its row's.  A row past the end, or on a
-    // page outside the pool, is redirected to one that may be read and staged as zeros.
-    auto load = [&](int t, int block) {
-      const bool in_pool = !paged || (block >= 0 && block < c.num_pages);
-      const unsigned long long pool = __ballot(in_pool);
-      const int64_t row = (static_cast<int64_t>(in_pool ? block : 0) * c.s_blk +
-                           static_cast<int64_t>(min(t * KEYS + l32, end - 1) & pmask) * c.s_tok + head) * T::ES;
-      ok = 0;
-      if (groups && (t + 1) * KEYS <= end) {
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          const int64_t byte =
-              static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(
-                                        static_cast<int>(row >> 32), n * RPW))) << 32) |
-                                   static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(row), n * RPW)));
-          k[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(c.k + byte + lane_off));
-          v[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(c.v + byte + lane_off));
-          ok |= static_cast<uint32_t>((pool >> (n * RPW)) & 1ull) << n;
-        }
-      } else {
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          const int of = n * RPW + lane / T::CH;
-          const int64_t byte =
-              static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(row >> 32), of))) << 32) |
-                                   static_cast<uint32_t>(__shfl(static_cast<int>(row), of))) + (lane % T::CH) * 16;
-          k[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(c.k + byte));
-          v[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(c.v + byte));
-          ok |= static_cast<uint32_t>(t * KEYS + of < end && ((pool >> of) & 1ull)) << n;
-        }
-      }
-    };
-
-    int block = load_block(t0 + wave);
-    int block_next = load_block(t0 + wave + 4);
-    load(t0 + wave, block);
+    Stream<D, BF16, true> rows(c, blk, hk, end, lane);
+    const int block = rows.load_block(t0 + wave);
+    int block_next = rows.load_block(t0 + wave + 4);
+    rows.load(t0 + wave, block);
     // Q as the second operand: chunk 2 st + half of the row, that is channels 8 (bf16) or 4 a
     // chunk; K's chunks are taken in the same order.
     u32x4 q[ST];
@@ -253,19 +188,9 @@ prefix_stream_kernel(const PrefixParams p) {
 
     for (int t = t0 + wave; t < t1; t += 4) {
       // The tile to LDS; its registers take the wave's next one while this is computed.
-      if (__any(ok != (1u << NV) - 1u)) {
-#pragma unroll
-        for (int n = 0; n < NV; ++n)
-          if (!((ok >> n) & 1u)) k[n] = v[n] = u32x4{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        const int a = T::at(n * RPW + lane / T::CH, lane % T::CH);
-        *reinterpret_cast<u32x4*>(kt + a) = k[n];
-        *reinterpret_cast<u32x4*>(vt + a) = v[n];
-      }
-      const int ahead = load_block(t + 8);
-      load(t + 4, block_next);
+      rows.store(kt, vt);
+      const int ahead = rows.load_block(t + 8);
+      rows.load(t + 4, block_next);
       block_next = ahead;
       wave_sync();
 
