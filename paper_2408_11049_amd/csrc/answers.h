@@ -40,8 +40,7 @@ constexpr int kMassPromptKeys = 256, kMassStepRows = 128;
 struct MassPlan {
   bool prompt = false;
   int32_t key_parts = 1;    // of a sequence, a step's
-  int32_t row_parts = 1;    // parts of part_rows rows; the workspace holds each part's weights
-  int32_t part_rows = 0;
+  int32_t row_parts = 1;    // of a pair of key blocks; the workspace holds each part's weights
   int64_t n_wgs = 0, reduce_wgs = 0;
   size_t workspace_bytes = 0;
 };

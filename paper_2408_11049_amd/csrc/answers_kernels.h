@@ -45,7 +45,7 @@ struct MassParams {
   int32_t* slot_pos;
   int64_t slot_stride;
   int32_t B, L, Hq, Hkv, G;
-  int32_t key_parts, row_parts, part_rows;
+  int32_t key_parts, row_parts;
   float* parts;               // [row_parts][B, Hkv][max_len] (row_parts > 1)
   float scale_log2;
 };

@@ -103,7 +103,6 @@ int md_kv_mass(const md_kv_mass_args* a, void* stream) {
   p.G = a->num_q_heads / a->num_kv_heads;
   p.key_parts = pl.key_parts;
   p.row_parts = pl.row_parts;
-  p.part_rows = pl.part_rows;
   p.parts = static_cast<float*>(a->workspace);
   p.scale_log2 = md::scale_log2(a->sm_scale, a->head_dim);
   return md::status(md::launch_kv_mass(p, pl, a->head_dim, a->dtype == MD_BF16,

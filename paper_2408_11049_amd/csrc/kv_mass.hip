@@ -13,6 +13,8 @@
 //   mass_prompt  many rows (a prompt's): bound by the matrix and vector units alike.  The rows are
 //                cut into parts, whose sums mass_reduce adds, so that early keys, which
 //                most rows see, are no longer work than late ones.
+#include <type_traits>
+
 #include "kv_stream.h"
 
 namespace md {
@@ -177,7 +179,32 @@ mass_step(const MassParams p) {
   }
 }
 
-// A part of the rows, 64 of them in LDS at a time (two such tiles in turn); 256 keys a
+// The rows that a prompt's key blocks of 256 keys see, in tiles of 64.  Blocks go in pairs, i with the i-th
+// from the end, as one list of tiles, i's first: later keys have fewer rows, and every pair has as many.
+// Part c takes every n_parts-th tile from the c-th on, and so as many masked ones as the others (in
+// contiguous parts those with the diagonal took half as long again).
+struct PairRows {
+  int kb[2], r0[2], tiles[2], n_parts;
+  __device__ __forceinline__ PairRows(int pair, int S, int base, int G, int r_end, int parts) : n_parts(parts) {
+    const int n = (S + kMassPromptKeys - 1) / kMassPromptKeys;
+    kb[0] = pair;
+    kb[1] = n - 1 - pair;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      r0[x] = max(0, kb[x] * kMassPromptKeys - base) * G;
+      tiles[x] = max(0, (r_end - r0[x] + 63) >> 6);
+    }
+    if (kb[1] <= kb[0]) tiles[1] = 0;  // a block in the middle is a pair by itself
+  }
+  // The part's first tile of the first or second block (from tiles[seg] on: none).
+  __device__ __forceinline__ int first(int seg, int part) const {
+    if (!seg) return part;
+    const int x = part - tiles[0] % n_parts;
+    return x < 0 ? x + n_parts : x;
+  }
+};
+
+// A part of a pair's rows, 64 of them in LDS at a time (two such tiles in turn); 256 keys a
 // workgroup, 64 a wave.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256)
@@ -195,94 +222,126 @@ mass_prompt(const MassParams p) {
   const int units = p.B * p.Hkv;
   const int unit = static_cast<int>(blockIdx.x) % units;
   const int part = (static_cast<int>(blockIdx.x) / units) % p.row_parts;
-  const int kb = static_cast<int>(blockIdx.x) / units / p.row_parts;
+  const int pair = static_cast<int>(blockIdx.x) / units / p.row_parts;
   const int hk = unit % p.Hkv, b = unit / p.Hkv;
   const int S = uniform(min(max(p.c.lens[b], 0), p.c.max_len));
-  const int key_first = kb * kMassPromptKeys;
-  if (key_first >= S) return;
   const int base = S - p.L;
   int n_count = p.L;
   if (p.accepted) n_count = min(max(uniform(p.accepted[b]), 0), p.L - 1) + 1;
-  // Rows of this part that count and see a key of this workgroup.
-  const int r_begin = max(part * p.part_rows, max(0, key_first - base) * p.G);
-  const int r_end = min(n_count * p.G, (part + 1) * p.part_rows);
-  if (r_begin >= r_end && p.row_parts > 1) return;  // mass_reduce does not ask for it
+  const PairRows list(pair, S, base, p.G, n_count * p.G, p.row_parts);
+  if (list.kb[1] < list.kb[0]) return;
 
-  int key[2], sees[2];
-  u32x4 k[2][ST];
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    key[x] = key_first + wave * 64 + x * 32 + l32;
-    sees[x] = max(0, min(key[x], S - 1) - base) * p.G;
-    const int64_t off = key[x] < S ? key_offset(p, b, hk, key[x], T::ES) : -1;
-#pragma unroll
-    for (int st = 0; st < ST; ++st)
-      k[x][st] = *reinterpret_cast<const u32x4*>(p.c.k + (off < 0 ? 0 : off) + (2 * st + half) * 16);
-  }
+  for (int seg = 0; seg <= (list.kb[1] > list.kb[0]); ++seg) {
+    // Rows of this part that count and see a key of the block.
+    const int kb = seg ? list.kb[1] : list.kb[0], r0_block = seg ? list.r0[1] : list.r0[0];
+    const int tiles = seg ? list.tiles[1] : list.tiles[0], first = list.first(seg, part);
+    if (first >= tiles && p.row_parts > 1) continue;  // mass_reduce does not ask for it
+    const int r_begin = r0_block + first * NR, r_end = min(n_count * p.G, r0_block + tiles * NR);
+    const int next = NR * p.row_parts;  // rows to the next tile
 
-  u32x4 sq[QP];
-  float sl = -INFINITY;
-  auto load_tile = [&](int r0) {
-    if (r0 >= r_end) return;
+    int key[2], sees[2];
+    u32x4 k[2][ST];
 #pragma unroll
-    for (int n = 0; n < QP; ++n) {
-      const int x = n * 256 + tid, r = r0 + x / T::CH;
-      sq[n] = r < r_end ? *reinterpret_cast<const u32x4*>(static_cast<const unsigned char*>(p.q) +
-                                                          query_row(p, b, hk, r) * T::ROW + (x % T::CH) * 16)
-                        : u32x4{0, 0, 0, 0};
-    }
-    if (tid < NR) sl = neg_lse(p, b, hk, r0 + tid, r_end);
-  };
-  auto store_tile = [&](int buf, int r0) {
-    if (r0 >= r_end) return;
-#pragma unroll
-    for (int n = 0; n < QP; ++n) {
-      const int x = n * 256 + tid;
-      *reinterpret_cast<u32x4*>(qt[buf] + T::at(x / T::CH, x % T::CH)) = sq[n];
-    }
-    if (tid < NR) {
-      nl[buf][tid] = sl;
-      const bool none = __any(sl == -INFINITY);
-      if (tid == 0) odd[buf] = none;
-    }
-  };
-
-  float w[2] = {};
-  load_tile(r_begin);
-  store_tile(0, r_begin);
-  load_tile(r_begin + NR);
-  __syncthreads();
-  int buf = 0;
-  for (int r0 = r_begin; r0 < r_end; r0 += NR, buf ^= 1) {
-    store_tile(buf ^ 1, r0 + NR);
-    load_tile(r0 + 2 * NR);
-    const bool masked = odd[buf] || __any(r0 < max(sees[0], sees[1]));
-#pragma unroll
-    for (int y = 0; y < NR / 32; ++y) {
-      u32x4 q[ST];
+    for (int x = 0; x < 2; ++x) {
+      key[x] = kb * kMassPromptKeys + wave * 64 + x * 32 + l32;
+      sees[x] = max(0, min(key[x], S - 1) - base) * p.G;
+      const int64_t off = key[x] < S ? key_offset(p, b, hk, key[x], T::ES) : -1;
 #pragma unroll
       for (int st = 0; st < ST; ++st)
-        q[st] = *reinterpret_cast<const u32x4*>(qt[buf] + T::at(y * 32 + l32, 2 * st + half));
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const f32x16 s = scores<D, BF16>(q, k[x]);
-        // Two instances: the mask costs as much as the rest of the vector work.
-        if (masked)
-          w[x] += weigh(s, nl[buf] + y * 32, p.scale_log2, half, true, sees[x] - (r0 + y * 32));
-        else
-          w[x] += weigh(s, nl[buf] + y * 32, p.scale_log2, half, false, 0);
-      }
+        k[x][st] = *reinterpret_cast<const u32x4*>(p.c.k + (off < 0 ? 0 : off) + (2 * st + half) * 16);
     }
-    __syncthreads();
-  }
+
+    // Four threads a row.  Their row's place moves by a step of whole tokens and a rest among the G
+    // of a token, without a division (which made 117 us of 108).
+    const int64_t token = static_cast<int64_t>(p.Hq) * T::ROW;
+    const int step_g = next % p.G;
+    const int64_t step = next / p.G * token + step_g * T::ROW, carry = token - static_cast<int64_t>(p.G) * T::ROW;
+    const unsigned char* at = static_cast<const unsigned char*>(p.q) +
+                              query_row(p, b, hk, r_begin + tid / 4) * T::ROW + (tid & 3) * 16;
+    int at_g = (r_begin + tid / 4) % p.G;
+    u32x4 sq[QP];
+    float sl = -INFINITY;
+    auto load_tile = [&](int r0) {
+      if (r0 >= r_end) return;
+      const bool there = r0 + tid / 4 < r_end;
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const float sum = w[x] + __shfl_xor(w[x], 32);
-    if (half || key[x] >= S) continue;
-    if (p.row_parts == 1)
-      store(p, unit, b, key[x], base, sum, p.mass[static_cast<int64_t>(unit) * p.slot_stride + key[x]]);
-    else
-      p.parts[(static_cast<int64_t>(part) * units + unit) * p.c.max_len + key[x]] = sum;
+      for (int n = 0; n < QP; ++n)
+        sq[n] = there ? *reinterpret_cast<const u32x4*>(at + n * 64) : u32x4{0, 0, 0, 0};
+      at_g += step_g;
+      const bool over = at_g >= p.G;
+      at += step + (over ? carry : 0);
+      at_g -= over ? p.G : 0;
+      if (tid < NR) sl = neg_lse(p, b, hk, r0 + tid, r_end);
+    };
+    auto store_tile = [&](int buf, int r0) {
+      if (r0 >= r_end) return;
+#pragma unroll
+      for (int n = 0; n < QP; ++n) *reinterpret_cast<u32x4*>(qt[buf] + T::at(tid / 4, n * 4 + (tid & 3))) = sq[n];
+      if (tid < NR) {
+        nl[buf][tid] = sl;
+        const bool none = __any(sl == -INFINITY);
+        if (tid == 0) odd[buf] = none;
+      }
+    };
+
+    float w[2] = {};
+    load_tile(r_begin);
+    store_tile(0, r_begin);
+    load_tile(r_begin + next);
+    __syncthreads();
+    int buf = 0;
+    for (int r0 = r_begin; r0 < r_end; r0 += next, buf ^= 1) {
+      store_tile(buf ^ 1, r0 + next);
+      load_tile(r0 + 2 * next);
+      // One block of 32 rows and 32 keys is weighed beside the next one's products.
+      auto weigh_tile = [&](auto masked) {
+        u32x4 q[ST];
+        f32x16 s[2];
+        auto read_q = [&](int y) {
+#pragma unroll
+          for (int st = 0; st < ST; ++st)
+            q[st] = *reinterpret_cast<const u32x4*>(qt[buf] + T::at(y * 32 + l32, 2 * st + half));
+        };
+        read_q(0);
+        s[0] = scores<D, BF16>(q, k[0]);
+#pragma unroll
+        for (int n = 0; n < NR / 16; ++n) {
+          const int y = n / 2, x = n & 1;
+          if (n + 1 < NR / 16) {
+            if (x) read_q(y + 1);
+            s[x ^ 1] = scores<D, BF16>(q, k[x ^ 1]);
+          }
+          w[x] += weigh(s[x], nl[buf] + y * 32, p.scale_log2, half, masked, sees[x] - (r0 + y * 32));
+          if constexpr (BF16 && !masked) {
+            if (n + 1 < NR / 16) {
+#pragma unroll
+              for (int i = 0; i < ST; ++i) {  // vector work between the matrix instructions
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 32 / ST, 0);
+                __builtin_amdgcn_sched_group_barrier(0x400, 16 / ST, 0);
+              }
+            }
+          }
+        }
+      };
+      // Two instances: the mask costs as much as the rest of the vector work.
+      if (odd[buf] || __any(r0 < sees[1])) {
+        if (__any(r0 + NR > sees[0])) weigh_tile(std::true_type{});  // else no row sees the wave's keys
+      } else {
+        weigh_tile(std::false_type{});
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float sum = w[x] + __shfl_xor(w[x], 32);
+      if (half || key[x] >= S) continue;
+      if (p.row_parts == 1)
+        store(p, unit, b, key[x], base, sum, p.mass[static_cast<int64_t>(unit) * p.slot_stride + key[x]]);
+      else
+        p.parts[(static_cast<int64_t>(part) * units + unit) * p.c.max_len + key[x]] = sum;
+    }
   }
 }
 
@@ -293,17 +352,19 @@ mass_reduce(const MassParams p) {
   const int unit = static_cast<int>(blockIdx.x) % units;
   const int key = static_cast<int>(blockIdx.x) / units * 256 + static_cast<int>(threadIdx.x);
   const int b = unit / p.Hkv;
-  const int S = min(max(p.c.lens[b], 0), p.c.max_len);
+  const int S = uniform(min(max(p.c.lens[b], 0), p.c.max_len));
   if (key >= S) return;
   const int base = S - p.L;
   int n_count = p.L;
-  if (p.accepted) n_count = min(max(p.accepted[b], 0), p.L - 1) + 1;
-  const int key_first = key / kMassPromptKeys * kMassPromptKeys;
-  const int r_begin = max(0, key_first - base) * p.G, r_end = n_count * p.G;
+  if (p.accepted) n_count = min(max(uniform(p.accepted[b]), 0), p.L - 1) + 1;
+  const int kb = uniform(key / kMassPromptKeys), n_kb = (S + kMassPromptKeys - 1) / kMassPromptKeys;
+  const int seg = kb > n_kb - 1 - kb;
+  const PairRows list(seg ? n_kb - 1 - kb : kb, S, base, p.G, n_count * p.G, p.row_parts);
+  const int tiles = seg ? list.tiles[1] : list.tiles[0];
   float w = 0.f;
-#pragma unroll 8
-  for (int c = r_begin / p.part_rows; c < p.row_parts && c * p.part_rows < r_end && r_begin < r_end; ++c)
-    w += p.parts[(static_cast<int64_t>(c) * units + unit) * p.c.max_len + key];
+#pragma unroll 4
+  for (int c = 0; c < p.row_parts; ++c)
+    if (list.first(seg, c) < tiles) w += p.parts[(static_cast<int64_t>(c) * units + unit) * p.c.max_len + key];
   store(p, unit, b, key, base, w, p.mass[static_cast<int64_t>(unit) * p.slot_stride + key]);
 }
 

@@ -113,14 +113,19 @@ PrefixPlan make_prefix_plan(const md_attn_args* a, const md_prefix* p, int num_c
   const int64_t heads = static_cast<int64_t>(p->num_prefixes) * a->num_kv_heads;
   const int64_t units = heads * pl.row_blocks;
   const int64_t own = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads * pl.own_blocks;
-  // Parts of a range: enough workgroups to fill the device's places, at least two tiles a part.
-  auto parts = [&](int64_t len, int64_t n, int64_t places, int64_t least) {
-    const int64_t most = ceil_div(len, least);
-    return static_cast<int32_t>(std::max<int64_t>(1, std::min(places / std::max<int64_t>(n, 1), most)));
+  // Parts of a range: as many workgroups as the device has places (two a compute unit, of the
+  // wide kernel one), of 256 tokens, two tiles a wave, at least; 128 up to one a compute unit.
+  // (8 sequences of 8 heads over a prefix of 8192: 15.5 us in 16 or 32 parts, 20 in 8, 21 in 64; 2 heads
+  // over one of 512, fp32: 8.6 us in 4 parts, 10.9 in 2.  Own caches, 64 x 4 heads of 1024 tokens: 26 us in
+  // 1 part, 28 in 2, 35 in 4; 64 x 8: 38, 37, 44.)
+  auto parts = [cus](int64_t len, int64_t n, bool wide) {
+    const int64_t once = std::max<int64_t>(cus / std::max<int64_t>(n, 1), 1);
+    const int64_t twice = std::max<int64_t>((wide ? 1 : 2) * cus / std::max<int64_t>(n, 1), 1);
+    return static_cast<int32_t>(std::max<int64_t>(
+        1, std::max(std::min(once, ceil_div(len, 128)), std::min(twice, ceil_div(len, 256)))));
   };
-  const int64_t k1 = env_knob("MD_C_PRE", 1, 512), k2 = env_knob("MD_C_OWN", 1, 512);
-  pl.c_pre = k1 ? k1 : parts(p->max_len, units, pl.wide ? cus : 2 * cus, 128);
-  pl.c_own = k2 ? k2 : parts(a->max_kv_len, own, 4 * cus, 128);
+  pl.c_pre = parts(p->max_len, units, pl.wide);
+  pl.c_own = parts(a->max_kv_len, own, false);
   pl.n_pre = static_cast<int32_t>(ceil_div(heads * pl.c_pre, 8) * 8 * pl.row_blocks);
   if (p->max_len == 0) pl.c_pre = pl.n_pre = 0;
   pl.n_own = ceil_div(static_cast<int64_t>(a->num_seqs) * pl.c_own, 8) * 8 * a->num_kv_heads * pl.own_blocks;
@@ -181,7 +186,6 @@ MassPlan make_mass_plan(const md_kv_mass_args* a, int num_cus) {
   const int64_t cus = num_cus > 0 ? num_cus : 256;
   const int64_t units = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads;
   const int64_t rows = static_cast<int64_t>(a->num_q_heads / a->num_kv_heads) * a->q_len;
-  pl.part_rows = static_cast<int32_t>(rows);
   pl.prompt = rows > kMassStepRows;
   if (!pl.prompt) {
     // Enough workgroups for the device's places, two a compute unit; a tile of 32 keys a wave at least.
@@ -192,14 +196,15 @@ MassPlan make_mass_plan(const md_kv_mass_args* a, int num_cus) {
     pl.n_wgs = ceil_div(static_cast<int64_t>(a->num_seqs) * pl.key_parts, 8) * 8 * a->num_kv_heads;
     return pl;
   }
-  const int64_t blocks = units * ceil_div(a->max_kv_len, kMassPromptKeys);
-  // Half of a prompt's (row, key) pairs are masked.  Four workgroups of what is left to each place of
-  // the device (two a compute unit), of 256 rows at least.
-  const int64_t parts = std::min(ceil_div(16 * cus, std::max<int64_t>(blocks, 1)), ceil_div(rows, 256));
-  const int64_t mp = env_knob("MD_MP", 1, 64);
-  pl.part_rows = static_cast<int32_t>(ceil_div(ceil_div(rows, std::max<int64_t>(mp ? mp : parts, 1)), 64) * 64);
-  pl.row_parts = static_cast<int32_t>(ceil_div(rows, pl.part_rows));
-  pl.n_wgs = blocks * pl.row_parts;
+  // A unit's key blocks go in pairs, the i-th with the i-th from the end: in a prompt, where later keys
+  // have fewer rows, all pairs have as many (kv_mass.hip).  Their rows are cut into parts that fill the
+  // device's places (two workgroups a compute unit) once, or, where that would leave an eighth of them
+  // empty, about four times; 256 rows of a pair at least.
+  const int64_t pairs = units * ceil_div(ceil_div(a->max_kv_len, kMassPromptKeys), 2);
+  const int64_t places = 2 * cus, once = places / pairs;
+  const int64_t parts = pairs * once * 8 >= places * 7 ? once : ceil_div(4 * places, pairs);
+  pl.row_parts = static_cast<int32_t>(std::max<int64_t>(1, std::min(parts, ceil_div(rows, 256))));
+  pl.n_wgs = pairs * pl.row_parts;
   pl.reduce_wgs = units * ceil_div(a->max_kv_len, 256);
   if (pl.row_parts > 1)
     pl.workspace_bytes = align_up(static_cast<size_t>(pl.row_parts) * units * a->max_kv_len * 4, 256);
