@@ -48,10 +48,8 @@ __device__ __forceinline__ int64_t query_row(const MassParams& p, int b, int hk,
 }
 
 // What a row's score gets under the exponential: -lse in log2; -inf: the row weighs nothing.
-__device__ __forceinline__ float neg_lse(const MassParams& p, int b, int hk, int r, int r_end) {
-  if (r >= r_end) return -INFINITY;
-  const float l = p.lse[query_row(p, b, hk, r)];
-  return l == -INFINITY ? -INFINITY : -l * kLog2e;
+__device__ __forceinline__ float neg_lse(float lse) {
+  return lse == -INFINITY ? -INFINITY : -lse * kLog2e;
 }
 
 template <int D, bool BF16>
@@ -148,7 +146,7 @@ mass_step(const MassParams p) {
                                           query_row(p, b, hk, r) * T::ROW + (c % T::CH) * 16);
     *reinterpret_cast<u32x4*>(qt + T::at(r, c % T::CH)) = q;
   }
-  if (tid < RT * 32) nl[tid] = neg_lse(p, b, hk, tid, r_end);
+  if (tid < RT * 32) nl[tid] = tid < r_end ? neg_lse(p.lse[query_row(p, b, hk, tid)]) : -INFINITY;
   __syncthreads();
 
   for (int t = first; t < t1; t += 4) {
@@ -271,15 +269,17 @@ mass_prompt(const MassParams p) {
       const bool over = at_g >= p.G;
       at += step + (over ? carry : 0);
       at_g -= over ? p.G : 0;
-      if (tid < NR) sl = neg_lse(p, b, hk, r0 + tid, r_end);
+      // As it is: arithmetic here would wait for the tile's rows, which were asked for before it.
+      if (tid < NR) sl = r0 + tid < r_end ? p.lse[query_row(p, b, hk, r0 + tid)] : -INFINITY;
     };
     auto store_tile = [&](int buf, int r0) {
       if (r0 >= r_end) return;
 #pragma unroll
       for (int n = 0; n < QP; ++n) *reinterpret_cast<u32x4*>(qt[buf] + T::at(tid / 4, n * 4 + (tid & 3))) = sq[n];
       if (tid < NR) {
-        nl[buf][tid] = sl;
-        const bool none = __any(sl == -INFINITY);
+        const float x = neg_lse(sl);
+        nl[buf][tid] = x;
+        const bool none = __any(x == -INFINITY);
         if (tid == 0) odd[buf] = none;
       }
     };
@@ -287,13 +287,19 @@ mass_prompt(const MassParams p) {
     float w[2] = {};
     load_tile(r_begin);
     store_tile(0, r_begin);
+    // The keys arrive here: a wait for them inside the loop would be one for the rows on their way too.
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int st = 0; st < ST; ++st) asm volatile("" : "+v"(k[x][st]));
     load_tile(r_begin + next);
     __syncthreads();
     int buf = 0;
     for (int r0 = r_begin; r0 < r_end; r0 += next, buf ^= 1) {
       store_tile(buf ^ 1, r0 + next);
       load_tile(r0 + 2 * next);
-      // One block of 32 rows and 32 keys is weighed beside the next one's products.
+      // One block of 32 rows and 32 keys is weighed beside the next one's products.  (The compiler's order
+      // stands: one matrix instruction to four vector ones, forced, took the same 97 us.)
       auto weigh_tile = [&](auto masked) {
         u32x4 q[ST];
         f32x16 s[2];
@@ -312,17 +318,6 @@ mass_prompt(const MassParams p) {
             s[x ^ 1] = scores<D, BF16>(q, k[x ^ 1]);
           }
           w[x] += weigh(s[x], nl[buf] + y * 32, p.scale_log2, half, masked, sees[x] - (r0 + y * 32));
-          if constexpr (BF16 && !masked) {
-            if (n + 1 < NR / 16) {
-#pragma unroll
-              for (int i = 0; i < ST; ++i) {  // vector work between the matrix instructions
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 32 / ST, 0);
-                __builtin_amdgcn_sched_group_barrier(0x400, 16 / ST, 0);
-              }
-            }
-          }
         }
       };
       // Two instances: the mask costs as much as the rest of the vector work.
