@@ -692,7 +692,9 @@ typedef struct {
  * all rows of its group.
  * Softmax and sums are fp32; with bf16 inputs the softmax weights are rounded to bf16 before
  * they multiply V (lse is not).  A query that sees nothing (an empty prefix, no own token) gets
- * o = 0, lse = -inf; one whose sum is NaN gets o = NaN, lse = -inf.  Lengths are clamped to
+ * o = 0, lse = -inf; one whose sum is NaN gets o = NaN, lse = -inf.  A NaN or an infinity in V of one
+ * of a sequence's L newest tokens may reach the rows before it too, as in md_verify_attn (a weight of 0
+ * times it); in K it reaches the rows that see it alone.  Lengths are clamped to
  * [0, max]; a sequence of fewer than L own tokens has its first rows see the prefix alone.
  * Tokens on pages outside [0, num_pages) are not dereferenced, and the queries that see them
  * get unspecified results.  err_word reports both caches.
