@@ -3,8 +3,11 @@
 // into the slots that this frees.
 //
 // One workgroup a (sequence, KV head) finds the key of rank n - budget by a radix select (three
-// rounds over keys in LDS), counts in slot order and lists (freed slot, kept slot) pairs; pairs are moved by the same workgroup or, where a call may have
-// more than kEvictFused of them a head, by a second launch over the whole device.
+// rounds over keys in LDS), counts in slot order and lists (freed slot, kept slot) pairs; pairs are
+// moved by the same workgroup or, where a call may have more than kEvictFused of them a head, by a
+// second launch over the whole device.
+#include <type_traits>
+
 #include "answers_kernels.h"
 
 namespace md {
@@ -120,8 +123,6 @@ evict_select(const EvictParams p) {
       if (j < min(n, KEYS)) keys[j] = order_key(u, pos[i], w[i]);
     }
   }
-  auto key_of = [&](int j) { return j < KEYS ? keys[j] : order_key(u, u.pos[j], u.mass[j]); };
-
   const int vecs = 2 * p.row_vecs;
   if (n - p.budget <= kFew && n <= KEYS) {
     // A step's few tokens: the least (key, slot) pair above the last one found, one after another
@@ -171,114 +172,138 @@ evict_select(const EvictParams p) {
     return;
   }
 
-  // The key of rank n - budget (from 1), 11, 11 and 10 bits a round (weights spread over few exponents, and
-  // atomics on one bin take turns: with the upper 8 bits alone they took longer than the rest): of the
-  // keys that agree with `prefix` in the bits above, `want` is the rank looked for.
-  uint32_t prefix = 0;
-  int want = n - p.budget;
-#pragma unroll
-  for (int round = 0; round < 3; ++round) {
-    const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
-    for (int i = tid; i < BINS; i += NT) hist[i] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += NT) {
-      const uint32_t key = key_of(j);
-      if (round == 0 || (key >> (shift + bits)) == (prefix >> (shift + bits)))
-        atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1u)], 1u);
-    }
-    __syncthreads();
-    // The bin in which the running count reaches `want`: 256 threads of eight bins each.
-    uint32_t h[8], mine = 0, incl = 0;
-    if (tid < 256) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) mine += h[i] = hist[tid * 8 + i];
-      incl = mine;
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = __shfl_up(incl, o);
-        if (lane >= o) incl += x;
-      }
-      if (lane == 63) counts[0][wave] = static_cast<int>(incl);
-    }
-    __syncthreads();
-    if (tid < 256) {
-      uint32_t run = incl - mine;
-      for (int x = 0; x < wave; ++x) run += static_cast<uint32_t>(counts[0][x]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (run < static_cast<uint32_t>(want) && static_cast<uint32_t>(want) <= run + h[i]) {
-          pick[0] = tid * 8 + i;
-          pick[1] = want - run;
-        }
-        run += h[i];
-      }
-    }
-    __syncthreads();
-    prefix |= pick[0] << shift;
-    want = static_cast<int>(pick[1]);
-  }
-  // Evicted: keys below `prefix`, and the first `want` slots whose key is `prefix`.
+  // (With the choice of LDS or memory inside its loops the select waits for every key in turn.)
+  auto select = [&](auto in_lds) {
+    auto key_of = [&](int j) {
+      if constexpr (in_lds) return keys[j];
+      return j < KEYS ? keys[j] : order_key(u, u.pos[j], u.mass[j]);
+    };
 
-  // Each wave takes a run of slots and counts, below and from the budget on, those that go by their key,
-  // those that stay, and those with the key `prefix`.
-  const int per = (n + NW * 64 - 1) / (NW * 64) * 64, lo = min(n, wave * per), hi = min(n, lo + per);
-  int holes = 0, extras = 0, ties_low = 0, ties_high = 0;
-  for (int j0 = lo; j0 < hi; j0 += 64) {
-    const int j = j0 + lane;
-    const bool in = j < hi, low = j < p.budget;
-    const uint32_t key = key_of(min(j, n - 1));
-    holes += __popcll(__ballot(in && low && key < prefix));
-    extras += __popcll(__ballot(in && !low && key > prefix));
-    ties_low += __popcll(__ballot(in && low && key == prefix));
-    ties_high += __popcll(__ballot(in && !low && key == prefix));
-  }
-  __syncthreads();
-  if (lane == 0) counts[0][wave] = ties_low + ties_high;
-  __syncthreads();
-  int tie0 = 0;
-  for (int x = 0; x < wave; ++x) tie0 += counts[0][x];
-  // Of this wave's ties the first `go` go.
-  const int go = min(max(want - tie0, 0), ties_low + ties_high);
-  holes += min(go, ties_low);
-  extras += ties_high - max(go - ties_low, 0);
-  if (lane == 0) {
-    counts[1][wave] = holes;
-    counts[2][wave] = extras;
-  }
-  __syncthreads();
-  int hole = 0, extra = 0, total = 0, tie = tie0;
-  for (int x = 0; x < NW; ++x) {
-    if (x < wave) {
-      hole += counts[1][x];
-      extra += counts[2][x];
+    // The key of rank n - budget (from 1), 11, 11 and 10 bits a round (weights spread over few exponents, and
+    // atomics on one bin take turns: with the upper 8 bits alone they took longer than the rest): of the
+    // keys that agree with `prefix` in the bits above, `want` is the rank looked for.
+    uint32_t prefix = 0;
+    int want = n - p.budget;
+#pragma unroll
+    for (int round = 0; round < 3; ++round) {
+      const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
+      for (int i = tid; i < BINS; i += NT) hist[i] = 0;
+      __syncthreads();
+#pragma unroll 4
+      for (int j = tid; j < n; j += NT) {
+        const uint32_t key = key_of(j);
+        if (round == 0 || (key >> (shift + bits)) == (prefix >> (shift + bits)))
+          atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1u)], 1u);
+      }
+      __syncthreads();
+      // The bin in which the running count reaches `want`: 256 threads of eight bins each.
+      uint32_t h[8], mine = 0, incl = 0;
+      if (tid < 256) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mine += h[i] = hist[tid * 8 + i];
+        incl = mine;
+        for (int o = 1; o < 64; o <<= 1) {
+          const uint32_t x = __shfl_up(incl, o);
+          if (lane >= o) incl += x;
+        }
+        if (lane == 63) counts[0][wave] = static_cast<int>(incl);
+      }
+      __syncthreads();
+      if (tid < 256) {
+        uint32_t run = incl - mine;
+        for (int x = 0; x < wave; ++x) run += static_cast<uint32_t>(counts[0][x]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (run < static_cast<uint32_t>(want) && static_cast<uint32_t>(want) <= run + h[i]) {
+            pick[0] = tid * 8 + i;
+            pick[1] = want - run;
+          }
+          run += h[i];
+        }
+      }
+      __syncthreads();
+      prefix |= pick[0] << shift;
+      want = static_cast<int>(pick[1]);
     }
-    total += counts[1][x];
-  }
-  // As many slots are freed below the budget as tokens are kept behind it: the x-th takes the x-th.
-  int2* const pairs = p.counts ? p.moves + static_cast<int64_t>(unit) * p.max_moves : listed;
-  auto before = [](unsigned long long m) {  // lanes of m before this one
-    return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32),
-                                                      __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0u)));
+    // Evicted: keys below `prefix`, and the first `want` slots whose key is `prefix`.
+
+    // Each wave takes a run of slots and counts, below and from the budget on, those that go by their key,
+    // those that stay, and those with the key `prefix`.
+    const int per = (n + NW * 64 - 1) / (NW * 64) * 64, lo = min(n, wave * per), hi = min(n, lo + per);
+    int holes = 0, extras = 0, ties_low = 0, ties_high = 0;
+    for (int j0 = lo; j0 < hi; j0 += 4 * 64) {
+      uint32_t key[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) key[i] = key_of(min(j0 + i * 64 + lane, n - 1));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = j0 + i * 64 + lane;
+        const bool in = j < hi, low = j < p.budget;
+        holes += __popcll(__ballot(in && low && key[i] < prefix));
+        extras += __popcll(__ballot(in && !low && key[i] > prefix));
+        ties_low += __popcll(__ballot(in && low && key[i] == prefix));
+        ties_high += __popcll(__ballot(in && !low && key[i] == prefix));
+      }
+    }
+    __syncthreads();
+    if (lane == 0) counts[0][wave] = ties_low + ties_high;
+    __syncthreads();
+    int tie0 = 0;
+    for (int x = 0; x < wave; ++x) tie0 += counts[0][x];
+    // Of this wave's ties the first `go` go.
+    const int go = min(max(want - tie0, 0), ties_low + ties_high);
+    holes += min(go, ties_low);
+    extras += ties_high - max(go - ties_low, 0);
+    if (lane == 0) {
+      counts[1][wave] = holes;
+      counts[2][wave] = extras;
+    }
+    __syncthreads();
+    int hole = 0, extra = 0, total = 0, tie = tie0;
+    for (int x = 0; x < NW; ++x) {
+      if (x < wave) {
+        hole += counts[1][x];
+        extra += counts[2][x];
+      }
+      total += counts[1][x];
+    }
+    // As many slots are freed below the budget as tokens are kept behind it: the x-th takes the x-th.
+    int2* const pairs = p.counts ? p.moves + static_cast<int64_t>(unit) * p.max_moves : listed;
+    auto before = [](unsigned long long m) {  // lanes of m before this one
+      return static_cast<int>(__builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(m >> 32),
+                                                        __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(m), 0u)));
+    };
+    for (int j0 = lo; j0 < hi; j0 += 4 * 64) {
+      uint32_t keys4[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) keys4[i] = key_of(min(j0 + i * 64 + lane, n - 1));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = j0 + i * 64 + lane;
+        const bool in = j < hi;
+        const uint32_t key = keys4[i];
+        const unsigned long long eq = __ballot(in && key == prefix);
+        const bool out = key < prefix || (key == prefix && tie + before(eq) < want);
+        tie += __popcll(eq);
+        const bool is_hole = in && out && j < p.budget, is_extra = in && !out && j >= p.budget;
+        const unsigned long long hm = __ballot(is_hole), em = __ballot(is_extra);
+        if (is_hole) pairs[hole + before(hm)].x = j;
+        if (is_extra) pairs[extra + before(em)].y = j;
+        hole += __popcll(hm);
+        extra += __popcll(em);
+      }
+    }
+    if (p.counts) {
+      if (tid == 0) p.counts[unit] = total;
+      return;
+    }
+    __syncthreads();
+    for (int x = tid; x < total * vecs; x += NT) move_vector(p, unit, listed[x / vecs], x % vecs);
   };
-  for (int j0 = lo; j0 < hi; j0 += 64) {
-    const int j = j0 + lane;
-    const bool in = j < hi;
-    const uint32_t key = key_of(min(j, n - 1));
-    const unsigned long long eq = __ballot(in && key == prefix);
-    const bool out = key < prefix || (key == prefix && tie + before(eq) < want);
-    tie += __popcll(eq);
-    const bool is_hole = in && out && j < p.budget, is_extra = in && !out && j >= p.budget;
-    const unsigned long long hm = __ballot(is_hole), em = __ballot(is_extra);
-    if (is_hole) pairs[hole + before(hm)].x = j;
-    if (is_extra) pairs[extra + before(em)].y = j;
-    hole += __popcll(hm);
-    extra += __popcll(em);
-  }
-  if (p.counts) {
-    if (tid == 0) p.counts[unit] = total;
-    return;
-  }
-  __syncthreads();
-  for (int x = tid; x < total * vecs; x += NT) move_vector(p, unit, listed[x / vecs], x % vecs);
+  if (n <= KEYS)
+    select(std::true_type{});
+  else
+    select(std::false_type{});
 }
 
 // Workgroups (unit, y): each takes every gridDim.y-th run of 256 vectors of the unit's pairs.
