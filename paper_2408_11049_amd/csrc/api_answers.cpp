@@ -62,6 +62,7 @@ int md_prefix_attn(const md_attn_args* a, const md_prefix* prefix, void* stream)
   p.row_blocks = pl.row_blocks;
   p.own_blocks = pl.own_blocks;
   p.c_pre = pl.c_pre;
+  p.pre_parts = pl.pre_parts;
   p.c_own = pl.c_own;
   p.n_pre = pl.n_pre;
   p.scale_log2 = md::scale_log2(a->sm_scale, a->head_dim);
@@ -73,7 +74,7 @@ int md_prefix_attn(const md_attn_args* a, const md_prefix* prefix, void* stream)
   const bool bf16 = a->dtype == MD_BF16;
   const int rc = md::status(md::launch_prefix_attn(p, pl, a->head_dim, bf16, s));
   if (rc != MD_OK) return rc;
-  return md::status(md::launch_merge_lse(pl.c_pre + pl.c_own, pl.n_rows, a->head_dim, bf16, p.part_o,
+  return md::status(md::launch_merge_lse(pl.pre_parts + pl.c_own, pl.n_rows, a->head_dim, bf16, p.part_o,
                                          p.part_lse, a->o, a->lse, s, true));
 }
 

@@ -5,8 +5,8 @@
 //   prefix_stream  32 query rows of a KV head against a part of a range of keys (of the prefix, or of
 //                  one sequence's own tokens), each wave its own tiles of 32 keys: bound by reading K
 //                  and V.  Own caches always, prefixes of few rows.
-//   prefix_wide    256 rows against a part of the prefix, in tiles that the waves share: bound by the
-//                  matrix and vector units.
+//   prefix_wide    256 or 128 rows against a part of the prefix, in tiles that the waves share: bound by
+//                  the matrix and vector units.
 //
 // Both compute S^T = K Q^T, which leaves a lane one query row: the softmax needs no shuffles but one
 // exchange between the halves of the wave when the running maximum moves, and P^T is in place as the
@@ -289,7 +289,7 @@ prefix_stream_kernel(const PrefixParams p) {
     sum += l_l[w][l32] * f[w];
   }
   const float inv = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
-  const int64_t prow = static_cast<int64_t>(pre ? chunk : p.c_pre + chunk) * p.n_rows + row_g;
+  const int64_t prow = static_cast<int64_t>(pre ? chunk : p.pre_parts + chunk) * p.n_rows + row_g;
 #pragma unroll
   for (int y = 0; y < (CB + 3) / 4; ++y) {
     const int cb = y * 4 + wave;
@@ -306,9 +306,10 @@ prefix_stream_kernel(const PrefixParams p) {
   if (tid < 32) p.part_lse[prow] = part_lse(m, sum);
 }
 
-// The prefix's part for groups of many rows, bf16: 256 rows a workgroup, two tiles of 32 a wave, A
-// and B, so that what a wave reads of K and V from LDS serves twice the products (with 32 rows
-// the reads alone take longer than the matrix instructions).  One wave a SIMD then holds Q, O and S in
+// The prefix's part for groups of many rows, bf16: 256 rows a workgroup (SPLIT: 128, two waves with the
+// first half of every tile's keys and two with the second, which are parts of their own), two tiles
+// of 32 a wave, A and B, so that what a wave reads of K and V from LDS serves twice the products (with
+// 32 rows the reads alone take longer than the matrix instructions).  One wave a SIMD then holds Q, O and S in
 // registers, and hides its vector work behind its own matrix instructions: per 32 keys
 //   S_B = K Q_B^T        beside the softmax of S_A,
 //   O_A += V^T P_A^T     beside the softmax of S_B,
@@ -319,7 +320,7 @@ prefix_stream_kernel(const PrefixParams p) {
 // Tiles of 64 tokens are whole but for the last one of the prefix, which comes after the loop.  In a whole
 // tile a wave's load instruction covers RPW rows of one page (pages hold at least RPW tokens here) at
 // one scalar address and a fixed offset a lane: no address arithmetic in the vector unit.
-template <int D, bool PAGED>
+template <int D, bool PAGED, int SPLIT>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 prefix_wide_kernel(const PrefixParams p) {
   using T = Tile<D, true>;
@@ -334,7 +335,7 @@ prefix_wide_kernel(const PrefixParams p) {
   const int u = (t8 / p.row_blocks) * 8 + (static_cast<int>(blockIdx.x) & 7);
   if (u >= p.P * p.Hkv * p.c_pre) return;
   const int chunk = u % p.c_pre, hk = (u / p.c_pre) % p.Hkv, blk = u / (p.c_pre * p.Hkv);
-  const int row_base = (t8 % p.row_blocks) * kPrefixWideRows, tok0 = blk * p.n * p.L;
+  const int row_base = (t8 % p.row_blocks) * (kPrefixWideRows / SPLIT), tok0 = blk * p.n * p.L;
   const KvView& c = p.pre;
   const int raw_len = uniform(c.lens[blk]);
   const int len = min(max(raw_len, 0), c.max_len);
@@ -347,7 +348,8 @@ prefix_wide_kernel(const PrefixParams p) {
     if (PAGED && t0 < t1) check_pages(c, blk, t0 * KEYS, min(len, t1 * KEYS), p.err);
   }
 
-  const int r0 = row_base + wave * 64;
+  const int r0 = row_base + (SPLIT == 2 ? wave & 1 : wave) * 64;
+  const int j_first = SPLIT == 2 ? wave >> 1 : 0;  // the half of every tile that a wave of two takes
   int64_t row_g[2];
   bool valid[2];
   u32x4 q[2][ST];
@@ -483,7 +485,8 @@ prefix_wide_kernel(const PrefixParams p) {
       load(buf ^ 1, t + 3);
       load_pages(buf ^ 1, t + 5);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int y = 0; y < 2 / SPLIT; ++y) {
+        const int j = SPLIT == 2 ? j_first : y;
         float sum, mx;
         read_v(lds[buf][1] + j * 32 * T::ROW);
         scores(1);
@@ -505,8 +508,9 @@ prefix_wide_kernel(const PrefixParams p) {
           __builtin_amdgcn_sched_group_barrier(0x400, 16 / (2 * CB), 0);
         }
         settle(1, sum, mx);
-        if (j == 1) __syncthreads();  // tile t + 1 is there; this buffer's last reads are done
-        read_k(j == 0 ? lds[buf][0] + 32 * T::ROW : lds[buf ^ 1][0]);
+        const bool last = y == 2 / SPLIT - 1;
+        if (last) __syncthreads();  // tile t + 1 is there; this buffer's last reads are done
+        read_k(last ? lds[buf ^ 1][0] + j_first * 32 * T::ROW : lds[buf][0] + 32 * T::ROW);
         values(1);
         scores(0);
       }
@@ -521,7 +525,7 @@ prefix_wide_kernel(const PrefixParams p) {
     load(0, t0 + 2);
     load_pages(0, t0 + 4);
     __syncthreads();
-    read_k(lds[0][0]);
+    read_k(lds[0][0] + j_first * 32 * T::ROW);
     scores(0);
     for (int t = t0;; t += 2) {
       turn(t, 0);
@@ -553,7 +557,7 @@ prefix_wide_kernel(const PrefixParams p) {
     }
     __syncthreads();
 #pragma unroll 1
-    for (int j = 0; j < 2; ++j) {
+    for (int j = j_first; j < (SPLIT == 2 ? j_first + 1 : 2); ++j) {
       read_k(lds[0][0] + j * 32 * T::ROW);
       read_v(lds[0][1] + j * 32 * T::ROW);
 #pragma unroll
@@ -571,7 +575,7 @@ prefix_wide_kernel(const PrefixParams p) {
   }
 #pragma unroll
   for (int x = 0; x < 2; ++x)
-    if (valid[x]) store_part<D>(p, chunk, row_g[x], half, acc[x], m[x], l[x] + __shfl_xor(l[x], 32));
+    if (valid[x]) store_part<D>(p, SPLIT == 2 ? chunk * 2 + j_first : chunk, row_g[x], half, acc[x], m[x], l[x] + __shfl_xor(l[x], 32));
 }
 
 template <int D, bool BF16>
@@ -580,10 +584,17 @@ hipError_t launch(const PrefixParams& p, const PrefixPlan& pl, hipStream_t s) {
   if constexpr (BF16) {
     if (pl.wide) {
       const dim3 grid(static_cast<uint32_t>(p.n_pre)), block(256);
-      if (p.pre.page_table)
-        hipLaunchKernelGGL((prefix_wide_kernel<D, true>), grid, block, 0, s, p);
-      else
-        hipLaunchKernelGGL((prefix_wide_kernel<D, false>), grid, block, 0, s, p);
+      if (pl.split == 2) {
+        if (p.pre.page_table)
+          hipLaunchKernelGGL((prefix_wide_kernel<D, true, 2>), grid, block, 0, s, p);
+        else
+          hipLaunchKernelGGL((prefix_wide_kernel<D, false, 2>), grid, block, 0, s, p);
+      } else {
+        if (p.pre.page_table)
+          hipLaunchKernelGGL((prefix_wide_kernel<D, true, 1>), grid, block, 0, s, p);
+        else
+          hipLaunchKernelGGL((prefix_wide_kernel<D, false, 1>), grid, block, 0, s, p);
+      }
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
       a.n_pre = 0;  // the own caches are left

@@ -131,14 +131,15 @@ int main() {
                     if (st == MD_ERR_UNSUPPORTED) continue;
                     check(st == MD_OK, "prefix plan", B, T);
                     check(pl.c_pre >= 1 && pl.c_own >= 1 && pl.n_pre + pl.n_own <= kMaxWgs256, "prefix parts", B, T);
-                    check(int64_t{pl.row_blocks} * (pl.wide ? kPrefixWideRows : kPrefixStreamRows) >= pl.group_rows,
+                    check(int64_t{pl.row_blocks} * (pl.wide ? kPrefixWideRows / pl.split : kPrefixStreamRows) >= pl.group_rows,
                           "prefix rows", B, L);
                     check(int64_t{pl.own_blocks} * kPrefixStreamRows >= G * L, "own rows", B, L);
                     check(int64_t{pl.n_pre} >= int64_t{P} * Hkv * pl.c_pre * pl.row_blocks && pl.n_pre % 8 == 0,
                           "prefix workgroups", B, T);
                     check(pl.n_own >= int64_t{B} * Hkv * pl.c_own * pl.own_blocks && pl.n_own % 8 == 0, "own workgroups", B, S);
+                    check(pl.pre_parts == pl.c_pre * pl.split && (pl.wide || pl.split == 1), "prefix split", B, T);
                     check(!pl.wide || (dtype == MD_BF16 && (page == 0 || page >= 4)), "wide", page, dtype);
-                    const size_t parts = static_cast<size_t>(pl.c_pre + pl.c_own) * static_cast<size_t>(pl.n_rows);
+                    const size_t parts = static_cast<size_t>(pl.pre_parts + pl.c_own) * static_cast<size_t>(pl.n_rows);
                     check(pl.part_o_bytes >= parts * 512 && pl.part_lse_bytes >= parts * 4 &&
                               pl.workspace_bytes == pl.part_o_bytes + pl.part_lse_bytes,
                           "prefix workspace", B, T);

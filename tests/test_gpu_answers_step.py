@@ -226,6 +226,10 @@ def test_malformed_tensors(case):
     ("bf16", 4, 2, 128, 3, [3 + i for i in range(18)], [0, 2000], 64, 16), # one of two prefixes empty
     ("bf16", 4, 1, 64, 16, [16] * 5, [129], 0, 0),                         # 320 rows: two blocks
     ("bf16", 1, 1, 128, 1, [1] * 65, [4000], 0, 16),                       # 65 rows, one a sequence
+    ("bf16", 4, 1, 64, 5, [5 + i for i in range(10)], [777], 0, 0),        # 200 rows: one block of 256
+    ("bf16", 4, 1, 64, 5, [5 + i for i in range(10)], [777], 16, 16),
+    ("bf16", 8, 1, 128, 4, [4 + i for i in range(30)], [500], 0, 0),       # 960: four
+    ("bf16", 8, 1, 64, 3, [3] * 16, [31], 16, 16),                         # 384: three of 128
     ("f32", 4, 2, 64, 5, [2000, 5, 700], [3000], 16, 16),
     ("bf16", 4, 1, 128, 3, [3000, 2000, 1000, 4], [1], 16, 16),            # long own caches in parts
 ])
