@@ -23,10 +23,14 @@ struct Tile {
   static constexpr int ES = BF16 ? 2 : 4;
   static constexpr int ROW = D * ES;          // bytes of a row
   static constexpr int CH = ROW / 16;         // 16-byte chunks of a row
-  // Rows sit unpadded, chunk c of row r in place c ^ turn(r): 16 rows at one c, as a wave reads an
-  // operand, then cover all banks.
+  // Rows sit unpadded, chunk c of row r in place c ^ turn(r).  The banks hold 256 bytes, and both ways
+  // of reading cover them all: 16 rows at one c (an operand), and four rows of a multiple of four at
+  // four chunks from a multiple of four on (a transposed operand; turned by r alone, those were half of
+  // the LDS's cycles in conflicts).
   static __device__ __forceinline__ int at(int r, int c) {
-    const int turn = ROW == 128 ? (r >> 1) & 7 : r & 15;
+    const int turn = ROW == 512 ? r & 15
+                   : ROW == 256 ? (r & 3) << 2 | ((r >> 2) & 3)
+                                : ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
     return r * ROW + ((c ^ turn) << 4);
   }
 };
