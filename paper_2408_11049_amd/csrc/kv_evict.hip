@@ -5,7 +5,8 @@
 // One workgroup a (sequence, KV head) finds the key of rank n - budget by a radix select (three
 // rounds over keys in LDS), counts in slot order and lists (freed slot, kept slot) pairs; pairs are
 // moved by the same workgroup or, where a call may have more than kEvictFused of them a head, by a
-// second launch over the whole device.
+// second launch over the whole device.  8 x 8 heads of 16384 .. 32768 tokens cut to 2049: 41 us for the select,
+// bound by its dependent rounds, and 18 for the moves (6.5 TB/s); 64 x 8 of 2054: 10 us in all.
 #include <type_traits>
 
 #include "answers_kernels.h"

