@@ -748,7 +748,7 @@ typedef struct {
  * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers, bad sizes, strides or page
  * geometry, q_len > max_kv_len > slot_stride, mass or slot_pos overlapping each other or an
  * input; MD_ERR_UNSUPPORTED for head_dim not in {64,128}, kv_stride_tok > 2^28
- * elements, max_kv_len > 2^31 - 65, L * G > 2^30, or sizes past the grid's 32 bits (2^24 - 1
+ * elements, max_kv_len > 2^31 - 257, L * G > 2^30, or sizes past the grid's 32 bits (2^24 - 1
  * workgroups); MD_ERR_WORKSPACE; MD_ERR_HIP.
  */
 int md_kv_mass(const md_kv_mass_args* a, void* stream);
@@ -776,7 +776,7 @@ size_t md_kv_mass_workspace_bytes(const md_kv_mass_args* a);
  * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers, a malformed cache, budget < 1,
  * n_sink < 0, recent < 0, n_sink + recent > budget, slot_stride < 1, mass, slot_pos, lens_out or
  * the workspace overlapping an input or each other; MD_ERR_UNSUPPORTED for head_dim not in {64,128},
- * B * Hkv > 2^22 - 1 or slot_stride > 2^31 - 65; MD_ERR_WORKSPACE; MD_ERR_HIP.
+ * B * Hkv > 2^22 - 1 or slot_stride > 2^31 - 2049; MD_ERR_WORKSPACE; MD_ERR_HIP.
  */
 int md_kv_evict(const md_kv_cache* c, float* mass, int32_t* slot_pos, int64_t slot_stride,
                 const int32_t* lens, const int32_t* seq_lens, int32_t budget, int32_t n_sink,

@@ -61,9 +61,14 @@ struct Stream {
     groups = !paged || (1 << page_shift) >= RPW;
     lane_off = static_cast<uint32_t>((lane / T::CH) * s_tok * T::ES + (lane % T::CH) * 16);
   }
+  // This lane's token of tile t, past the end the last one.  Tiles ahead of the last one's end may lie past
+  // 31 bits.
+  __device__ __forceinline__ int token(int t) const {
+    return min(min(t, (end - 1) / KEYS) * KEYS + (lane & 31), end - 1);
+  }
   // The block (sequence or page) of this lane's token of tile t, lane & 31; past the end the last one's.
   __device__ __forceinline__ int load_block(int t) const {
-    const int tok = min(t * KEYS + (lane & 31), end - 1);
+    const int tok = token(t);
     const int id = table[paged ? tok >> page_shift : 0];
     return paged ? id : blk;
   }
@@ -72,7 +77,7 @@ struct Stream {
   __device__ __forceinline__ void load(int t, int block) {
     const bool in_pool = !paged || (block >= 0 && block < num_pages);
     const unsigned long long pool = __ballot(in_pool);
-    const int tok = min(t * KEYS + (lane & 31), end - 1);
+    const int tok = token(t);
     const int64_t row = (static_cast<int64_t>(in_pool ? block : 0) * s_blk +
                          static_cast<int64_t>(paged ? tok & ((1 << page_shift) - 1) : tok) * s_tok + head) * T::ES;
     const int lo = static_cast<int>(row), hi = static_cast<int>(row >> 32);
@@ -84,7 +89,7 @@ struct Stream {
       if constexpr (VALUES) vr[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + byte));
     };
     ok = 0;
-    if (groups && (t + 1) * KEYS <= end) {
+    if (groups && t < end / KEYS) {
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
         get(n, join(__builtin_amdgcn_readlane(lo, n * RPW), __builtin_amdgcn_readlane(hi, n * RPW)) + lane_off);
@@ -95,7 +100,7 @@ struct Stream {
       for (int n = 0; n < NV; ++n) {
         const int of = n * RPW + lane / T::CH;
         get(n, join(__shfl(lo, of), __shfl(hi, of)) + (lane % T::CH) * 16);
-        ok |= static_cast<uint32_t>(t * KEYS + of < end && ((pool >> of) & 1ull)) << n;
+        ok |= static_cast<uint32_t>(t <= (end - 1 - of) / KEYS && of < end && ((pool >> of) & 1ull)) << n;
       }
     }
   }

@@ -179,7 +179,9 @@ int check_mass_sizes(const md_kv_mass_args* a) {
     return MD_ERR_INVALID_ARG;
   if (check_kv_geom(geom(a)) != MD_OK) return MD_ERR_INVALID_ARG;
   if (a->head_dim != 64 && a->head_dim != 128) return MD_ERR_UNSUPPORTED;
-  if (a->kv_stride_tok > kMaxTokStride || a->max_kv_len > kMaxPosition) return MD_ERR_UNSUPPORTED;
+  // (Key blocks of 256 may end past the last token.)
+  if (a->kv_stride_tok > kMaxTokStride || a->max_kv_len > INT32_MAX - kMassPromptKeys)
+    return MD_ERR_UNSUPPORTED;
   const int64_t G = a->num_q_heads / a->num_kv_heads;
   if (G * a->q_len > (1 << 30)) return MD_ERR_UNSUPPORTED;
   const int64_t units = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads;
@@ -259,7 +261,8 @@ int check_evict_sizes(const md_kv_cache* c, int64_t slot_stride, int32_t budget)
   const int64_t heads = c->num_kv_heads;
   if (heads > 1 && c->kv_stride_head < c->head_dim) return MD_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return MD_ERR_UNSUPPORTED;
-  if (slot_stride > kMaxPosition || static_cast<int64_t>(c->num_seqs) * heads > kMaxWgs1024)
+  // (A thread's slots go on by up to 1024.)
+  if (slot_stride > INT32_MAX - 2048 || static_cast<int64_t>(c->num_seqs) * heads > kMaxWgs1024)
     return MD_ERR_UNSUPPORTED;
   return MD_OK;
 }

@@ -138,6 +138,7 @@ BAD_MASS = [
     ("too few columns", dict(MASS_PAGES, max_pages_per_seq=6), INV), ("no pages", dict(MASS_PAGES, num_pages=0), INV),
     ("rows past 2^30", dict(q_len=1 << 29, max_kv_len=1 << 29, slot_stride=1 << 29), UNS),
     ("bound past what can be addressed", dict(max_kv_len=MAX, slot_stride=1 << 33), UNS),
+    ("key blocks past 31 bits", dict(max_kv_len=2 ** 31 - 256, slot_stride=1 << 33), UNS),
     ("workgroups past 2^24", dict(num_seqs=1 << 23), UNS),
     ("mass is slot_pos", dict(slot_pos=D), INV), ("mass over the lse", dict(lse=D + 4), INV),
     ("mass among the keys", dict(mass=B_ + 1024), INV), ("slot_pos over pos0", dict(slot_pos=F), INV),
@@ -199,6 +200,7 @@ BAD_EVICT = [
     *[(f"{n} misaligned", {}, {n: F + 0x1002}, INV) for n in ("mass", "slot_pos", "lens", "seq_lens", "lens_out")],
     ("budget 0", {}, dict(budget=0), INV), ("no slots", {}, dict(slot_stride=0), INV),
     ("slots past what can be addressed", {}, dict(slot_stride=MAX), UNS),
+    ("slots whose successors are", {}, dict(slot_stride=2 ** 31 - 2048), UNS),
     ("sinks below 0", {}, dict(n_sink=-1), INV), ("recent below 0", {}, dict(recent=-1), INV),
     ("more held than kept", {}, dict(n_sink=60, recent=41), INV),
     ("held past 32 bits", {}, dict(n_sink=MAX, recent=MAX), INV),

@@ -334,7 +334,44 @@ def test_logprobs_of_a_large_vocabulary():
     check_logp(x, np.array([V - 1, 4096]), 32, chunks=4)
 
 
-# ---- offsets past 32 bits ----
+# ---- lengths up to the last ones, offsets past 32 bits ----
+
+def test_the_longest_lengths():
+    """2^31 - 65 shared tokens and 2^31 - 257 cached ones, one page of them again and again: token numbers
+    of the tiles read ahead lie past 31 bits."""
+    gen = torch.Generator().manual_seed(4)
+    page, d, n = 1 << 20, 64, 2 ** 31 - 65
+    k, v = (rand(gen, (1, page, 1, d), "bf16") for _ in "kv")
+    k *= 0.1
+    table = torch.zeros((1, 2048), dtype=I32, device=DEV)
+    for rows in (4, 66):                     # a stream, and tiles that waves share
+        q = rand(gen, (rows, 1, 1, d), "bf16")
+        none = torch.zeros(rows, dtype=I32, device=DEV)
+        own = torch.zeros((rows, 8, 1, d), dtype=torch.bfloat16, device=DEV)
+        word = torch.zeros(1, dtype=I32, device=DEV)
+        o, lse = md.md_prefix_attn(q, own, own, none, k, v, ints([n]), prefix_page_table=table, max_prefix_len=n,
+                                   err_word=word)
+        s = q[:, 0, 0].double() @ k[0, :, 0].double().T / 8.0
+        assert int(word) == md.MD_ERRW_SHORT_LEN
+        # 65 of 2^31 keys are missing: 2^-24 of the sum.  A lane adds 2^15 tiles' weights in fp32 (2^-9 at
+        # most), and O two products of bf16 weights each (2^-8 and 2^-9 of mean |v| < 1).
+        assert ((lse[:, 0, 0] - torch.logsumexp(s, 1) - np.log(2048.0)).abs() < 2 ** -8).all()
+        want = torch.softmax(s, 1) @ v[0, :, 0].double()
+        assert (o[:, 0, 0].double() - want).abs().max() < 2 ** -7
+    n = 2 ** 31 - 257
+    q = rand(gen, (1, 3, 2, d), "bf16")
+    mass, pos = torch.zeros((1, 1, n), device=DEV), torch.zeros((1, 1, n), dtype=I32, device=DEV)
+    lse = torch.full((1, 3, 2), 1.0, device=DEV)
+    md.md_kv_mass(q, k, ints([n]), lse, mass, pos, ints([77]), page_table=table, max_kv_len=n)
+    w = torch.exp(q[0].reshape(6, d).float() @ k[0, :, 0].float().T / 8.0 - 1.0).sum(0)
+    for i in (0, 1000, 2046):
+        assert torch.allclose(mass[0, 0, i * page:(i + 1) * page], w, rtol=1e-4)
+    last = mass[0, 0, 2047 * page:]
+    assert torch.allclose(last[:-2], w[: len(last) - 2], rtol=1e-4)     # the last three see fewer rows
+    assert last[-1] < last[-2] or last[-1] < w[len(last) - 1]
+    assert pos[0, 0, -3:].tolist() == [77, 78, 79] and not pos[0, 0, :-3].any()
+
+
 
 def test_offsets_past_32_bits():
     """A page pool of more than 2^31 elements, used at its end; rows of logits as far apart."""
