@@ -129,7 +129,7 @@ mass_step(const MassParams p) {
   if (p.accepted) n_count = min(max(uniform(p.accepted[b]), 0), p.L - 1) + 1;
   const int r_end = n_count * p.G;
 
-  Stream<D, BF16, false> rows(p.c, b, hk, min(S, t1 * 32), lane);  // (the next part is not read ahead)
+  Stream<D, BF16, false, false> rows(p.c, b, hk, min(S, t1 * 32), lane);  // (the next part is not read ahead)
   const int first = t0 + wave;
   const int block = rows.load_block(first);
   int block_next = rows.load_block(first + 4);

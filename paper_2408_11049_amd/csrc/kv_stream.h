@@ -38,8 +38,10 @@ struct Tile {
 // The rows of K (and V) of tokens [.., end) of one (block, KV head), 32 a tile, one tile in a wave's registers
 // on its way.  Every load is issued whatever the tile, so that no branch stands between the loads and their
 // use and those on their way can be counted: a row past the end, or on a page outside the pool, is
-// redirected to one that may be read and staged as zeros.
-template <int D, bool BF16, bool VALUES>
+// redirected to one that may be read and staged as zeros.  CACHED: other workgroups read the same rows
+// soon, else the loads are nontemporal (own caches of 64 x 256 .. 2048 tokens, 5 query tokens: 88 us nontemporal
+// and 98 not with one workgroup a KV head's rows, 131 and 119 with two).
+template <int D, bool BF16, bool VALUES, bool CACHED>
 struct Stream {
   using T = Tile<D, BF16>;
   static constexpr int KEYS = 32, NV = KEYS * T::CH / 64, RPW = 64 / T::CH;  // RPW: rows a load instruction
@@ -85,8 +87,12 @@ struct Stream {
       return static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(b)) << 32) | static_cast<uint32_t>(a));
     };
     auto get = [&](int n, int64_t byte) {
-      kr[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + byte));
-      if constexpr (VALUES) vr[n] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + byte));
+      auto one = [](const unsigned char* x) {
+        const u32x4* const p = reinterpret_cast<const u32x4*>(x);
+        return CACHED ? *p : __builtin_nontemporal_load(p);
+      };
+      kr[n] = one(k + byte);
+      if constexpr (VALUES) vr[n] = one(v + byte);
     };
     ok = 0;
     if (groups && t < end / KEYS) {

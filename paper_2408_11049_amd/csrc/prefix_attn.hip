@@ -104,14 +104,14 @@ struct Places {
   }
 };
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool CACHED>
 __global__ void __launch_bounds__(256)
 // Two workgroups a compute unit; 128 fp32 channels need more than 256 registers.
 __attribute__((amdgpu_waves_per_eu(D == 128 && !BF16 ? 1 : 2)))
 prefix_stream_kernel(const PrefixParams p) {
   using T = Tile<D, BF16>;
   constexpr int KEYS = kPrefixStreamTile;
-  static_assert(KEYS == Stream<D, BF16, true>::KEYS, "tiles of the plan");
+  static_assert(KEYS == Stream<D, BF16, true, CACHED>::KEYS, "tiles of the plan");
   constexpr int ST = T::CH / 2;       // 16-byte operand chunks a lane holds of its row
   constexpr int CB = D / 32;          // blocks of 32 channels
   constexpr int BYTES = KEYS * T::ROW;
@@ -177,7 +177,7 @@ prefix_stream_kernel(const PrefixParams p) {
     const Places<D, BF16> at(lane);
     unsigned char* const kt = lds[wave];
     unsigned char* const vt = lds[wave] + BYTES;
-    Stream<D, BF16, true> rows(c, blk, hk, end, lane);
+    Stream<D, BF16, true, CACHED> rows(c, blk, hk, end, lane);
     const int block = rows.load_block(t0 + wave);
     int block_next = rows.load_block(t0 + wave + 4);
     rows.load(t0 + wave, block);
@@ -604,8 +604,12 @@ hipError_t launch(const PrefixParams& p, const PrefixPlan& pl, hipStream_t s) {
       a.n_pre = 0;  // the own caches are left
     }
   }
-  hipLaunchKernelGGL((prefix_stream_kernel<D, BF16>), dim3(static_cast<uint32_t>(a.n_pre + pl.n_own)), dim3(256),
-                     0, s, a);
+  // Whether workgroups share rows of K and V: the prefix's, where it is in this launch, or the own ones.
+  const dim3 grid(static_cast<uint32_t>(a.n_pre + pl.n_own)), block(256);
+  if ((a.n_pre > 0 && pl.row_blocks > 1) || pl.own_blocks > 1)
+    hipLaunchKernelGGL((prefix_stream_kernel<D, BF16, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((prefix_stream_kernel<D, BF16, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
