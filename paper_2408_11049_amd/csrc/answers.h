@@ -13,9 +13,10 @@
 namespace md {
 
 // Shared-prefix attention: query rows of a workgroup and keys of a tile where the call is bound by
-// reading K and V, and where bf16 groups of more than kPrefixFewRows rows a KV head are by the products.
+// reading K and V, and where bf16 groups of more than kPrefixFewRows rows a KV head, with kPrefixWideTokens
+// tokens of the prefix a workgroup at least, are by the products.
 constexpr int kPrefixStreamRows = 32, kPrefixStreamTile = 32;
-constexpr int kPrefixWideRows = 256, kPrefixWideTile = 64, kPrefixFewRows = 64;
+constexpr int kPrefixWideRows = 256, kPrefixWideTile = 64, kPrefixFewRows = 160, kPrefixWideTokens = 512;
 // Tokens that a page has to hold for the latter: a load instruction's rows.
 constexpr int kPrefixWidePage(int d) { return d == 128 ? 4 : 8; }
 struct PrefixPlan {

@@ -106,17 +106,21 @@ PrefixPlan make_prefix_plan(const md_attn_args* a, const md_prefix* p, int num_c
   const int64_t G = a->num_q_heads / a->num_kv_heads;
   pl.n_rows = static_cast<int64_t>(a->num_seqs) * a->q_len * a->num_q_heads;
   pl.group_rows = static_cast<int32_t>(a->num_seqs / p->num_prefixes * a->q_len * G);
-  pl.wide = a->dtype == MD_BF16 && pl.group_rows > kPrefixFewRows && p->max_len > 0 &&
+  // The wide kernel where its workgroups, one a compute unit, have tiles enough to start and end for.  (8 heads
+  // over 32768 tokens, a call: 160 rows 65 us streamed and 68 wide, 192 rows 72 and 70, 256 rows 87 and 73.
+  // Over 4096: 256 rows 32 and 39, 512 rows 43 and 49.)
+  const int64_t heads = static_cast<int64_t>(p->num_prefixes) * a->num_kv_heads;
+  pl.wide = a->dtype == MD_BF16 && pl.group_rows > kPrefixFewRows &&
+            heads * ceil_div(pl.group_rows, kPrefixWideRows) * p->max_len >= kPrefixWideTokens * cus &&
             (p->page_size == 0 || p->page_size >= kPrefixWidePage(a->head_dim));
   // Workgroups of 128 rows where the last one of 256 would be half empty: their two waves a half of the keys
-  // take 0.56 of the time of four waves with 256 rows, which pays up to seven of them (4 prefixes of up to
-  // 16384 tokens, 128 rows: 76 us became 54; 256 rows would become 63 of 56, 1280 rows 254 of 220).
+  // take 0.56 of the time of four waves with 256 rows, which pays up to seven of them (128 rows over up to
+  // 16384 tokens: 76 us became 54; 256 rows would become 63 of 56, 1280 rows 254 of 220).
   const int64_t halves = ceil_div(pl.group_rows, kPrefixWideRows / 2);
   if (pl.wide && halves % 2 == 1 && halves <= 7) pl.split = 2;
   pl.row_blocks = static_cast<int32_t>(
       ceil_div(pl.group_rows, pl.wide ? kPrefixWideRows / pl.split : kPrefixStreamRows));
   pl.own_blocks = static_cast<int32_t>(ceil_div(G * a->q_len, kPrefixStreamRows));
-  const int64_t heads = static_cast<int64_t>(p->num_prefixes) * a->num_kv_heads;
   const int64_t units = heads * pl.row_blocks;
   const int64_t own = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads * pl.own_blocks;
   // Parts of a range: as many workgroups as the device has places (two a compute unit, of the

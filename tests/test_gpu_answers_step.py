@@ -237,11 +237,23 @@ def test_prefix_kernels(case):
     check_prefix(*case)
 
 
+@pytest.mark.parametrize("case", [
+    # Groups of many rows over long prefixes: tiles that the waves of a workgroup share.
+    ("bf16", 32, 8, 128, 1, [1 + i % 9 for i in range(48)], [16384 + 63], 0, 0),      # 192 rows, a tail of 63
+    ("bf16", 32, 8, 128, 1, [1 + i % 9 for i in range(50)], [16384], 16, 4),          # whole tiles
+    ("bf16", 32, 8, 64, 1, [1 + i % 9 for i in range(64)], [16384 + 65], 16, 8),      # 256 rows
+    ("bf16", 32, 8, 64, 2, [2 + i % 9 for i in range(36)], [16384 + 1], 0, 0),        # 288: three of 128
+    ("bf16", 32, 8, 128, 4, [4 + i % 9 for i in range(34)], [40, 16390], 16, 16),     # 272 and a short one beside
+], ids=["192", "200", "256", "288", "272"])
+def test_prefix_kernel_of_many_rows(case):
+    check_prefix(*case)
+
+
 def test_prefix_wide_rows_of_nan_and_infinity():
     """In tiles of many rows, too, a NaN query reaches its own row alone, and a NaN key every row."""
     gen = torch.Generator().manual_seed(7)
-    own, pre = Cache(gen, [1] * 80, 1, 1, 128, "bf16"), Cache(gen, [700], 700, 1, 128, "bf16")
-    q = rand(gen, (80, 1, 2, 128), "bf16")
+    own, pre = Cache(gen, [1] * 90, 1, 8, 128, "bf16"), Cache(gen, [17000], 17000, 8, 128, "bf16")
+    q = rand(gen, (90, 1, 16, 128), "bf16")
     clean, l0 = md.md_prefix_attn(q, own.k, own.v, own.lens, pre.k, pre.v, pre.lens)
     bad = q.clone()
     bad[33, 0, 1, 5] = float("nan")
@@ -252,7 +264,8 @@ def test_prefix_wide_rows_of_nan_and_infinity():
     k = pre.k.clone()
     k[0, 333, 0, 0] = float("nan")
     o, lse = md.md_prefix_attn(q, own.k, own.v, own.lens, k, pre.v, pre.lens)
-    assert o.isnan().all() and (lse == float("-inf")).all()
+    assert o[:, :, :2].isnan().all() and (lse[:, :, :2] == float("-inf")).all()
+    assert torch.equal(o[:, :, 2:], clean[:, :, 2:]) and torch.equal(lse[:, :, 2:], l0[:, :, 2:])
     huge = (q * 1e4).clamp(-3e4, 3e4)                                      # scores far past the exponential's range
     o, lse = md.md_prefix_attn(huge, own.k, own.v, own.lens, pre.k, pre.v, pre.lens)
     assert torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
@@ -344,7 +357,7 @@ def test_the_longest_lengths():
     k, v = (rand(gen, (1, page, 1, d), "bf16") for _ in "kv")
     k *= 0.1
     table = torch.zeros((1, 2048), dtype=I32, device=DEV)
-    for rows in (4, 66):                     # a stream, and tiles that waves share
+    for rows in (4, 168):                    # a stream, and tiles that waves share
         q = rand(gen, (rows, 1, 1, d), "bf16")
         none = torch.zeros(rows, dtype=I32, device=DEV)
         own = torch.zeros((rows, 8, 1, d), dtype=torch.bfloat16, device=DEV)
@@ -398,8 +411,10 @@ def test_offsets_past_32_bits():
             md.md_kv_mass(q, kk, small.lens, a[1], mass, pos, ints([0, 5, 9]), page_table=tt)
             states.append((mass, pos))
         assert all(torch.equal(x, y) for x, y in zip(*states))
-    many = rand(gen, (3, 1, Hq, d), "bf16").repeat(16, 1, 1, 1)              # 96 rows of a prefix and KV head
-    lens, rep = small.lens.repeat(16), 16
+    # 192 rows of a prefix and KV head, 16400 tokens of it
+    many, lens, rep = rand(gen, (3, 1, Hq, d), "bf16").repeat(32, 1, 1, 1), small.lens.repeat(32), 32
+    pre.lens.fill_(16400)
+    pre.table, ptable = (t[:, :12].repeat(1, 86)[:, :1025].contiguous() for t in (pre.table, ptable))
     a = md.md_prefix_attn(many, small.k, small.v, lens, pre.k, pre.v, pre.lens, page_table=small.table.repeat(rep, 1),
                           prefix_page_table=pre.table)
     b = md.md_prefix_attn(many, k, v, lens, k, v, pre.lens, page_table=table.repeat(rep, 1), prefix_page_table=ptable)
