@@ -123,14 +123,16 @@ PrefixPlan make_prefix_plan(const md_attn_args* a, const md_prefix* p, int num_c
   pl.own_blocks = static_cast<int32_t>(ceil_div(G * a->q_len, kPrefixStreamRows));
   const int64_t units = heads * pl.row_blocks;
   const int64_t own = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads * pl.own_blocks;
-  // Parts of a range: as many workgroups as the device has places (two a compute unit, of the
-  // wide kernel one), of 256 tokens, two tiles a wave, at least; 128 up to one a compute unit.
+  // Parts of a range: as many workgroups as the device has places (two a compute unit; one of the wide kernel
+  // and, by its registers, of fp32 with 128 channels: 4 sequences over 32768 tokens 79 us so, 95 with
+  // two), of 256 tokens, two tiles a wave, at least; 128 up to one a compute unit.
   // (8 sequences of 8 heads over a prefix of 8192: 15.5 us in 16 or 32 parts, 20 in 8, 21 in 64; 2 heads
   // over one of 512, fp32: 8.6 us in 4 parts, 10.9 in 2.  Own caches, 64 x 4 heads of 1024 tokens: 26 us in
   // 1 part, 28 in 2, 35 in 4; 64 x 8: 38, 37, 44.)
-  auto parts = [cus](int64_t len, int64_t n, bool wide) {
+  const bool big = a->dtype == MD_F32 && a->head_dim == 128;
+  auto parts = [cus, big](int64_t len, int64_t n, bool wide) {
     const int64_t once = std::max<int64_t>(cus / std::max<int64_t>(n, 1), 1);
-    const int64_t twice = std::max<int64_t>((wide ? 1 : 2) * cus / std::max<int64_t>(n, 1), 1);
+    const int64_t twice = std::max<int64_t>((wide || big ? 1 : 2) * cus / std::max<int64_t>(n, 1), 1);
     return static_cast<int32_t>(std::max<int64_t>(
         1, std::max(std::min(once, ceil_div(len, 128)), std::min(twice, ceil_div(len, 256)))));
   };
