@@ -186,6 +186,7 @@ logprobs_kernel(const LogpParams p) {
   constexpr int VN = BF16 ? 8 : 4, NV = PL / VN;  // logits of a 16-byte vector, vectors a lane
   __shared__ __attribute__((aligned(16))) Key l_key[4][kList + 8];
   __shared__ int l_n[4];
+  __shared__ int l_bound[4];  // apart from l_n, which a wave without logits writes while others still read these
   __shared__ Stats l_stats[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = static_cast<int>(blockIdx.x) / p.n_segs, seg = static_cast<int>(blockIdx.x) % p.n_segs;
@@ -274,10 +275,10 @@ logprobs_kernel(const LogpParams p) {
           const uint32_t trial = kth | (1u << bit);
           if (__popcll(__ballot(key >= trial)) >= count) kth = trial;
         }
-        if (lane == 0) l_n[wave] = static_cast<int>(kth >> 1);  // in 31 bits, for signed comparisons
+        if (lane == 0) l_bound[wave] = static_cast<int>(kth >> 1);  // in 31 bits, for signed comparisons
         __syncthreads();
-        const int lo = min(min(l_n[0], l_n[1]), min(l_n[2], l_n[3]));
-        const int hi = max(max(l_n[0], l_n[1]), max(l_n[2], l_n[3]));
+        const int lo = min(min(l_bound[0], l_bound[1]), min(l_bound[2], l_bound[3]));
+        const int hi = max(max(l_bound[0], l_bound[1]), max(l_bound[2], l_bound[3]));
         kth = static_cast<uint32_t>(whole ? lo : hi) << 1;
         if (kth > 0x007fffffu)  // above the order of -inf
           list.floor = __uint_as_float((kth >> 31) ? kth & 0x7fffffffu : ~kth);
