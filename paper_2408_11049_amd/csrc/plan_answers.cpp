@@ -240,6 +240,8 @@ int validate_mass(const md_kv_mass_args* a, MassPlan* plan) {
     if (!aligned(x, 4)) return MD_ERR_INVALID_ARG;
   if (!rows_ok(geom(a), a->num_kv_heads, a->head_dim, a->dtype)) return MD_ERR_INVALID_ARG;
   *plan = make_mass_plan(a, device_cu_count());
+  // (The launches as they are padded, which the count of units above does not bound.)
+  if (plan->n_wgs > kMaxWgs256 || plan->reduce_wgs > kMaxWgs256) return MD_ERR_UNSUPPORTED;
   if (plan->workspace_bytes && (!a->workspace || a->workspace_bytes < plan->workspace_bytes ||
                                 !aligned(a->workspace, 256)))
     return MD_ERR_WORKSPACE;
