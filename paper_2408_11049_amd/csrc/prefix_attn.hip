@@ -158,7 +158,11 @@ prefix_stream_kernel(const PrefixParams p) {
   const int end = min(len, t1 * KEYS);
   const bool paged = c.page_table != nullptr;
   if (p.err && row_base == 0 && hk == 0) {
-    if (chunk == 0 && tid == 0) check_length(raw_len, pre ? 0 : p.L, c.max_len, p.err);
+    if (chunk == 0 && tid == 0) {
+      check_length(raw_len, pre ? 0 : p.L, c.max_len, p.err);
+      // Prefixes of no tokens have no workgroup: the first of their sequences looks at the length.
+      if (p.c_pre == 0 && blk % p.n == 0) check_length(p.pre.lens[blk / p.n], 0, 0, p.err);
+    }
     if (paged && t0 < t1) check_pages(c, blk, t0 * KEYS, end, p.err);
   }
 
