@@ -802,7 +802,9 @@ size_t md_kv_evict_workspace_bytes(const md_kv_cache* c, int64_t slot_stride, in
  *   top, top_logprobs  device int32 and fp32 [rows, top_k] out (NULL with top_k = 0)
  *   workspace     >= md_token_logprobs_workspace_bytes() (0: none), 256-byte aligned, any
  *                 contents
- * Every logit is read once; sums are fp32 in a fixed order.
+ * Every logit is read once, and once more by a wave of the kernel that finds too many candidates for the top tokens
+ * among its own (clustered values) or too few (masked ones).  Sums are fp32 in a fixed order; x - lse is (x - max) - ln
+ * sum exp(x - max), so that its error goes by its own size and not by the logits'.
  * Errors: MD_ERR_INVALID_ARG for NULL or misaligned pointers (logits: their element size), rows < 0,
  * vocab outside [1, 2^30], row_stride < vocab (with rows > 1), top_k outside [0, 32], a bad dtype,
  * outputs or the workspace overlapping an input or each other; MD_ERR_UNSUPPORTED for

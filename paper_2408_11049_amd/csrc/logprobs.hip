@@ -1,14 +1,16 @@
 // logprobs.hip -- per row of logits: the log probability of a given token, the entropy and
-// the top_k most likely tokens, from one pass over the row.
+// the top_k most likely tokens, from one pass over the row (see the top tokens for what is read again).
 //
 // A workgroup takes a segment of a row, 256 lanes holding 16 or 32 logits each in
 // registers at a time.  Sums: each lane keeps a maximum m, z = sum exp(x - m) and
-// t = sum exp(x - m) (x - m); lse = m + ln z, entropy = ln z - t / z.  Differences to the maximum
-// are taken before the scaling to log2, so that large logits lose nothing.
+// t = sum exp(x - m) (x - m); a log probability is (x - m) - ln z, the entropy ln z - t / z.  Differences to the
+// maximum are taken before the scaling to log2, and m + ln z, which would be rounded by half a step of m, is never
+// formed, so that large logits lose nothing.
 // Top tokens: with each wave's (top_k / 4)-th largest lane maximum, the least of the four is below
 // top_k logits at least, so only logits from there on are candidates, some twice top_k of them; they go
 // to a list in LDS, which is cut to its best top_k where it would overflow (rows of equal
-// or clustered values).  Candidates are ranked by counting the better ones.
+// or clustered values; those logits are read again).  Where no bound stands, the masked ones are looked for, from
+// memory too.  Candidates are ranked by counting the better ones.
 // Rows of several segments are joined by a second launch.  320 rows of 128256 fp32, top 20: 37 us (4.5 TB/s,
 // vector issue 54%) and 6 for the join; one row of 50001 bf16, top 5: 6.5 and 4.
 #include <float.h>
@@ -77,19 +79,19 @@ __device__ __forceinline__ Stats wave_join(const Stats& s) {
 }
 
 struct Finals {
-  float lse, entropy;
+  float m, lz, entropy;  // lse = m + lz, apart
 };
-// A row of nothing but -inf has lse -inf and entropy 0; a NaN or +inf makes both NaN.
+// A row of nothing but -inf has m -inf and entropy 0; a NaN or +inf makes lz and the entropy NaN.
 __device__ __forceinline__ Finals finals(const Stats& s) {
-  if (s.z != s.z) return Finals{s.z, s.z};
-  if (s.m == -INFINITY) return Finals{-INFINITY, 0.f};
+  if (s.z != s.z) return Finals{s.m, s.z, s.z};
+  if (s.m == -INFINITY) return Finals{-INFINITY, 0.f, 0.f};
   const float lz = __builtin_amdgcn_logf(s.z) * kLn2;
-  return Finals{s.m + lz, lz - s.t / s.z};
+  return Finals{s.m, lz, lz - s.t / s.z};
 }
 // x - lse of a logit: -inf for a masked one, whatever the row.
-__device__ __forceinline__ float log_prob(float x, float lse) {
-  if (lse != lse) return lse;
-  return x == -INFINITY ? -INFINITY : x - lse;
+__device__ __forceinline__ float log_prob(float x, const Finals& f) {
+  if (f.lz != f.lz) return f.lz;
+  return x == -INFINITY ? -INFINITY : (x - f.m) - f.lz;
 }
 
 template <bool BF16>
@@ -346,14 +348,14 @@ logprobs_kernel(const LogpParams p) {
   const Finals f = finals(st);
   if (tid == 0) {
     if (p.tokens)
-      p.logprobs[row] = tok < 0 ? 0.f : (tok < p.vocab ? log_prob(x_tok, f.lse) : NAN);
+      p.logprobs[row] = tok < 0 ? 0.f : (tok < p.vocab ? log_prob(x_tok, f) : NAN);
     if (p.entropy) p.entropy[row] = f.entropy;
   }
   if (K > 0) {
     const int64_t o = static_cast<int64_t>(row) * K;
     best_of(l_key, l_n, K, [&](int r, float v, int i) {
       p.top[o + r] = i;
-      p.top_logprobs[o + r] = log_prob(v, f.lse);
+      p.top_logprobs[o + r] = log_prob(v, f);
     });
     if (tid < K && tid >= total) {
       p.top[o + tid] = -1;
@@ -402,14 +404,14 @@ logprobs_join_kernel(const LogpParams p) {
   const Finals f = finals(join(join(l_stats[0], l_stats[1]), join(l_stats[2], l_stats[3])));
   if (tid == 0) {
     if (p.tokens)
-      p.logprobs[row] = tok < 0 ? 0.f : (tok < p.vocab ? log_prob(x_tok, f.lse) : NAN);
+      p.logprobs[row] = tok < 0 ? 0.f : (tok < p.vocab ? log_prob(x_tok, f) : NAN);
     if (p.entropy) p.entropy[row] = f.entropy;
   }
   if (K > 0) {
     const int64_t o = static_cast<int64_t>(row) * K;
     best_of(l_key, l_n, K, [&](int r, float v, int i) {
       p.top[o + r] = i;
-      p.top_logprobs[o + r] = log_prob(v, f.lse);
+      p.top_logprobs[o + r] = log_prob(v, f);
     });
     const int total = l_n[0] + l_n[1] + l_n[2] + l_n[3];
     if (tid < K && tid >= total) {
