@@ -5,6 +5,7 @@ import torch
 
 import paper_2408_11049_amd as md
 import plain_answers as plain
+from prefix_wide_cases import CASES, Inputs
 from test_gpu_answers import DEV, host, rand
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,39 @@ def test_error_word_without_prefix_tokens():
     assert bits((0, -1)) == md.MD_ERRW_SHORT_LEN
     assert bits((5, -5)) == md.MD_ERRW_LONG_LEN | md.MD_ERRW_SHORT_LEN
     assert bits((0, 0), (20, 9, 21, 2)) == md.MD_ERRW_LONG_LEN
+
+
+def on_device(rows, cap, page, gen):
+    """[n, cap, Hkv, d] or pages in random order and their table, of lists of [S, Hkv, d]; NaN where no token is."""
+    Hkv, d = rows[0].shape[1:]
+    cols = -(-cap // page) if page else 1
+    toks = page or cap
+    t = torch.full((len(rows) * cols, toks, Hkv, d), float("nan"), dtype=torch.bfloat16)
+    table = torch.randperm(len(t), generator=gen).reshape(len(rows), cols) if page else torch.arange(len(t))[:, None]
+    for b, r in enumerate(rows):
+        for c in range(-(-len(r) // toks)):
+            part = r[c * toks:(c + 1) * toks]
+            t[table[b, c], :len(part)] = part
+    return t.to(DEV), table.to(torch.int32).to(DEV) if page else None
+
+
+@pytest.mark.parametrize("name", CASES)
+def test_shared_tiles_of_short_prefixes(name):
+    """Groups of many rows over prefixes that end anywhere in a tile, a half of one and a part, none and one of a
+    tile a part among them; the same bits again."""
+    c = Inputs(name)
+    ints = {n: torch.tensor(x, dtype=torch.int32, device=DEV) for n, x in (("own", c.lens), ("pre", c.plens))}
+    k, table = on_device(c.k, max(c.lens), c.page, torch.Generator().manual_seed(1))
+    v, _ = on_device(c.v, max(c.lens), c.page, torch.Generator().manual_seed(1))
+    pk, ptable = on_device(c.pk, c.bound, c.ppage, torch.Generator().manual_seed(2))
+    pv, _ = on_device(c.pv, c.bound, c.ppage, torch.Generator().manual_seed(2))
+    q = c.q.to(DEV)
+    kw = dict(page_table=table, prefix_page_table=ptable, max_prefix_len=c.bound)
+    o, lse = md.md_prefix_attn(q, k, v, ints["own"], pk, pv, ints["pre"], **kw)
+    again = md.md_prefix_attn(q, k, v, ints["own"], pk, pv, ints["pre"], **kw)
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+    for p in range(len(c.plens)):
+        ro, rl, ob, lb = c.oracle(p)
+        mine = slice(p * c.n, (p + 1) * c.n)
+        eo, el = np.abs(host(o[mine]) - ro), np.abs(host(lse[mine]) - rl)
+        assert (eo <= ob).all() and (el <= lb).all(), (c.plens[p], eo.max(), el.max())
