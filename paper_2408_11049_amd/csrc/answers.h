@@ -21,11 +21,11 @@ constexpr int kPrefixWideRows = 256, kPrefixWideTile = 64, kPrefixFewRows = 160,
 constexpr int kPrefixWidePage(int d) { return d == 128 ? 4 : 8; }
 struct PrefixPlan {
   bool wide = false;
-  int32_t split = 1;        // wide: 2 where the keys of a tile are split between the waves
   int32_t group_rows = 0;   // rows of a (prefix, KV head): B / P * L * G
   int32_t row_blocks = 0, own_blocks = 0;  // of the workgroups' rows: a group's, a sequence's
   int32_t c_pre = 0, c_own = 0;  // parts of the prefix's and of the own keys
-  int32_t pre_parts = 0;    // c_pre * split: results of the prefix a row
+  static constexpr int32_t split = 1;  // results of a part of the prefix a row
+  int32_t pre_parts = 0;    // and of the whole prefix
   int32_t n_pre = 0;        // workgroups of the prefix, padded to whole rounds of the XCDs
   int64_t n_own = 0;        // and of the own caches
   int64_t n_rows = 0;       // B * L * Hq

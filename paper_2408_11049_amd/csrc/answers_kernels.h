@@ -27,7 +27,7 @@ struct PrefixParams {
   const void* q;
   int32_t P, n;               // prefixes, sequences of each
   int32_t L, Hq, Hkv, G;
-  int32_t group_rows, row_blocks, own_blocks, c_pre, pre_parts, c_own, n_pre;
+  int32_t group_rows, row_blocks, own_blocks, c_pre, c_own, n_pre;
   float scale_log2;           // softmax scale * log2(e)
   float* part_o;              // [c_pre + c_own][n_rows][d]
   float* part_lse;            // [c_pre + c_own][n_rows]

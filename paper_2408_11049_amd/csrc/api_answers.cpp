@@ -62,7 +62,6 @@ int md_prefix_attn(const md_attn_args* a, const md_prefix* prefix, void* stream)
   p.row_blocks = pl.row_blocks;
   p.own_blocks = pl.own_blocks;
   p.c_pre = pl.c_pre;
-  p.pre_parts = pl.pre_parts;
   p.c_own = pl.c_own;
   p.n_pre = pl.n_pre;
   p.scale_log2 = md::scale_log2(a->sm_scale, a->head_dim);

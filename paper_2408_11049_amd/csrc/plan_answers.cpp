@@ -113,13 +113,10 @@ PrefixPlan make_prefix_plan(const md_attn_args* a, const md_prefix* p, int num_c
   pl.wide = a->dtype == MD_BF16 && pl.group_rows > kPrefixFewRows &&
             heads * ceil_div(pl.group_rows, kPrefixWideRows) * p->max_len >= kPrefixWideTokens * cus &&
             (p->page_size == 0 || p->page_size >= kPrefixWidePage(a->head_dim));
-  // Workgroups of 128 rows where the last one of 256 would be half empty: their two waves a half of the keys
-  // take 0.56 of the time of four waves with 256 rows, which pays up to seven of them (128 rows over up to
-  // 16384 tokens: 76 us became 54; 256 rows would become 63 of 56, 1280 rows 254 of 220).
-  const int64_t halves = ceil_div(pl.group_rows, kPrefixWideRows / 2);
-  if (pl.wide && halves % 2 == 1 && halves <= 7) pl.split = 2;
-  pl.row_blocks = static_cast<int32_t>(
-      ceil_div(pl.group_rows, pl.wide ? kPrefixWideRows / pl.split : kPrefixStreamRows));
+  // (Workgroups of 128 rows, two waves with a half of each tile's keys, where the last one of 256 is half empty: 320
+  // rows a call over 16384 and 32768 tokens 66 and 99 us for 65 and 98, 576 rows 95 and 148 for 92 and 144, 832 rows
+  // 129 and 209 for 113 and 179; 64 channels at best 2% less.)
+  pl.row_blocks = static_cast<int32_t>(ceil_div(pl.group_rows, pl.wide ? kPrefixWideRows : kPrefixStreamRows));
   pl.own_blocks = static_cast<int32_t>(ceil_div(G * a->q_len, kPrefixStreamRows));
   const int64_t units = heads * pl.row_blocks;
   const int64_t own = static_cast<int64_t>(a->num_seqs) * a->num_kv_heads * pl.own_blocks;
@@ -140,7 +137,7 @@ PrefixPlan make_prefix_plan(const md_attn_args* a, const md_prefix* p, int num_c
   pl.c_own = parts(a->max_kv_len, own, false);
   pl.n_pre = static_cast<int32_t>(ceil_div(heads * pl.c_pre, 8) * 8 * pl.row_blocks);
   if (p->max_len == 0) pl.c_pre = pl.n_pre = 0;
-  pl.pre_parts = pl.c_pre * pl.split;
+  pl.pre_parts = pl.c_pre * PrefixPlan::split;
   pl.n_own = ceil_div(static_cast<int64_t>(a->num_seqs) * pl.c_own, 8) * 8 * a->num_kv_heads * pl.own_blocks;
   const size_t n = static_cast<size_t>(pl.pre_parts + pl.c_own) * static_cast<size_t>(pl.n_rows);
   pl.part_o_bytes = align_up(n * a->head_dim * 4, 256);

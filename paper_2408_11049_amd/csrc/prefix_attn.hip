@@ -5,8 +5,8 @@
 //   prefix_stream  32 query rows of a KV head against a part of a range of keys (of the prefix, or of
 //                  one sequence's own tokens), each wave its own tiles of 32 keys: bound by reading K
 //                  and V.  Own caches always, prefixes of few rows.
-//   prefix_wide    256 or 128 rows against a part of the prefix, in tiles that the waves share: bound by
-//                  the matrix and vector units.
+//   prefix_wide    256 rows against a part of the prefix, in tiles that the waves share: bound by the
+//                  matrix and vector units.
 //
 // 32 query heads on 8 of 128 channels, bf16, 16-token pages: 64 x 5 rows over 32768 shared tokens 196 us
 // (wide, 0.9 PFLOP/s), over 256 .. 2048 own ones 69 us (stream, 4.4 TB/s); 64 x 1 rows 59 us and, of up to
@@ -297,7 +297,7 @@ prefix_stream_kernel(const PrefixParams p) {
     sum += l_l[w][l32] * f[w];
   }
   const float inv = sum > 0.f ? 1.f / sum : (sum == sum ? 0.f : sum);
-  const int64_t prow = static_cast<int64_t>(pre ? chunk : p.pre_parts + chunk) * p.n_rows + row_g;
+  const int64_t prow = static_cast<int64_t>(pre ? chunk : p.c_pre + chunk) * p.n_rows + row_g;
 #pragma unroll
   for (int y = 0; y < (CB + 3) / 4; ++y) {
     const int cb = y * 4 + wave;
@@ -314,10 +314,9 @@ prefix_stream_kernel(const PrefixParams p) {
   if (tid < 32) p.part_lse[prow] = part_lse(m, sum);
 }
 
-// The prefix's part for groups of many rows, bf16: 256 rows a workgroup (SPLIT: 128, two waves with the
-// first half of every tile's keys and two with the second, which are parts of their own), two tiles
-// of 32 a wave, A and B, so that what a wave reads of K and V from LDS serves twice the products (with
-// 32 rows the reads alone take longer than the matrix instructions).  One wave a SIMD then holds Q, O and S in
+// The prefix's part for groups of many rows, bf16: 256 rows a workgroup, two tiles of 32 a wave, A and B, so that
+// what a wave reads of K and V from LDS serves twice the products (with 32 rows the reads alone take longer
+// than the matrix instructions).  One wave a SIMD then holds Q, O and S in
 // registers, and hides its vector work behind its own matrix instructions: per 32 keys
 //   S_B = K Q_B^T        beside the softmax of S_A,
 //   O_A += V^T P_A^T     beside the softmax of S_B,
@@ -328,7 +327,7 @@ prefix_stream_kernel(const PrefixParams p) {
 // Tiles of 64 tokens are whole but for the last one of the prefix, which comes after the loop.  In a whole
 // tile a wave's load instruction covers RPW rows of one page (pages hold at least RPW tokens here) at
 // one scalar address and a fixed offset a lane: no address arithmetic in the vector unit.
-template <int D, bool PAGED, int SPLIT>
+template <int D, bool PAGED>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 prefix_wide_kernel(const PrefixParams p) {
   using T = Tile<D, true>;
@@ -343,7 +342,7 @@ prefix_wide_kernel(const PrefixParams p) {
   const int u = (t8 / p.row_blocks) * 8 + (static_cast<int>(blockIdx.x) & 7);
   if (u >= p.P * p.Hkv * p.c_pre) return;
   const int chunk = u % p.c_pre, hk = (u / p.c_pre) % p.Hkv, blk = u / (p.c_pre * p.Hkv);
-  const int row_base = (t8 % p.row_blocks) * (kPrefixWideRows / SPLIT), tok0 = blk * p.n * p.L;
+  const int row_base = (t8 % p.row_blocks) * kPrefixWideRows, tok0 = blk * p.n * p.L;
   const KvView& c = p.pre;
   const int raw_len = uniform(c.lens[blk]);
   const int len = min(max(raw_len, 0), c.max_len);
@@ -356,8 +355,7 @@ prefix_wide_kernel(const PrefixParams p) {
     if (PAGED && t0 < t1) check_pages(c, blk, t0 * KEYS, min(len, t1 * KEYS), p.err);
   }
 
-  const int r0 = row_base + (SPLIT == 2 ? wave & 1 : wave) * 64;
-  const int j_first = SPLIT == 2 ? wave >> 1 : 0;  // the half of every tile that a wave of two takes
+  const int r0 = row_base + wave * 64;
   int64_t row_g[2];
   bool valid[2];
   u32x4 q[2][ST];
@@ -493,8 +491,7 @@ prefix_wide_kernel(const PrefixParams p) {
       load(buf ^ 1, t + 3);
       load_pages(buf ^ 1, t + 5);
 #pragma unroll
-      for (int y = 0; y < 2 / SPLIT; ++y) {
-        const int j = SPLIT == 2 ? j_first : y;
+      for (int j = 0; j < 2; ++j) {
         float sum, mx;
         read_v(lds[buf][1] + j * 32 * T::ROW);
         scores(1);
@@ -516,9 +513,8 @@ prefix_wide_kernel(const PrefixParams p) {
           __builtin_amdgcn_sched_group_barrier(0x400, 16 / (2 * CB), 0);
         }
         settle(1, sum, mx);
-        const bool last = y == 2 / SPLIT - 1;
-        if (last) __syncthreads();  // tile t + 1 is there; this buffer's last reads are done
-        read_k(last ? lds[buf ^ 1][0] + j_first * 32 * T::ROW : lds[buf][0] + 32 * T::ROW);
+        if (j == 1) __syncthreads();  // tile t + 1 is there; this buffer's last reads are done
+        read_k(j == 1 ? lds[buf ^ 1][0] : lds[buf][0] + 32 * T::ROW);
         values(1);
         scores(0);
       }
@@ -533,7 +529,7 @@ prefix_wide_kernel(const PrefixParams p) {
     load(0, t0 + 2);
     load_pages(0, t0 + 4);
     __syncthreads();
-    read_k(lds[0][0] + j_first * 32 * T::ROW);
+    read_k(lds[0][0]);
     scores(0);
     for (int t = t0;; t += 2) {
       turn(t, 0);
@@ -565,7 +561,7 @@ prefix_wide_kernel(const PrefixParams p) {
     }
     __syncthreads();
 #pragma unroll 1
-    for (int j = j_first; j < (SPLIT == 2 ? j_first + 1 : 2); ++j) {
+    for (int j = 0; j < 2; ++j) {
       read_k(lds[0][0] + j * 32 * T::ROW);
       read_v(lds[0][1] + j * 32 * T::ROW);
 #pragma unroll
@@ -583,7 +579,7 @@ prefix_wide_kernel(const PrefixParams p) {
   }
 #pragma unroll
   for (int x = 0; x < 2; ++x)
-    if (valid[x]) store_part<D>(p, SPLIT == 2 ? chunk * 2 + j_first : chunk, row_g[x], half, acc[x], m[x], l[x] + __shfl_xor(l[x], 32));
+    if (valid[x]) store_part<D>(p, chunk, row_g[x], half, acc[x], m[x], l[x] + __shfl_xor(l[x], 32));
 }
 
 template <int D, bool BF16>
@@ -592,17 +588,10 @@ hipError_t launch(const PrefixParams& p, const PrefixPlan& pl, hipStream_t s) {
   if constexpr (BF16) {
     if (pl.wide) {
       const dim3 grid(static_cast<uint32_t>(p.n_pre)), block(256);
-      if (pl.split == 2) {
-        if (p.pre.page_table)
-          hipLaunchKernelGGL((prefix_wide_kernel<D, true, 2>), grid, block, 0, s, p);
-        else
-          hipLaunchKernelGGL((prefix_wide_kernel<D, false, 2>), grid, block, 0, s, p);
-      } else {
-        if (p.pre.page_table)
-          hipLaunchKernelGGL((prefix_wide_kernel<D, true, 1>), grid, block, 0, s, p);
-        else
-          hipLaunchKernelGGL((prefix_wide_kernel<D, false, 1>), grid, block, 0, s, p);
-      }
+      if (p.pre.page_table)
+        hipLaunchKernelGGL((prefix_wide_kernel<D, true>), grid, block, 0, s, p);
+      else
+        hipLaunchKernelGGL((prefix_wide_kernel<D, false>), grid, block, 0, s, p);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
       a.n_pre = 0;  // the own caches are left

@@ -1,5 +1,5 @@
 """Calls of md_prefix_attn whose groups of many rows share short prefixes in the tiles that the waves of a workgroup
-share, and their float64 oracle.  Tiles hold 64 keys, in halves of 32.
+share, and their float64 oracle.  Tiles hold 64 keys, in blocks of 32.
 
 Each row looks for one key (its weight there is most of the row's: the keys at tile ends, part ends and the
 last ones, in turn), or away from all of them (each of its scores is near -8, so that a key that is none, of score 0,
@@ -10,25 +10,25 @@ import torch
 import plain_answers as plain
 
 # name: Hq, Hkv, d, L, sequences a prefix, own page, prefix page, bound on the prefixes, their lengths;
-# what the plan has to be at 256 compute units: halves of a tile's keys a wave, parts of a prefix.
+# the parts of a prefix that the plan has to make at 256 compute units.
 ONE_PART = [520, 519, 513, 512, 511, 449, 448, 447, 385, 384, 321, 320, 319, 257, 256, 255, 200, 193, 192, 191, 130, 129,
             128, 127, 97, 96, 65, 64, 63, 33, 1, 0]
 CASES = {
-    "one part, 168 rows": ((64, 8, 128, 3, 7, 0, 0, 520, ONE_PART), 1, 1),
-    "one part, 168 rows, pages of 4": ((64, 8, 128, 3, 7, 16, 4, 520, ONE_PART), 1, 1),
-    "one part, 240 rows, 64 channels, pages of 8": ((32, 8, 64, 4, 15, 16, 8, 520, ONE_PART), 1, 1),
-    "eight parts, 200 rows": ((32, 8, 128, 2, 25, 16, 16, 4096, [4096, 517, 2049, 4033]), 1, 8),
-    "eight parts, 200 rows, 64 channels": ((32, 8, 64, 2, 25, 0, 0, 4096, [1087, 4095, 577, 576]), 1, 8),
-    "four parts, 960 rows": ((64, 8, 128, 8, 15, 0, 16, 2048, [2047, 130]), 1, 4),
-    "halves, one part, 264 rows": ((32, 8, 128, 2, 33, 0, 0, 1024, [1024, 993, 961, 959, 97, 33, 32, 0]), 2, 1),
-    "halves, one part, 384 rows, 64 channels": ((32, 8, 64, 4, 24, 16, 16, 1024, [1023, 992, 129, 96, 65, 64, 31, 1]), 2, 1),
-    "halves, ten parts, 288 rows": ((32, 8, 128, 4, 18, 16, 16, 8192, [700]), 2, 10),
-    "halves, ten parts, 288 rows, 64 channels": ((32, 8, 64, 4, 18, 0, 0, 8192, [2015]), 2, 10),
+    "one part, 168 rows": ((64, 8, 128, 3, 7, 0, 0, 520, ONE_PART), 1),
+    "one part, 168 rows, pages of 4": ((64, 8, 128, 3, 7, 16, 4, 520, ONE_PART), 1),
+    "one part, 240 rows, 64 channels, pages of 8": ((32, 8, 64, 4, 15, 16, 8, 520, ONE_PART), 1),
+    "eight parts, 200 rows": ((32, 8, 128, 2, 25, 16, 16, 4096, [4096, 517, 2049, 4033]), 8),
+    "eight parts, 200 rows, 64 channels": ((32, 8, 64, 2, 25, 0, 0, 4096, [1087, 4095, 577, 576]), 8),
+    "four parts, 960 rows": ((64, 8, 128, 8, 15, 0, 16, 2048, [2047, 130]), 4),
+    "two parts, 264 rows": ((32, 8, 128, 2, 33, 0, 0, 1024, [1024, 993, 961, 959, 97, 33, 32, 0]), 2),
+    "two parts, 384 rows, 64 channels": ((32, 8, 64, 4, 24, 16, 16, 1024, [1023, 992, 129, 96, 65, 64, 31, 1]), 2),
+    "sixteen parts, 288 rows": ((32, 8, 128, 4, 18, 16, 16, 8192, [700]), 16),
+    "sixteen parts, 288 rows, 64 channels": ((32, 8, 64, 4, 18, 0, 0, 8192, [2015]), 16),
 }
 
 
 def edges(T, parts):
-    """Keys at which tiles, halves of them and parts of a prefix of T tokens begin and end."""
+    """Keys at which tiles, blocks and parts of a prefix of T tokens begin and end."""
     tiles = -(-T // 64)
     at = [tiles * c // parts * 64 for c in range(1, parts)]
     at += [32, 64, 128, T // 64 * 64, T // 32 * 32, T // 64 * 64 - 64, T]
@@ -40,7 +40,7 @@ class Inputs:
     """Host tensors: q [B, L, Hq, d], and the rows of own caches and prefixes, bf16, as lists of [S, Hkv, d]."""
 
     def __init__(self, name):
-        (self.Hq, self.Hkv, self.d, self.L, self.n, self.page, self.ppage, self.bound, self.plens), self.split, self.parts = CASES[name]
+        (self.Hq, self.Hkv, self.d, self.L, self.n, self.page, self.ppage, self.bound, self.plens), self.parts = CASES[name]
         gen = torch.Generator().manual_seed(len(name))
         self.B, G = self.n * len(self.plens), self.Hq // self.Hkv
         self.lens = [self.L + b % 9 for b in range(self.B)]

@@ -1,4 +1,4 @@
-// Prints the plan of md_prefix_attn at 256 compute units: wide, split, parts of the prefix
+// Prints the plan of md_prefix_attn at 256 compute units: wide, parts of the prefix
 // (tests/test_prefix_wide_plans.py).  Arguments: B P L Hq Hkv d, the own and the prefix's page size, the bound on the prefix.
 #include <stdio.h>
 #include <stdlib.h>
@@ -36,6 +36,6 @@ int main(int argc, char** argv) {
   p.num_pages = 1;
   if (md::check_prefix_sizes(&a, &p) != MD_OK) return 1;
   const md::PrefixPlan pl = md::make_prefix_plan(&a, &p, 256);
-  printf("%d %d %d\n", pl.wide, pl.split, pl.c_pre);
+  printf("%d %d\n", pl.wide, pl.c_pre);
   return 0;
 }

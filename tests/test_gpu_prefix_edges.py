@@ -58,7 +58,7 @@ def on_device(rows, cap, page, gen):
 
 @pytest.mark.parametrize("name", CASES)
 def test_shared_tiles_of_short_prefixes(name):
-    """Groups of many rows over prefixes that end anywhere in a tile, a half of one and a part, none and one of a
+    """Groups of many rows over prefixes that end anywhere in a tile, a block of one and a part, none and one of a
     tile a part among them; the same bits again."""
     c = Inputs(name)
     ints = {n: torch.tensor(x, dtype=torch.int32, device=DEV) for n, x in (("own", c.lens), ("pre", c.plens))}

@@ -1,4 +1,4 @@
-"""Without a GPU: the cases of tests/prefix_wide_cases.py reach the tiles that waves share, split as they say, and their
+"""Without a GPU: the cases of tests/prefix_wide_cases.py reach the tiles that waves share, in as many parts as they say, and their
 inputs tell a key too few, too many or counted twice from a rounding."""
 import os
 import subprocess
@@ -23,15 +23,15 @@ def driver(tmp_path_factory):
 
 @pytest.mark.parametrize("name", CASES)
 def test_plan_of_the_case(driver, name):
-    (Hq, Hkv, d, L, n, page, ppage, bound, plens), split, parts = CASES[name]
+    (Hq, Hkv, d, L, n, page, ppage, bound, plens), parts = CASES[name]
     out = subprocess.run([driver, *map(str, (n * len(plens), len(plens), L, Hq, Hkv, d, page, ppage, bound))],
                          capture_output=True, text=True, check=True).stdout
-    assert out.split() == ["1", str(split), str(parts)]
+    assert out.split() == ["1", str(parts)]
     assert max(plens) <= bound
 
 
 @pytest.mark.parametrize("name,prefixes", [("one part, 240 rows, 64 channels, pages of 8", (2, 16, 29)),
-                                           ("halves, ten parts, 288 rows", (0,)), ("eight parts, 200 rows", (1,))])
+                                           ("sixteen parts, 288 rows", (0,)), ("eight parts, 200 rows", (1,))])
 def test_wrong_keys_are_told_from_roundings(name, prefixes):
     """The oracle with one key left out, one counted twice, or a key of zeros behind the last: at every edge some row
     is out of its bounds on o, and some on lse."""
