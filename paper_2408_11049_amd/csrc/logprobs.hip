@@ -11,8 +11,8 @@
 // to a list in LDS, which is cut to its best top_k where it would overflow (rows of equal
 // or clustered values; those logits are read again).  Where no bound stands, the masked ones are looked for, from
 // memory too.  Candidates are ranked by counting the better ones.
-// Rows of several segments are joined by a second launch.  320 rows of 128256 fp32, top 20: 37 us (4.5 TB/s,
-// vector issue 54%) and 6 for the join; one row of 50001 bf16, top 5: 6.5 and 4.
+// Rows of several segments are joined by a second launch.  320 rows of 128256 fp32, top 20: 36 us (4.6 TB/s,
+// vector issue 54%) and 6 for the join, 41 a call, of bf16 38; one row of 50001 bf16, top 5: 6.5 and 4.
 #include <float.h>
 
 #include "answers_kernels.h"

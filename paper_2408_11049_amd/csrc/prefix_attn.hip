@@ -8,9 +8,9 @@
 //   prefix_wide    256 rows against a part of the prefix, in tiles that the waves share: bound by the
 //                  matrix and vector units.
 //
-// 32 query heads on 8 of 128 channels, bf16, 16-token pages: 64 x 5 rows over 32768 shared tokens 196 us
-// (wide, 0.9 PFLOP/s), over 256 .. 2048 own ones 69 us (stream, 4.4 TB/s); 64 x 1 rows 59 us and, of up to
-// 1024, 38 us; 8 x 1 rows over 8001 and up to 301 in one launch of the stream 15 us.
+// 32 query heads on 8 of 128 channels, bf16, 16-token pages: 64 x 5 rows over 32768 shared tokens 190 us
+// (wide, 0.9 PFLOP/s), over 256 .. 2048 own ones 70 us (stream, 4.3 TB/s); 64 x 1 rows 57 us and, of up to
+// 1024, 40 us; 8 x 1 rows over 8001 and up to 301 in one launch of the stream 16 us.
 //
 // Both compute S^T = K Q^T, which leaves a lane one query row: the softmax needs no shuffles but one
 // exchange between the halves of the wave when the running maximum moves, and P^T is in place as the
